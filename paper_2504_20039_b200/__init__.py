@@ -4,3 +4,4 @@ from .binding import (  # noqa: F401
     AJ_OK, AJ_ERR_INVALID_ARG, AJ_ERR_UNSUPPORTED, AJ_ERR_WORKSPACE, AJ_ERR_CUDA, AJ_ERR_TIMEOUT, AJ_ERR_NOT_SM100,
     AjError, Handle, lib, status_string, version, verify_static, AJ_STATIC_MAX_ROWS, pair_schedule, shard_exchange_bytes, shard_exchange_alloc, shard_exchange_free, shard_range, ipc_export, ipc_import, ipc_close, lr_fit, lr_release,
 )
+from .kv import AJ_KV_FLAG_FORCE_SIMT, KvHandle  # noqa: F401

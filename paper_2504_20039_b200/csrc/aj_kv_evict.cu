@@ -1,0 +1,290 @@
+// Eviction from the cache by accumulated attention weight.
+//
+// Per (sequence, key head) with more than `keep` slots: keep the `keep` largest keys, where a key is the weight's
+// order-preserving integer image (the largest integer for the protected first and newest tokens, zero for NaN),
+// lower slots first among equals; then move the r-th kept slot past `keep` into the r-th dropped slot below it.
+// Sources lie at or past `keep` and destinations below it, so the moves touch disjoint slots and need no order.
+//
+// A cluster of CTAs serves one (sequence, head): each selects for itself (a radix select of four 8-bit digits over
+// keys in shared memory reads 8 bytes per slot, from L2 but for the first) and then makes its share of the moves,
+// which are what costs: 4 * D elements read or written per moved slot.  With few (sequence, head) pairs a
+// larger cluster spreads them over the SMs.  Nothing is written before every CTA of the cluster has selected, so the
+// state arrays may be updated in place.
+#include "aj_kv.cuh"
+
+namespace aj {
+namespace kv {
+
+namespace {
+
+constexpr int THREADS = 1024, NWARP = THREADS / 32;
+constexpr int LIST = 4096;             // moves a CTA lists at a time
+constexpr int KEYS_MAX = 40 * 1024;    // slots whose keys fit in shared memory; longer ones re-read the weights
+constexpr int HIST = 8;                // copies of the histogram, so that equal digits of a warp group do not queue up
+
+struct Shared {
+    unsigned hist[HIST][256];
+    unsigned scan[NWARP + 1], scan2[NWARP + 1];
+    int newest, need;
+    unsigned prefix;
+};
+
+__device__ inline unsigned warp_sum(unsigned x) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+    return x;
+}
+
+// Exclusive prefix over the warps of one value per warp; scan[NWARP] gets the total.
+__device__ inline void scan_warps(unsigned *scan, unsigned mine) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) scan[warp] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        unsigned x = scan[lane], y = x;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned z = __shfl_up_sync(~0u, y, o);
+            if (lane >= o) y += z;
+        }
+        scan[lane] = y - x;
+        if (lane == 31) scan[NWARP] = y;
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap) {
+    extern __shared__ __align__(16) unsigned dyn[];
+    __shared__ Shared sh;
+    const View &v = a.v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = blockIdx.x % n_split, item = blockIdx.x / n_split;
+    const int h = item % v.Hkv, b = item / v.Hkv;
+    const int L = min(max(__ldg(v.lens + b), 0), v.cap), keep = a.keep;
+    const size_t at = (size_t)item * v.cap;
+    const float *w_in = a.weight + at;
+    const int *p_in = a.slot_pos + at;
+
+    // The new length is written once every CTA of this sequence has read the old one (they may be one array).
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const unsigned total = (unsigned)v.Hkv * n_split;
+        __threadfence();
+        if (atomicInc(counters + b, total - 1) == total - 1) a.lens_out[b] = min(L, keep);
+    }
+    if (L <= keep) {  // the same for the whole cluster
+        for (int j = part * THREADS + threadIdx.x; j < L; j += n_split * THREADS) {
+            if (a.weight_out != a.weight) a.weight_out[at + j] = w_in[j];
+            if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = p_in[j];
+        }
+        return;
+    }
+
+    const int n_words = (L + 31) >> 5;
+    unsigned *list = dyn;                  // [2][LIST] holes, movers
+    unsigned *kept = dyn + 2 * LIST;       // [ceil(cap / 32)] one bit per slot
+    unsigned *keys = kept + ((v.cap + 31) >> 5);
+    const bool cached = L <= keys_cap;
+
+    if (threadIdx.x == 0) {
+        sh.newest = -0x7fffffff - 1;
+        sh.prefix = 0;
+        sh.need = keep;
+    }
+    __syncthreads();
+    int newest = -0x7fffffff - 1;
+    for (int j = threadIdx.x; j < L; j += THREADS) newest = max(newest, __ldcg(p_in + j));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
+    if (lane == 0) atomicMax(&sh.newest, newest);
+    __syncthreads();
+    const long long recent_from = (long long)sh.newest - a.recent;
+    auto make_key = [&](int j) -> unsigned {
+        const int p = __ldcg(p_in + j);
+        const float w = __ldcg(w_in + j);
+        if (p < a.sinks || p > recent_from) return 0xffffffffu;
+        return w != w ? 0u : ordered_image(w);
+    };
+    auto key_at = [&](int j) -> unsigned { return cached ? keys[j] : make_key(j); };
+    if (cached) {
+        for (int j = threadIdx.x; j < L; j += THREADS) keys[j] = make_key(j);
+    }
+
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < HIST * 256; i += THREADS) (&sh.hist[0][0])[i] = 0;
+        __syncthreads();
+        const unsigned prefix = sh.prefix, high = shift == 24 ? 0u : ~0u << (shift + 8);
+        for (int j = threadIdx.x; j < L; j += THREADS) {
+            const unsigned k = key_at(j);
+            if (((k ^ prefix) & high) == 0) atomicAdd(&sh.hist[warp % HIST][(k >> shift) & 255], 1u);
+        }
+        __syncthreads();
+        if (warp == 0) {
+            // lane i holds digits 255 - 8 i .. 248 - 8 i, from the top
+            unsigned c[8], mine = 0;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                c[i] = 0;
+#pragma unroll
+                for (int r = 0; r < HIST; r++) c[i] += sh.hist[r][255 - 8 * lane - i];
+                mine += c[i];
+            }
+            unsigned up = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned z = __shfl_up_sync(~0u, up, o);
+                if (lane >= o) up += z;
+            }
+            unsigned before = up - mine;
+            const unsigned need = (unsigned)sh.need;
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                if (before < need && need <= before + c[i]) {
+                    sh.prefix = prefix | ((unsigned)(255 - 8 * lane - i) << shift);
+                    sh.need = (int)(need - before);
+                }
+                before += c[i];
+            }
+        }
+        __syncthreads();
+    }
+    const unsigned thr = sh.prefix, need = (unsigned)sh.need;
+
+    // one bit per slot: kept.  A warp takes a run of words; among keys equal to the threshold the lowest slots stay
+    const int run = (n_words + NWARP - 1) / NWARP;
+    const int w0 = warp * run, w1 = min(n_words, w0 + run);
+    unsigned eq = 0;
+    for (int w = w0; w < w1; w++) {
+        const int j = w * 32 + lane;
+        const unsigned k = j < L ? key_at(j) : 0u;
+        const unsigned gt = __ballot_sync(~0u, j < L && k > thr), e = __ballot_sync(~0u, j < L && k == thr);
+        if (lane == 0) kept[w] = gt;
+        eq += __popc(e);
+    }
+    scan_warps(sh.scan, eq);
+    unsigned rank = sh.scan[warp];
+    for (int w = w0; w < w1 && rank < need; w++) {
+        const int j = w * 32 + lane;
+        const unsigned k = j < L ? key_at(j) : 0u;
+        const unsigned e = __ballot_sync(~0u, j < L && k == thr);
+        const bool mine = (e >> lane & 1) && rank + __popc(e & ((1u << lane) - 1)) < need;
+        const unsigned add = __ballot_sync(~0u, mine);
+        if (lane == 0) kept[w] |= add;
+        rank += __popc(e);
+    }
+    __syncthreads();
+
+    auto below = [&](int w) -> unsigned {  // bits of word w whose slot lies below keep
+        const int n = keep - w * 32;
+        return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+    };
+    auto valid = [&](int w) -> unsigned {
+        const int n = L - w * 32;
+        return n >= 32 ? ~0u : (1u << n) - 1;
+    };
+    unsigned holes = 0, movers = 0;
+    for (int w = w0 + lane; w < w1; w += 32) {
+        holes += __popc(~kept[w] & below(w));
+        movers += __popc(kept[w] & ~below(w) & valid(w));
+    }
+    scan_warps(sh.scan, warp_sum(holes));
+    scan_warps(sh.scan2, warp_sum(movers));
+    const int n_moves = (int)sh.scan2[NWARP];  // as many holes as movers
+    const int share = (n_moves + n_split - 1) / n_split;
+    const int m0 = part * share, m1 = min(n_moves, m0 + share);
+
+    // every CTA of the cluster is done reading the weights and positions
+    if (n_split > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    if (a.weight_out != a.weight || a.slot_pos_out != a.slot_pos) {
+        for (int j = part * THREADS + threadIdx.x; j < keep; j += n_split * THREADS) {
+            if (kept[j >> 5] >> (j & 31) & 1) {
+                if (a.weight_out != a.weight) a.weight_out[at + j] = __ldcg(w_in + j);
+                if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = __ldcg(p_in + j);
+            }
+        }
+    }
+    const int n16 = v.D * a.elem / 16;  // 16-byte pieces of a row
+    for (int c0 = m0; c0 < m1; c0 += LIST) {
+        const int c1 = min(m1, c0 + LIST);
+        unsigned hr = sh.scan[warp], mr = sh.scan2[warp];
+        for (int w = w0; w < w1; w += 32) {  // 32 words at a time, one per lane
+            const int wl = w + lane;
+            unsigned hb = 0, mb = 0;
+            if (wl < w1) {
+                hb = ~kept[wl] & below(wl);
+                mb = kept[wl] & ~below(wl) & valid(wl);
+            }
+            unsigned hs = __popc(hb), ms = __popc(mb);
+            const unsigned hc = hs, mc = ms;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned x = __shfl_up_sync(~0u, hs, o), y = __shfl_up_sync(~0u, ms, o);
+                if (lane >= o) {
+                    hs += x;
+                    ms += y;
+                }
+            }
+            int r = (int)(hr + hs - hc);
+            for (; hb; hb &= hb - 1, r++)
+                if (r >= c0 && r < c1) list[r - c0] = wl * 32 + __ffs(hb) - 1;
+            r = (int)(mr + ms - mc);
+            for (; mb; mb &= mb - 1, r++)
+                if (r >= c0 && r < c1) list[LIST + r - c0] = wl * 32 + __ffs(mb) - 1;
+            hr += __shfl_sync(~0u, hs, 31);
+            mr += __shfl_sync(~0u, ms, 31);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < c1 - c0; i += THREADS) {
+            const int dst = list[i], src = list[LIST + i];
+            a.weight_out[at + dst] = __ldcg(w_in + src);
+            a.slot_pos_out[at + dst] = __ldcg(p_in + src);
+        }
+        const int pieces = (c1 - c0) * n16;
+        for (int i = threadIdx.x; i < pieces; i += THREADS) {
+            const int r = i / n16, c = i - r * n16;
+            const int dst = list[r], page = __ldg(v.table + (size_t)b * v.width + (dst >> v.page_shift));
+            if ((unsigned)page >= (unsigned)v.n_pages) continue;  // not in the pool: never written
+            const size_t from = page_row(v, b, h, list[LIST + r]) * n16 + c;
+            const size_t to = (((size_t)page * v.Hkv + h) * v.page + (dst & (v.page - 1))) * n16 + c;
+            const uint4 x = __ldcg((const uint4 *)a.k_pages + from), y = __ldcg((const uint4 *)a.v_pages + from);
+            ((uint4 *)a.k_pages)[to] = x;
+            ((uint4 *)a.v_pages)[to] = y;
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s) {
+    const int items = a.v.B * a.v.Hkv;
+    int n_split = 1;
+    while (n_split < 8 && items * n_split * 2 <= num_sms) n_split *= 2;
+    const int words = (a.v.cap + 31) / 32, keys = a.v.cap < KEYS_MAX ? a.v.cap : KEYS_MAX;
+    // the keys share what the bit map of a very long cache leaves
+    const size_t fixed = (size_t)(2 * LIST + words) * 4;
+    const size_t room = 212 * 1024 - fixed;
+    const int keys_cap = (size_t)keys * 4 <= room ? keys : (int)(room / 4);
+    const size_t smem = fixed + (size_t)keys_cap * 4;
+    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(items * n_split);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = n_split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, evict_kernel, a, counters, n_split, keys_cap);
+}
+
+}  // namespace kv
+}  // namespace aj
