@@ -68,6 +68,14 @@ struct EvictArgs {
 
 cudaError_t launch_append(const AppendArgs &a, bool bf16, cudaStream_t s);
 cudaError_t launch_attend_simt(const AttendArgs &a, bool bf16, int num_sms, cudaStream_t s);
+// few rows: at most FEW_ROWS = new tokens x query heads per key head; bf16, head size 64 or 128
+constexpr int FEW_ROWS = 16;
+cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s);
+size_t few_parts_floats(int D, int num_sms);
+// many rows: at most 128 query heads per key head; bf16, head size 64 or 128; at most umma_max_batch sequences
+cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s);
+size_t umma_parts_floats(int D, int num_sms);
+int umma_max_batch(int D);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s);
 

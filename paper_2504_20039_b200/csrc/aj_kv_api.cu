@@ -8,15 +8,21 @@
 
 using namespace aj;
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct aj_kv_s {
     int device = 0, num_sms = 0;
     int max_B = 0, max_q = 0, Hq = 0, Hkv = 0, D = 0, page = 0, page_shift = 0, dtype = 0;
     unsigned flags = 0;
+    bool tensor = false;           // bf16 and a head size that the tensor-core kernels take
     float *parts = nullptr;
     size_t parts_floats = 0;
     unsigned *counters = nullptr;  // [n_counters] attention items, then [max_B] eviction
     int n_counters = 0;
     int *status = nullptr;
+    EncodeTiledFn encode = nullptr;
     int last_launches = 0;
     const char *last_path = "none";
 };
@@ -83,6 +89,16 @@ kv::View view_of(aj_kv h, int n_pages, const int32_t *table, int width, const in
     return v;
 }
 
+// A tensor map of pages as [n_pages * Hkv * page_size, D], boxes of 64 elements x one page, 128-byte swizzle.
+bool page_map(aj_kv h, CUtensorMap *m, const void *pages, int n_pages) {
+    const cuuint64_t dims[2] = {(cuuint64_t)h->D, (cuuint64_t)n_pages * h->Hkv * h->page};
+    const cuuint64_t strides[1] = {(cuuint64_t)h->D * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)h->page}, one[2] = {1, 1};
+    return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pages), dims, strides, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 aj_status done(cudaError_t e) {
     if (e == cudaSuccess) return AJ_OK;
     cudaGetLastError();
@@ -135,8 +151,23 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     // CUDA-core kernels: 6 waves of pieces, or two per item if that is more, up to 64 MB
     const int G = Hq / Hkv;
     const long long items = (long long)max_B * Hkv * (((long long)max_q * G + kv::SIMT_ROWS - 1) / kv::SIMT_ROWS);
-    h->n_counters = (int)(items < 65536 ? items : 65536);
+    h->n_counters = (int)(items < 65536 ? items : 65536);  // (at least one for each of the at most 65535 key heads of a batch)
     h->parts_floats = (size_t)(7 * sms) * kv::SIMT_ROWS * (D + 2);
+    h->tensor = dtype == AJ_BF16 && (D == 64 || D == 128) && !(flags & AJ_KV_FLAG_FORCE_SIMT);
+    if (h->tensor && kv::few_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::few_parts_floats(D, sms);
+    const bool many = h->tensor && (long long)max_q * G > kv::FEW_ROWS && G <= 128;  // calls for the tcgen05 kernel
+    if (many && kv::umma_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::umma_parts_floats(D, sms);
+    if (many) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn) {
+            cudaGetLastError();
+            delete h;
+            return AJ_ERR_CUDA;
+        }
+        h->encode = reinterpret_cast<EncodeTiledFn>(fn);
+    }
     const size_t n = (size_t)h->n_counters + max_B;
     if (cudaMalloc(&h->parts, h->parts_floats * 4) != cudaSuccess || cudaMalloc(&h->counters, n * 4) != cudaSuccess ||
         cudaMemset(h->counters, 0, n * 4) != cudaSuccess || cudaMalloc(&h->status, 256) != cudaSuccess ||
@@ -228,6 +259,35 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     a.n_counters = h->n_counters;
     a.status = h->status;
     h->last_launches = 1;
+    if (h->tensor && n_q * a.v.G <= kv::FEW_ROWS) {
+        h->last_path = "few";
+        return done(kv::launch_attend_few(a, h->num_sms, (cudaStream_t)cuda_stream));
+    }
+    if (h->tensor && a.v.G <= 128) {
+        h->last_path = "umma";
+        h->last_launches = 0;
+        CUtensorMap mk, mv;
+        if (!page_map(h, &mk, k_pages, n_pages) || !page_map(h, &mv, v_pages, n_pages)) return AJ_ERR_CUDA;
+        const int most = kv::umma_max_batch(h->D);  // a very large batch runs in slices
+        for (int b0 = 0; b0 < B; b0 += most) {
+            kv::AttendArgs s = a;
+            s.v.B = B - b0 < most ? B - b0 : most;
+            s.v.table += (size_t)b0 * table_width;
+            s.v.lens += b0;
+            if (q_start) {
+                s.v.q_start += b0;
+            } else {
+                const size_t rows = (size_t)b0 * n_q;
+                s.q = (const char *)q + rows * q_stride * 2;
+                s.out = (char *)out + rows * out_stride * 2;
+                if (lse) s.lse += rows * h->Hq;
+            }
+            st = done(kv::launch_attend_umma(s, mk, mv, h->num_sms, (cudaStream_t)cuda_stream));
+            if (st != AJ_OK) return st;
+            h->last_launches += 2;
+        }
+        return AJ_OK;
+    }
     h->last_path = "simt";
     return done(kv::launch_attend_simt(a, h->dtype == AJ_BF16, h->num_sms, (cudaStream_t)cuda_stream));
 }

@@ -1,0 +1,640 @@
+// aj_kv_attend for many query rows per key head (verification windows and prompts), bf16, on tcgen05.
+//
+//   S = Q K^T   128 rows (token, query head) x 128 slots, f32 in tensor memory
+//   P = exp2(scale * S - m)   one thread per row, bf16, written back over S in tensor memory
+//   O += P V    P from tensor memory, V from shared memory as it lies in the pages (head elements contiguous)
+//
+// A CTA per SM holds two such row tiles ("streams").  A piece of work of more than 128 rows gives each stream half of
+// the tokens, and both read the same K and V tiles; a piece of at most 128 rows (a verification window) gives
+// both streams the same rows and every other tile of 128 slots, so that in either case one stream's softmax runs
+// under the other's matrix products.  Tensor memory: S0 S1 (128 columns each), O0 O1 (D columns each).
+//
+//   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); load the stream's queries, store results
+//   warp 8          one thread issues tcgen05.mma: PV of a stream, then its next QK^T, then the other stream's
+//   warp 9          (warps 10 and 11 only complete the warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
+//                   one box per lane, in the order K0 K1 V0 K2 V1 ... in which they are consumed
+//
+// The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
+// CTA: causal prompts and ragged caches are balanced alike.  Items that span CTAs leave unnormalised partial results
+// (f32) in the workspace, which a second kernel, launched as a programmatic dependent, joins.
+//
+// What bounds it: a window of K + 1 rows reads 512 bytes of K and V per slot and head and is bound by HBM up to about
+// 256 rows; a prompt is bound by the exponentials (16 per clock and SM: 2048 cycles per two tiles of 128 x 128)
+// together with the tensor pipe (2048 cycles for their four products).
+//
+// The running maximum is a reference that is raised only when a score exceeds it by more than 2^8, so the rescaling of
+// O (a round trip through tensor memory) is rare; weights up to 2^8 are as exact as weights up to 1.
+// Every wait is bounded (aj_ptx.cuh); one that runs out sets the status word and the CTA leaves by the normal way out.
+#include "aj_kv.cuh"
+#include "aj_ptx.cuh"
+
+namespace aj {
+namespace kv {
+
+namespace {
+
+constexpr int TILE = 128;
+constexpr int THREADS = 384;
+// Registers: launched with 168 a thread (3 x 168 = 504 per thread of a warpgroup row); the softmax warpgroups take 208
+// each and leave 88 to the third, 2 x 208 + 88 = 504.
+constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 88;
+constexpr uint32_t B_MN_MAJOR = 1u << 16;
+
+template <int D> struct Cfg {
+    static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
+    static constexpr int STAGES = D == 128 ? 5 : 8;
+    static constexpr int BARS = 2 * STAGES + 8;
+    static constexpr int PRE_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;
+    static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
+    static constexpr int smem(int B) { return PRE_AT + (B + 1) * 4 + 1024; }
+};
+
+// The tokens of a row piece and the tiles of slots that they see.
+struct Piece {
+    int ta, n_tok, tok0;          // first token, tokens, tokens of stream 0 (== n_tok: both streams share the rows)
+    int first, n_sink, first_tile, units;
+};
+
+struct Line {                     // position in the line of tiles
+    int b, h, qt, n_qt, unit;     // sequence, key head, row piece, tile within the item
+    Seq s;
+    Piece p;
+};
+
+__device__ inline int pieces_of(const Seq &s, int tpt) { return (s.nq + 2 * tpt - 1) / (2 * tpt); }
+
+__device__ inline Piece piece_of(const View &v, const Seq &s, int qt, int n_qt, int tpt) {
+    Piece p;
+    const int each = s.nq / n_qt, more = s.nq - each * n_qt;  // spread evenly
+    p.ta = qt * each + min(qt, more);
+    p.n_tok = each + (qt < more);
+    p.tok0 = p.n_tok <= tpt ? p.n_tok : (p.n_tok + 1) >> 1;
+    const int p_lo = s.L - s.nq + p.ta, end = max(0, p_lo + p.n_tok);
+    p.first = v.window ? min(max(0, p_lo - v.window + 1), end) : 0;
+    p.first_tile = p.first / TILE;
+    p.n_sink = min((min(v.sinks, p.first) + TILE - 1) / TILE, p.first_tile);
+    p.units = max(1, p.n_sink + (end + TILE - 1) / TILE - p.first_tile);
+    return p;
+}
+
+// Prefix sums over the sequences of their tiles, by all threads; returns the total.
+__device__ inline int build_line(const View &v, int tpt, int *pre) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    for (int b = warp; b < v.B; b += warps) {
+        const Seq s = seq_of(v, b);
+        const int n = pieces_of(s, tpt);
+        int u = 0;
+        for (int i = lane; i < n; i += 32) u += piece_of(v, s, i, n, tpt).units;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
+        if (lane == 0) pre[b + 1] = u * v.Hkv;
+    }
+    if (threadIdx.x == 0) pre[0] = 0;
+    __syncthreads();
+    if (warp == 0) {
+        int carry = 0;
+        for (int b0 = 1; b0 <= v.B; b0 += 32) {
+            int x = b0 + lane <= v.B ? pre[b0 + lane] : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(~0u, x, o);
+                if (lane >= o) x += y;
+            }
+            if (b0 + lane <= v.B) pre[b0 + lane] = carry + x;
+            carry += __shfl_sync(~0u, x, 31);
+        }
+    }
+    __syncthreads();
+    return pre[v.B];
+}
+
+__device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
+    Line c;
+    int lo = 0, hi = v.B;  // pre[lo] <= u < pre[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pre[mid] <= u) lo = mid; else hi = mid;
+    }
+    c.b = lo;
+    c.s = seq_of(v, lo);
+    c.n_qt = pieces_of(c.s, tpt);
+    const int per_head = (pre[lo + 1] - pre[lo]) / v.Hkv;
+    int r = u - pre[lo];
+    c.h = r / per_head;
+    r -= c.h * per_head;
+    for (c.qt = 0;; c.qt++) {
+        c.p = piece_of(v, c.s, c.qt, c.n_qt, tpt);
+        if (r < c.p.units) break;
+        r -= c.p.units;
+    }
+    c.unit = r;
+    return c;
+}
+
+// To the first tile of the next item.
+__device__ inline void next_item(const View &v, int tpt, const int *pre, Line &c) {
+    c.unit = 0;
+    if (++c.qt == c.n_qt) {
+        c.qt = 0;
+        if (++c.h == v.Hkv) {
+            c.h = 0;
+            do {
+                if (++c.b >= v.B) return;
+            } while (pre[c.b] == pre[c.b + 1]);
+            c.s = seq_of(v, c.b);
+            c.n_qt = pieces_of(c.s, tpt);
+        }
+    }
+    c.p = piece_of(v, c.s, c.qt, c.n_qt, tpt);
+}
+
+__device__ inline int tile_of(const Piece &p, int unit) { return unit < p.n_sink ? unit : unit - p.n_sink + p.first_tile; }
+
+// Order of the K and V tiles of a segment of n tiles in the ring: K0 K1 V0 K2 V1 ... V(n-1).
+__device__ inline int pos_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
+__device__ inline int pos_v(int t, int n) { return t + 1 < n ? 2 * t + 2 : 2 * n - 1; }
+
+__device__ inline void umma_ts(uint32_t d, uint32_t a, unsigned long long bdesc, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(acc)
+        : "memory");
+}
+// V as it lies in the pages: element blocks of 64 (128 bytes per slot), 128 slots each, 16 KB apart.
+__device__ inline unsigned long long desc_v(uint32_t addr) {
+    return (unsigned long long)((addr & 0x3FFFF) >> 4) | (unsigned long long)(16384 >> 4) << 16 |
+           (unsigned long long)(1024 >> 4) << 32 | (unsigned long long)1 << 46 | (unsigned long long)2 << 61;
+}
+
+#define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define I8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+
+__device__ inline void tmem_ld64(uint32_t addr, uint32_t (&r)[64]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24), R8(r, 32), R8(r, 40), R8(r, 48), R8(r, 56)
+        : "r"(addr)
+        : "memory");
+}
+__device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
+        ::I8(r, 0), I8(r, 8), I8(r, 16), I8(r, 24), "r"(addr)
+        : "memory");
+}
+__device__ inline void tmem_st2(uint32_t addr, float x, float y) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n\ttcgen05.wait::st.sync.aligned;"
+                 ::"r"(addr), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)) : "memory");
+}
+__device__ inline void tmem_ld2(uint32_t addr, float &x, float &y) {
+    uint32_t a, b;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
+    x = __uint_as_float(a);
+    y = __uint_as_float(b);
+}
+__device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ inline void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ inline void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
+__device__ inline uint32_t pack2(float lo, float hi) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1)
+attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, AttendArgs a, int tpt) {
+    using C = Cfg<D>;
+    constexpr int NS = C::STAGES, HALVES = D / 64;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (base - raw);
+    const uint32_t q_at = base, ring = base + 2 * C::TILE_BYTES, bars = ring + NS * C::TILE_BYTES;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (NS + s); };
+    auto s_full = [&](int x) { return bars + 8u * (2 * NS + x); };
+    auto p_ready = [&](int x) { return bars + 8u * (2 * NS + 2 + x); };
+    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 4 + x); };
+    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 6 + x); };
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    int *pre = reinterpret_cast<int *>(smem + C::PRE_AT);
+    const View &v = a.v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NS; s++) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+        }
+        for (int x = 0; x < 2; x++) {
+            mbar_init(s_full(x), 1);
+            mbar_init(p_ready(x), 128);
+            mbar_init(o_done(x), 1);
+            mbar_init(q_ready(x), 128);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
+    const int total = build_line(v, tpt, pre);  // synchronises the CTA
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int per = (total + gridDim.x - 1) / gridDim.x;
+    const int u0 = min(total, (int)blockIdx.x * per), u1 = min(total, u0 + per);
+    auto give_up = [&]() {
+        *abort_flag = 1;
+        atomicCAS(a.status, DEV_OK, DEV_TIMEOUT);
+    };
+
+    if (u0 < u1) {
+        if (warp >= 8)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
+        else
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
+        Line c = seek(v, tpt, pre, u0);
+        if (warp == 9) {
+            // ---------------------------------------------------------------- TMA
+            const unsigned long long pol = policy_evict_normal();
+            const int per_tile = TILE >> v.page_shift, boxes = per_tile * HALVES;  // at most 16
+            const uint32_t box_bytes = (uint32_t)v.page * 128u;
+            uint32_t g = 0;
+            bool ok = true;
+            for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
+                const int n = min(c.p.units - c.unit, u1 - u);
+                for (int i = 0; ok && i < 2 * n; i++) {
+                    // position i holds K of tile t, or V of tile t
+                    const bool is_v = i == 2 * n - 1 || (i >= 2 && (i & 1) == 0);
+                    const int t = is_v ? (i == 2 * n - 1 ? n - 1 : (i - 2) >> 1) : (i == 0 ? 0 : (i + 1) >> 1);
+                    const int s = g % NS;
+                    const int idx = lane % per_tile, half = lane / per_tile;
+                    const int slot = tile_of(c.p, c.unit + t) * TILE + (idx << v.page_shift);
+                    // pages past the length and pages that no row of the item sees are not fetched
+                    const bool on = lane < boxes && slot < c.s.L && (slot + v.page > c.p.first || slot < v.sinks);
+                    const int page = on ? page_of(v, c.b, slot) : 0;
+                    const unsigned n_on = __popc(__ballot_sync(~0u, on));
+                    ok = __all_sync(~0u, mbar_wait(empty(s), ((g / NS) & 1u) ^ 1u, abort_flag));
+                    if (!ok) {
+                        give_up();
+                        break;
+                    }
+                    if (lane == 0) mbar_expect_tx(full(s), n_on * box_bytes);
+                    __syncwarp();
+                    if (on)
+                        tma_load_2d(ring + s * C::TILE_BYTES + half * 16384 + (uint32_t)(idx << v.page_shift) * 128u, is_v ? &tmap_v : &tmap_k,
+                                    half * 64, (page * v.Hkv + c.h) << v.page_shift, full(s), pol);
+                    g++;
+                }
+                u += n;
+            }
+            // every copy has landed before the CTA may leave (after a time-out too)
+            int never = 0;
+            for (uint32_t i = g > NS ? g - NS : 0; i < g; i++) mbar_wait(full(i % NS), (i / NS) & 1u, &never);
+        } else if (warp == 8) {
+            // ---------------------------------------------------------------- MMA
+            if (lane == 0) {
+                constexpr uint32_t idesc_s = instr_desc(128, 128), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
+                uint32_t g = 0, n_p[2] = {0, 0}, n_q = 0;
+                bool ok = true;
+                auto wait = [&](uint32_t bar, uint32_t parity) {
+                    if (ok && !mbar_wait(bar, parity & 1u, abort_flag)) {
+                        give_up();
+                        ok = false;
+                    }
+                    tc_fence_after();
+                    return ok;
+                };
+                for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
+                    const int n = min(c.p.units - c.unit, u1 - u);
+                    const bool shared_rows = c.p.tok0 == c.p.n_tok;
+                    const int last = shared_rows ? 0 : 1;  // the stream after which a tile is free, if it is stream-independent
+                    auto qk = [&](int x, int t) {
+                        const uint32_t at = g + pos_k(t), s = at % NS;
+                        if (!wait(full(s), at / NS)) return;
+                        const uint32_t kt = ring + s * C::TILE_BYTES, qt = q_at + x * C::TILE_BYTES;
+#pragma unroll
+                        for (int k = 0; k < D / 16; k++)
+                            umma_bf16(tmem + x * 128, smem_desc_sw128(qt + (k / 4) * 16384) + 2 * (k % 4),
+                                      smem_desc_sw128(kt + (k / 4) * 16384) + 2 * (k % 4), idesc_s, k != 0);
+                        umma_commit(s_full(x));
+                        if (shared_rows || x == last) umma_commit(empty(s));
+                    };
+                    auto pv = [&](int x, int t, bool first) {
+                        if (!wait(p_ready(x), n_p[x])) return;
+                        n_p[x]++;
+                        const uint32_t at = g + pos_v(t, n), s = at % NS;
+                        if (!wait(full(s), at / NS)) return;
+                        const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
+#pragma unroll
+                        for (int k = 0; k < TILE / 16; k++)
+                            umma_ts(tmem + 256 + x * D, tmem + x * 128 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, !(first && k == 0));
+                        if (shared_rows || x == last) umma_commit(empty(s));
+                    };
+                    wait(q_ready(0), n_q);
+                    if (ok) wait(q_ready(1), n_q);
+                    n_q++;
+                    if (shared_rows) {
+                        if (ok) qk(0, 0);
+                        if (ok && n > 1) qk(1, 1);
+                        for (int t = 0; ok && t < n; t++) {
+                            const int x = t & 1;
+                            pv(x, t, t < 2);
+                            if (!ok) break;
+                            if (t + 2 < n) qk(x, t + 2);
+                            else umma_commit(o_done(x));
+                        }
+                    } else {
+                        if (ok) qk(0, 0);
+                        if (ok) qk(1, 0);
+                        for (int t = 0; ok && t < n; t++)
+                            for (int x = 0; ok && x < 2; x++) {
+                                pv(x, t, t == 0);
+                                if (!ok) break;
+                                if (t + 1 < n) qk(x, t + 1);
+                                else umma_commit(o_done(x));
+                            }
+                    }
+                    g += 2 * n;
+                    u += n;
+                }
+            }
+        } else if (warp < 8) {
+            // ---------------------------------------------------------------- softmax of stream x
+            const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
+            const uint32_t lanes = (uint32_t)(wq * 32) << 16;
+            const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * D + lanes;
+            uint32_t n_s = 0, n_o = 0, g = 0;
+            bool dead = false;
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                if (!dead && !__all_sync(~0u, mbar_wait(bar, parity & 1u, abort_flag))) {
+                    give_up();
+                    dead = true;  // go through the motions, so that the barriers below stay matched
+                }
+                tc_fence_after();
+            };
+            const float scale = a.scale_log2;
+            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
+                const int n = min(c.p.units - c.unit, u1 - u);
+                const bool shared_rows = c.p.tok0 == c.p.n_tok;
+                const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
+                const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
+                const int n_rows = tok * v.G;
+                // the stream's queries, 16 bytes per thread and step, into the swizzled K-major layout
+                {
+                    constexpr int CPR = D / 8;
+                    const __nv_bfloat16 *qp = (const __nv_bfloat16 *)a.q + (size_t)c.h * v.G * D;
+                    for (int i = row; i < 128 * CPR; i += 128) {
+                        const int r = i / CPR, cc = i % CPR;
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (r < n_rows)
+                            w = __ldg(reinterpret_cast<const uint4 *>(qp + ((size_t)c.s.row0 + ta + r / v.G) * a.q_stride + (size_t)(r % v.G) * D) + cc);
+                        *reinterpret_cast<uint4 *>(smem + x * C::TILE_BYTES + (cc >> 3) * 16384 + r * 128 + (((cc & 7) ^ (r & 7)) << 4)) = w;
+                    }
+                    fence_async_shared();
+                    mbar_arrive(q_ready(x));
+                }
+                const int p_first = c.s.L - c.s.nq + ta;           // slot of the stream's first token
+                const int my_p = p_first + min(row, n_rows - 1) / v.G, p_last = p_first + tok - 1;
+                float m = -INFINITY, l = 0.0f;
+                const int step = shared_rows ? 2 : 1;
+                bool first = true;
+                for (int t = shared_rows ? x : 0; t < n; t += step, first = false) {
+                    const int j0 = tile_of(c.p, c.unit + t) * TILE;
+                    wait(s_full(x), n_s);
+                    n_s++;
+                    uint32_t sr[2][64];
+                    tmem_ld64(t_s, sr[0]);
+                    tmem_ld64(t_s + 64, sr[1]);
+                    if (j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window)) {
+                        const int hi = my_p - j0, lo = v.window ? my_p - v.window + 1 - j0 : -1, sk = v.sinks - j0;
+#pragma unroll
+                        for (int i = 0; i < 128; i++)
+                            if (i > hi || (i < lo && i >= sk)) sr[i >> 6][i & 63] = 0xff800000u;
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 128; i += 2)
+                        mx = fmaxf(mx, fmaxf(__uint_as_float(sr[i >> 6][i & 63]), __uint_as_float(sr[i >> 6][(i + 1) & 63])));
+                    mx *= scale;
+                    const bool raise = mx > m + 8.0f;
+                    if (first) {
+                        m = mx;
+                    } else if (__any_sync(~0u, raise)) {
+                        // all of this stream's products so far are done (the commit behind S followed them)
+                        const float c2 = raise ? ex2(m - mx) : 1.0f;
+                        if (raise) m = mx;
+                        l *= c2;
+#pragma unroll
+                        for (int k = 0; k < D / 32; k++) {
+                            float ov[32];
+                            uint32_t ow[32];
+                            tmem_ld32(t_o + k * 32, ov);
+#pragma unroll
+                            for (int i = 0; i < 32; i++) ow[i] = __float_as_uint(ov[i] * c2);
+                            tmem_st32(t_o + k * 32, ow);
+                        }
+                    }
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    float sum[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int hf = 0; hf < 2; hf++) {
+                        uint32_t pw[32];
+#pragma unroll
+                        for (int i = 0; i < 32; i++) {
+                            const float e0 = ex2(fmaf(__uint_as_float(sr[hf][2 * i]), scale, -ref));
+                            const float e1 = ex2(fmaf(__uint_as_float(sr[hf][2 * i + 1]), scale, -ref));
+                            sum[i & 1] += e0;
+                            sum[2 + (i & 1)] += e1;
+                            pw[i] = pack2(e0, e1);
+                        }
+                        tmem_st32(t_s + hf * 32, pw);
+                    }
+                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                    // slots that nobody sees may hold anything: their values are cleared before the product
+                    const int dead_from = c.s.L - j0;
+                    if (dead_from < TILE || (j0 < c.p.first && c.p.first > v.sinks)) {
+                        const uint32_t at = g + pos_v(t, n), s = at % NS;
+                        wait(full(s), at / NS);
+                        const int j = j0 + row;
+                        if (j >= c.s.L || (j < c.p.first && j >= v.sinks)) {
+#pragma unroll
+                            for (int hh = 0; hh < HALVES; hh++)
+#pragma unroll
+                                for (int i = 0; i < 8; i++)
+                                    *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + hh * 16384 + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_shared();
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    mbar_arrive(p_ready(x));
+                }
+                // ---- the segment is done: store, or leave a partial result
+                const bool any = !first;
+                if (any) {
+                    wait(o_done(x), n_o);
+                    n_o++;
+                }
+                const bool whole = c.unit == 0 && n == c.p.units;
+                float4 *part = reinterpret_cast<float4 *>(a.parts + ((size_t)blockIdx.x * 2 + (c.unit == 0 ? 1 : 0)) * C::PART);
+                const int t_row = row / v.G;
+                const size_t out_row = (size_t)c.s.row0 + ta + t_row;
+                const int head = c.h * v.G + row % v.G;
+                const bool both = shared_rows && n > 1;  // two streams of the same rows: stream 0 joins and stores
+                const uint32_t t_s1 = tmem + 128 + lanes, t_o1 = tmem + 256 + D + lanes;
+                float w0 = 1.0f, w1 = 0.0f;
+                if (both) {
+                    // warps w and w + 4 reach the same lanes: stream 1 leaves its maximum and sum over its scores
+                    if (x == 1) tmem_st2(t_s1, m, l);
+                    tc_fence_before();
+                    bar_sync(1, 256);
+                    tc_fence_after();
+                    if (x == 0) {
+                        float m1, l1;
+                        tmem_ld2(t_s1, m1, l1);
+                        const float mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.0f : mm;
+                        w0 = ex2(m - ref);
+                        w1 = ex2(m1 - ref);
+                        l = l * w0 + l1 * w1;
+                        m = mm;
+                    }
+                }
+                if (!shared_rows || x == 0) {
+                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < D / 32; k++) {
+                        float ov[32];
+                        tmem_ld32(t_o + k * 32, ov);
+                        if (both) {
+                            float o1[32];
+                            tmem_ld32(t_o1 + k * 32, o1);
+#pragma unroll
+                            for (int i = 0; i < 32; i++) ov[i] = ov[i] * w0 + o1[i] * w1;
+                        }
+                        if (row < n_rows) {
+                            if (whole) {
+                                uint4 *o = reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D + k * 32);
+#pragma unroll
+                                for (int i = 0; i < 4; i++)
+                                    o[i] = make_uint4(pack2(ov[8 * i] * inv, ov[8 * i + 1] * inv), pack2(ov[8 * i + 2] * inv, ov[8 * i + 3] * inv),
+                                                      pack2(ov[8 * i + 4] * inv, ov[8 * i + 5] * inv), pack2(ov[8 * i + 6] * inv, ov[8 * i + 7] * inv));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 8; i++)
+                                    part[(k * 8 + i) * 256 + x * 128 + row] = make_float4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+                            }
+                        }
+                    }
+                    if (row < n_rows) {
+                        if (whole) {
+                            if (a.lse) a.lse[out_row * v.Hq + head] = l > 0.0f ? (m + log2f(l)) * LN2 : -INFINITY;
+                        } else {
+                            float *pm = reinterpret_cast<float *>(part) + 256 * D + x * 128 + row;
+                            pm[0] = m;
+                            pm[256] = l;
+                        }
+                    }
+                }
+                tc_fence_before();
+                if (both) bar_sync(1, 256);  // stream 1's tensor memory is read
+                g += 2 * n;
+                u += n;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// Joins the partial results of the items that span CTAs.  CTA (i, y) serves 32 rows of the item whose first
+// piece is the last of attention CTA i.
+template <int D>
+__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_cta) {
+    extern __shared__ int pre[];
+    using C = Cfg<D>;
+    const View &v = a.v;
+    const int total = build_line(v, tpt, pre), per = (total + n_cta - 1) / n_cta;
+    const int u1 = min(total, ((int)blockIdx.x + 1) * per), u0 = (int)blockIdx.x * per;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (u0 >= u1 || u1 >= total) return;
+    const Line c = seek(v, tpt, pre, u1 - 1);
+    const int i0 = u1 - 1 - c.unit, i1 = i0 + c.p.units;
+    if (i0 < u0 || i1 <= u1) return;  // begins in an earlier CTA, or ends in this one
+    const int n_parts = (i1 - 1) / per - (int)blockIdx.x + 1;
+    const int r = blockIdx.y * 32 + (threadIdx.x & 31), x = r >> 7, row = r & 127;
+    const bool shared_rows = c.p.tok0 == c.p.n_tok;
+    const int tok = x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
+    if (row >= tok * v.G || (x == 1 && shared_rows)) return;
+    auto part = [&](int i) { return a.parts + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * C::PART; };
+    float mm = -INFINITY, ll = 0.0f;
+    for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, __ldcg(part(i) + 256 * D + r));
+    const float ref = mm == -INFINITY ? 0.0f : mm;
+    constexpr int CH = D / 4, PER = CH / 8;
+    float4 acc[PER];
+#pragma unroll
+    for (int k = 0; k < PER; k++) acc[k] = make_float4(0, 0, 0, 0);
+    for (int i = 0; i < n_parts; i++) {
+        const float w = ex2(__ldcg(part(i) + 256 * D + r) - ref);
+        ll += w * __ldcg(part(i) + 256 * (D + 1) + r);
+#pragma unroll
+        for (int k = 0; k < PER; k++) {
+            const float4 y = __ldcg(reinterpret_cast<const float4 *>(part(i)) + ((threadIdx.x >> 5) * PER + k) * 256 + r);
+            acc[k].x += w * y.x;
+            acc[k].y += w * y.y;
+            acc[k].z += w * y.z;
+            acc[k].w += w * y.w;
+        }
+    }
+    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+    const size_t out_row = (size_t)c.s.row0 + c.p.ta + (x ? c.p.tok0 : 0) + row / v.G;
+    const int head = c.h * v.G + row % v.G;
+    uint2 *o = reinterpret_cast<uint2 *>((__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D) + (threadIdx.x >> 5) * PER;
+#pragma unroll
+    for (int k = 0; k < PER; k++) o[k] = make_uint2(pack2(acc[k].x * inv, acc[k].y * inv), pack2(acc[k].z * inv, acc[k].w * inv));
+    if (threadIdx.x < 32 && a.lse) a.lse[out_row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+}
+
+template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s) {
+    using C = Cfg<D>;
+    const int tpt = 128 / a.v.G;
+    const int smem = C::smem(a.v.B);
+    auto kernel = attend_umma_kernel<D>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<num_sms, THREADS, smem, s>>>(mk, mv, a, tpt);
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(num_sms, 8);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = (a.v.B + 1) * 4;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<D>, a, tpt, num_sms);
+}
+
+}  // namespace
+
+int umma_max_batch(int D) { return (232448 - (D == 64 ? Cfg<64>::smem(0) : Cfg<128>::smem(0))) / 4 - 1; }
+size_t umma_parts_floats(int D, int num_sms) { return (size_t)num_sms * 2 * 256 * (D + 2); }
+
+cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s) {
+    return a.v.D == 64 ? umma<64>(a, mk, mv, num_sms, s) : umma<128>(a, mk, mv, num_sms, s);
+}
+
+}  // namespace kv
+}  // namespace aj
