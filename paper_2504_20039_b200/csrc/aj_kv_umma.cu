@@ -35,9 +35,9 @@ namespace {
 
 constexpr int TILE = 128;
 constexpr int THREADS = 384;
-// Registers: launched with 168 a thread (3 x 168 = 504 per thread of a warpgroup row); the softmax warpgroups take 208
-// each and leave 88 to the third, 2 x 208 + 88 = 504.
-constexpr int REGS_SOFTMAX = 208, REGS_OTHER = 88;
+// Registers: launched with 168 a thread (3 x 168 = 504 per thread of a warpgroup row); the softmax warpgroups take 200
+// each and leave 104 to the third, 2 x 200 + 104 = 504.
+constexpr int REGS_SOFTMAX = 200, REGS_OTHER = 104;
 constexpr uint32_t B_MN_MAJOR = 1u << 16;
 
 template <int D> struct Cfg {
@@ -181,6 +181,22 @@ __device__ inline void tmem_ld64(uint32_t addr, uint32_t (&r)[64]) {
         : "r"(addr)
         : "memory");
 }
+// x *= c for 16 columns of this thread's lane
+__device__ inline void tmem_scale16(uint32_t addr, float c) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : R8(r, 0), R8(r, 8)
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; i++) r[i] = __float_as_uint(__uint_as_float(r[i]) * c);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::I8(r, 0), I8(r, 8), "r"(addr)
+        : "memory");
+}
 __device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -257,12 +273,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     };
 
     if (u0 < u1) {
-        if (warp >= 8)
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
-        else
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
-        Line c = seek(v, tpt, pre, u0);
-        if (warp == 9) {
+        if (warp >= 8) {
+          asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
+          Line c = seek(v, tpt, pre, u0);
+          if (warp == 9) {
             // ---------------------------------------------------------------- TMA
             const unsigned long long pol = policy_evict_normal();
             const int per_tile = TILE >> v.page_shift, boxes = per_tile * HALVES;  // at most 16
@@ -299,7 +313,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // every copy has landed before the CTA may leave (after a time-out too)
             int never = 0;
             for (uint32_t i = g > NS ? g - NS : 0; i < g; i++) mbar_wait(full(i % NS), (i / NS) & 1u, &never);
-        } else if (warp == 8) {
+          } else if (warp == 8) {
             // ---------------------------------------------------------------- MMA
             if (lane == 0) {
                 constexpr uint32_t idesc_s = instr_desc(128, 128), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
@@ -367,8 +381,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     u += n;
                 }
             }
-        } else if (warp < 8) {
+          }
+        } else {
             // ---------------------------------------------------------------- softmax of stream x
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
+            Line c = seek(v, tpt, pre, u0);
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
             const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * D + lanes;
@@ -433,15 +450,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         const float c2 = raise ? ex2(m - mx) : 1.0f;
                         if (raise) m = mx;
                         l *= c2;
-#pragma unroll
-                        for (int k = 0; k < D / 32; k++) {
-                            float ov[32];
-                            uint32_t ow[32];
-                            tmem_ld32(t_o + k * 32, ov);
-#pragma unroll
-                            for (int i = 0; i < 32; i++) ow[i] = __float_as_uint(ov[i] * c2);
-                            tmem_st32(t_o + k * 32, ow);
-                        }
+#pragma unroll 1
+                        for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
                     float sum[4] = {0, 0, 0, 0};
