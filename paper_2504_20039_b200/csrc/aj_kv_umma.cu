@@ -10,8 +10,8 @@
 // under the other's matrix products.  Tensor memory: S0 S1 (128 columns each), O0 O1 (D columns each).
 //
 //   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); load the stream's queries, store results
-//   warp 8          one thread issues tcgen05.mma: PV of a stream, then its next QK^T, then the other stream's
-//   warp 9          (warps 10 and 11 only complete the warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
+//   warps 8, 10     issue tcgen05.mma for stream 0 and 1: PV of a tile, then QK^T of the stream's next
+//   warp 9          (warp 11 only completes the warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
 //                   one box per lane, in the order K0 K1 V0 K2 V1 ... in which they are consumed
 //
 // The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
@@ -43,10 +43,11 @@ constexpr uint32_t B_MN_MAJOR = 1u << 16;
 template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
     static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BARS = 2 * STAGES + 8;
-    static constexpr int PRE_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;
+    static constexpr int BARS = 2 * STAGES + 10;
+    static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maximum and sum of stream 1's rows
+    static constexpr int PRE_AT = ML_AT + 2 * 128 * 4;
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
-    static constexpr int smem(int B) { return PRE_AT + (B + 1) * 4 + 1024; }
+    static constexpr int smem(int B) { return PRE_AT + (B + 1) * 4; }
 };
 
 // The tokens of a row piece and the tiles of slots that they see.
@@ -55,21 +56,32 @@ struct Piece {
     int first, n_sink, first_tile, units;
 };
 
-struct Line {                     // position in the line of tiles
-    int b, h, qt, n_qt, unit;     // sequence, key head, row piece, tile within the item
+struct Seqs {                     // a sequence and how its new tokens are cut into pieces
     Seq s;
+    int n, each, more;            // pieces, spread evenly
+};
+
+struct Line {                     // position in the line of tiles
+    int b, h, qt, unit;           // sequence, key head, row piece, tile within the item
+    Seqs q;
     Piece p;
 };
 
-__device__ inline int pieces_of(const Seq &s, int tpt) { return (s.nq + 2 * tpt - 1) / (2 * tpt); }
+__device__ inline Seqs pieces_of(const View &v, int b, int tpt) {
+    Seqs q;
+    q.s = seq_of(v, b);
+    q.n = (q.s.nq + 2 * tpt - 1) / (2 * tpt);
+    q.each = q.n ? q.s.nq / q.n : 0;
+    q.more = q.s.nq - q.each * q.n;
+    return q;
+}
 
-__device__ inline Piece piece_of(const View &v, const Seq &s, int qt, int n_qt, int tpt) {
+__device__ inline Piece piece_of(const View &v, const Seqs &q, int qt, int tpt) {
     Piece p;
-    const int each = s.nq / n_qt, more = s.nq - each * n_qt;  // spread evenly
-    p.ta = qt * each + min(qt, more);
-    p.n_tok = each + (qt < more);
+    p.ta = qt * q.each + min(qt, q.more);
+    p.n_tok = q.each + (qt < q.more);
     p.tok0 = p.n_tok <= tpt ? p.n_tok : (p.n_tok + 1) >> 1;
-    const int p_lo = s.L - s.nq + p.ta, end = max(0, p_lo + p.n_tok);
+    const int p_lo = q.s.L - q.s.nq + p.ta, end = max(0, p_lo + p.n_tok);
     p.first = v.window ? min(max(0, p_lo - v.window + 1), end) : 0;
     p.first_tile = p.first / TILE;
     p.n_sink = min((min(v.sinks, p.first) + TILE - 1) / TILE, p.first_tile);
@@ -79,15 +91,23 @@ __device__ inline Piece piece_of(const View &v, const Seq &s, int qt, int n_qt, 
 
 // Prefix sums over the sequences of their tiles, by all threads; returns the total.
 __device__ inline int build_line(const View &v, int tpt, int *pre) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    for (int b = warp; b < v.B; b += warps) {
-        const Seq s = seq_of(v, b);
-        const int n = pieces_of(s, tpt);
-        int u = 0;
-        for (int i = lane; i < n; i += 32) u += piece_of(v, s, i, n, tpt).units;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (v.n_q <= 16 * tpt) {  // few pieces: a thread per sequence; else a warp
+        for (int b = threadIdx.x; b < v.B; b += blockDim.x) {
+            const Seqs q = pieces_of(v, b, tpt);
+            int u = 0;
+            for (int i = 0; i < q.n; i++) u += piece_of(v, q, i, tpt).units;
+            pre[b + 1] = u * v.Hkv;
+        }
+    } else {
+        for (int b = warp; b < v.B; b += blockDim.x >> 5) {
+            const Seqs q = pieces_of(v, b, tpt);
+            int u = 0;
+            for (int i = lane; i < q.n; i += 32) u += piece_of(v, q, i, tpt).units;
 #pragma unroll
-        for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
-        if (lane == 0) pre[b + 1] = u * v.Hkv;
+            for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
+            if (lane == 0) pre[b + 1] = u * v.Hkv;
+        }
     }
     if (threadIdx.x == 0) pre[0] = 0;
     __syncthreads();
@@ -108,45 +128,60 @@ __device__ inline int build_line(const View &v, int tpt, int *pre) {
     return pre[v.B];
 }
 
+// By a whole warp.
 __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
     Line c;
+    const int lane = threadIdx.x & 31;
     int lo = 0, hi = v.B;  // pre[lo] <= u < pre[hi]
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (pre[mid] <= u) lo = mid; else hi = mid;
     }
     c.b = lo;
-    c.s = seq_of(v, lo);
-    c.n_qt = pieces_of(c.s, tpt);
+    c.q = pieces_of(v, lo, tpt);
     const int per_head = (pre[lo + 1] - pre[lo]) / v.Hkv;
     int r = u - pre[lo];
     c.h = r / per_head;
     r -= c.h * per_head;
-    for (c.qt = 0;; c.qt++) {
-        c.p = piece_of(v, c.s, c.qt, c.n_qt, tpt);
-        if (r < c.p.units) break;
-        r -= c.p.units;
+    for (int q0 = 0;; q0 += 32) {
+        const int n = q0 + lane < c.q.n ? piece_of(v, c.q, q0 + lane, tpt).units : 0;
+        int x = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o) x += y;
+        }
+        const int all = __shfl_sync(~0u, x, 31);
+        if (r < all) {
+            const int at = __ffs(__ballot_sync(~0u, r < x)) - 1;
+            c.qt = q0 + at;
+            c.unit = r - __shfl_sync(~0u, x - n, at);
+            break;
+        }
+        r -= all;
     }
-    c.unit = r;
+    c.p = piece_of(v, c.q, c.qt, tpt);
     return c;
 }
 
 // To the first tile of the next item.
 __device__ inline void next_item(const View &v, int tpt, const int *pre, Line &c) {
     c.unit = 0;
-    if (++c.qt == c.n_qt) {
+    if (++c.qt == c.q.n) {
         c.qt = 0;
         if (++c.h == v.Hkv) {
             c.h = 0;
             do {
                 if (++c.b >= v.B) return;
             } while (pre[c.b] == pre[c.b + 1]);
-            c.s = seq_of(v, c.b);
-            c.n_qt = pieces_of(c.s, tpt);
+            c.q = pieces_of(v, c.b, tpt);
         }
     }
-    c.p = piece_of(v, c.s, c.qt, c.n_qt, tpt);
+    c.p = piece_of(v, c.q, c.qt, tpt);
 }
+
+// Does stream x have a tile in a segment of n tiles of this piece?
+__device__ inline bool has_tile(const Piece &p, int x, int n) { return x == 0 || p.tok0 < p.n_tok || n > 1; }
 
 __device__ inline int tile_of(const Piece &p, int unit) { return unit < p.n_sink ? unit : unit - p.n_sink + p.first_tile; }
 
@@ -204,18 +239,15 @@ __device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
         ::I8(r, 0), I8(r, 8), I8(r, 16), I8(r, 24), "r"(addr)
         : "memory");
 }
-__device__ inline void tmem_st2(uint32_t addr, float x, float y) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};\n\ttcgen05.wait::st.sync.aligned;"
-                 ::"r"(addr), "r"(__float_as_uint(x)), "r"(__float_as_uint(y)) : "memory");
-}
-__device__ inline void tmem_ld2(uint32_t addr, float &x, float &y) {
-    uint32_t a, b;
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];\n\ttcgen05.wait::ld.sync.aligned;" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
-    x = __uint_as_float(a);
-    y = __uint_as_float(b);
+__device__ inline uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+__device__ inline bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ inline void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ inline void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 __device__ inline void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
 
 __device__ inline uint32_t pack2(float lo, float hi) {
@@ -228,9 +260,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, AttendArgs a, int tpt) {
     using C = Cfg<D>;
     constexpr int NS = C::STAGES, HALVES = D / 64;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    uint8_t *smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles need 1024-byte alignment
+    const uint32_t base = smem_u32(smem);
     const uint32_t q_at = base, ring = base + 2 * C::TILE_BYTES, bars = ring + NS * C::TILE_BYTES;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
@@ -238,23 +269,25 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto p_ready = [&](int x) { return bars + 8u * (2 * NS + 2 + x); };
     auto o_done = [&](int x) { return bars + 8u * (2 * NS + 4 + x); };
     auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 6 + x); };
+    auto drained = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *pre = reinterpret_cast<int *>(smem + C::PRE_AT);
     const View &v = a.v;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
             mbar_init(full(s), 1);
-            mbar_init(empty(s), 1);
+            mbar_init(empty(s), 2);  // both streams, or the one that uses the tile twice
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(s_full(x), 1);
             mbar_init(p_ready(x), 128);
             mbar_init(o_done(x), 1);
             mbar_init(q_ready(x), 128);
+            mbar_init(drained(x), 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -293,7 +326,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     const int idx = lane % per_tile, half = lane / per_tile;
                     const int slot = tile_of(c.p, c.unit + t) * TILE + (idx << v.page_shift);
                     // pages past the length and pages that no row of the item sees are not fetched
-                    const bool on = lane < boxes && slot < c.s.L && (slot + v.page > c.p.first || slot < v.sinks);
+                    const bool on = lane < boxes && slot < c.q.s.L && (slot + v.page > c.p.first || slot < v.sinks);
                     const int page = on ? page_of(v, c.b, slot) : 0;
                     const unsigned n_on = __popc(__ballot_sync(~0u, on));
                     ok = __all_sync(~0u, mbar_wait(empty(s), ((g / NS) & 1u) ^ 1u, abort_flag));
@@ -310,77 +343,81 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
                 u += n;
             }
-            // every copy has landed before the CTA may leave (after a time-out too)
+            // Before the CTA may leave, every copy has landed (after a time-out too) and every stage has been released:
+            // a commit that is still on its way must not arrive in shared memory that belongs to the next CTA.
             int never = 0;
-            for (uint32_t i = g > NS ? g - NS : 0; i < g; i++) mbar_wait(full(i % NS), (i / NS) & 1u, &never);
-          } else if (warp == 8) {
-            // ---------------------------------------------------------------- MMA
-            if (lane == 0) {
-                constexpr uint32_t idesc_s = instr_desc(128, 128), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
-                uint32_t g = 0, n_p[2] = {0, 0}, n_q = 0;
-                bool ok = true;
-                auto wait = [&](uint32_t bar, uint32_t parity) {
-                    if (ok && !mbar_wait(bar, parity & 1u, abort_flag)) {
-                        give_up();
-                        ok = false;
-                    }
-                    tc_fence_after();
-                    return ok;
-                };
-                for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
-                    const int n = min(c.p.units - c.unit, u1 - u);
-                    const bool shared_rows = c.p.tok0 == c.p.n_tok;
-                    const int last = shared_rows ? 0 : 1;  // the stream after which a tile is free, if it is stream-independent
-                    auto qk = [&](int x, int t) {
-                        const uint32_t at = g + pos_k(t), s = at % NS;
-                        if (!wait(full(s), at / NS)) return;
-                        const uint32_t kt = ring + s * C::TILE_BYTES, qt = q_at + x * C::TILE_BYTES;
-#pragma unroll
-                        for (int k = 0; k < D / 16; k++)
-                            umma_bf16(tmem + x * 128, smem_desc_sw128(qt + (k / 4) * 16384) + 2 * (k % 4),
-                                      smem_desc_sw128(kt + (k / 4) * 16384) + 2 * (k % 4), idesc_s, k != 0);
-                        umma_commit(s_full(x));
-                        if (shared_rows || x == last) umma_commit(empty(s));
-                    };
-                    auto pv = [&](int x, int t, bool first) {
-                        if (!wait(p_ready(x), n_p[x])) return;
-                        n_p[x]++;
-                        const uint32_t at = g + pos_v(t, n), s = at % NS;
-                        if (!wait(full(s), at / NS)) return;
-                        const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
-#pragma unroll
-                        for (int k = 0; k < TILE / 16; k++)
-                            umma_ts(tmem + 256 + x * D, tmem + x * 128 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, !(first && k == 0));
-                        if (shared_rows || x == last) umma_commit(empty(s));
-                    };
-                    wait(q_ready(0), n_q);
-                    if (ok) wait(q_ready(1), n_q);
-                    n_q++;
-                    if (shared_rows) {
-                        if (ok) qk(0, 0);
-                        if (ok && n > 1) qk(1, 1);
-                        for (int t = 0; ok && t < n; t++) {
-                            const int x = t & 1;
-                            pv(x, t, t < 2);
-                            if (!ok) break;
-                            if (t + 2 < n) qk(x, t + 2);
-                            else umma_commit(o_done(x));
-                        }
-                    } else {
-                        if (ok) qk(0, 0);
-                        if (ok) qk(1, 0);
-                        for (int t = 0; ok && t < n; t++)
-                            for (int x = 0; ok && x < 2; x++) {
-                                pv(x, t, t == 0);
-                                if (!ok) break;
-                                if (t + 1 < n) qk(x, t + 1);
-                                else umma_commit(o_done(x));
-                            }
-                    }
-                    g += 2 * n;
-                    u += n;
+            for (uint32_t i = g > NS ? g - NS : 0; i < g; i++) {
+                mbar_wait(full(i % NS), (i / NS) & 1u, &never);
+                if (ok && !__all_sync(~0u, mbar_wait(empty(i % NS), (i / NS) & 1u, abort_flag))) {
+                    give_up();
+                    ok = false;
                 }
             }
+          } else if (warp <= 10) {
+            // ---------------------------------------------------------------- MMA: warp 8 stream 0, warp 10 stream 1
+            // The whole warp walks the loop and waits, one elected lane issues.
+            const int x = warp == 8 ? 0 : 1;
+            constexpr uint32_t idesc_s = instr_desc(128, 128), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
+            const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
+            const unsigned long long qd = smem_desc_sw128(q_at + x * C::TILE_BYTES);
+            uint32_t g = 0, n_p = 0, n_q = 0;
+            bool ok = true;
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                if (ok && !__all_sync(~0u, mbar_wait(bar, parity & 1u, abort_flag))) {
+                    give_up();
+                    ok = false;
+                }
+                tc_fence_after();
+                return ok;
+            };
+            for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
+                const int n = min(c.p.units - c.unit, u1 - u);
+                const bool shared_rows = c.p.tok0 == c.p.n_tok;
+                const int step = shared_rows ? 2 : 1, t0 = shared_rows ? x : 0;
+                auto qk = [&](int t) {
+                    const uint32_t at = g + pos_k(t), s = at % NS;
+                    if (!wait(full(s), at / NS)) return;
+                    const unsigned long long kd = smem_desc_sw128(ring + s * C::TILE_BYTES);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; k++)
+                            umma_bf16(t_s, qd + (k / 4) * (16384 >> 4) + 2 * (k % 4), kd + (k / 4) * (16384 >> 4) + 2 * (k % 4), idesc_s, k != 0);
+                        umma_commit(s_full(x));
+                        umma_commit(empty(s));
+                        if (shared_rows) umma_commit(empty(s));
+                    }
+                    __syncwarp();
+                };
+                if (t0 < n) {
+                    wait(q_ready(x), n_q);
+                    n_q++;
+                    if (ok) qk(t0);
+                }
+                for (int t = t0; ok && t < n; t += step) {
+                    if (!wait(p_ready(x), n_p)) break;
+                    n_p++;
+                    const uint32_t at = g + pos_v(t, n), s = at % NS;
+                    if (!wait(full(s), at / NS)) break;
+                    const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < TILE / 16; k++)
+                            umma_ts(t_o, t_s + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, k == 0 ? t != t0 : 1);
+                        umma_commit(empty(s));
+                        if (shared_rows) umma_commit(empty(s));
+                        if (t + step >= n) umma_commit(o_done(x));
+                    }
+                    __syncwarp();
+                    if (t + step < n) qk(t + step);
+                }
+                g += 2 * n;
+                u += n;
+            }
+            // nothing that this warp issued is in flight when the CTA leaves, after a time-out either
+            int never = 0;
+            if (elect_one()) umma_commit(drained(x));
+            __syncwarp();
+            mbar_wait(drained(x), 0, &never);
           }
         } else {
             // ---------------------------------------------------------------- softmax of stream x
@@ -399,27 +436,41 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 tc_fence_after();
             };
             const float scale = a.scale_log2;
-            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
+            // A stream's queries into the swizzled K-major layout, asynchronously; rows past its tokens get zeros.
+            auto fetch_queries = [&](const Line &c) {
+                constexpr int CPR = D / 8;
+                const bool lead = x == 0 || c.p.tok0 == c.p.n_tok;
+                const int n_rows = (lead ? c.p.tok0 : c.p.n_tok - c.p.tok0) * v.G;
+                const __nv_bfloat16 *qp = (const __nv_bfloat16 *)a.q + ((size_t)c.q.s.row0 + c.p.ta + (lead ? 0 : c.p.tok0)) * a.q_stride + (size_t)c.h * v.G * D;
+#pragma unroll 4
+                for (int i = 0; i < CPR; i++) {
+                    const int r = i * (128 / CPR) + row / CPR, cc = row % CPR, t = r / v.G;
+                    const uint32_t dst = q_at + x * C::TILE_BYTES + (cc >> 3) * 16384 + r * 128 + (((cc & 7) ^ (r & 7)) << 4);
+                    const int bytes = r < n_rows ? 16 : 0;
+                    const void *src = r < n_rows ? (const void *)(qp + (size_t)t * a.q_stride + (size_t)(r - t * v.G) * D + cc * 8) : a.q;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+                }
+            };
+            auto queries_ready = [&]() {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_async_shared();
+                mbar_arrive(q_ready(x));
+            };
+            if (has_tile(c.p, x, min(c.p.units - c.unit, u1 - u0))) {
+                fetch_queries(c);
+                queries_ready();
+            }
+            Line nx = c;
+            for (int u = u0; u < u1; c = nx) {
                 const int n = min(c.p.units - c.unit, u1 - u);
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
                 const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
                 const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
                 const int n_rows = tok * v.G;
-                // the stream's queries, 16 bytes per thread and step, into the swizzled K-major layout
-                {
-                    constexpr int CPR = D / 8;
-                    const __nv_bfloat16 *qp = (const __nv_bfloat16 *)a.q + (size_t)c.h * v.G * D;
-                    for (int i = row; i < 128 * CPR; i += 128) {
-                        const int r = i / CPR, cc = i % CPR;
-                        uint4 w = make_uint4(0, 0, 0, 0);
-                        if (r < n_rows)
-                            w = __ldg(reinterpret_cast<const uint4 *>(qp + ((size_t)c.s.row0 + ta + r / v.G) * a.q_stride + (size_t)(r % v.G) * D) + cc);
-                        *reinterpret_cast<uint4 *>(smem + x * C::TILE_BYTES + (cc >> 3) * 16384 + r * 128 + (((cc & 7) ^ (r & 7)) << 4)) = w;
-                    }
-                    fence_async_shared();
-                    mbar_arrive(q_ready(x));
-                }
-                const int p_first = c.s.L - c.s.nq + ta;           // slot of the stream's first token
+                next_item(v, tpt, pre, nx);
+                if (!shared_rows && x == 1) bar_arrive(2, 256);  // stream 0 goes first
+                const bool more = u + n < u1 && has_tile(nx.p, x, min(nx.p.units, u1 - u - n));  // queries to fetch for the next item
+                const int p_first = c.q.s.L - c.q.s.nq + ta;           // slot of the stream's first token
                 const int my_p = p_first + min(row, n_rows - 1) / v.G, p_last = p_first + tok - 1;
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
@@ -428,14 +479,24 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     const int j0 = tile_of(c.p, c.unit + t) * TILE;
                     wait(s_full(x), n_s);
                     n_s++;
+                    // this stream's last product with its queries is done: fetch the next ones under the softmax
+                    const bool closing = more && t + step >= n;
+                    if (closing) fetch_queries(nx);
                     uint32_t sr[2][64];
                     tmem_ld64(t_s, sr[0]);
                     tmem_ld64(t_s + 64, sr[1]);
                     if (j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window)) {
-                        const int hi = my_p - j0, lo = v.window ? my_p - v.window + 1 - j0 : -1, sk = v.sinks - j0;
+                        // one bit per slot of the tile; no branch per element
+                        const int hi = my_p - j0 + 1, lo = v.window ? my_p - v.window + 1 - j0 : 0, sk = v.sinks - j0;
 #pragma unroll
-                        for (int i = 0; i < 128; i++)
-                            if (i > hi || (i < lo && i >= sk)) sr[i >> 6][i & 63] = 0xff800000u;
+                        for (int w = 0; w < 4; w++) {
+                            const uint32_t bits = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
+#pragma unroll
+                            for (int i = 0; i < 32; i++) {
+                                uint32_t &s = sr[w >> 1][(w & 1) * 32 + i];
+                                s = bits & (1u << i) ? s : 0xff800000u;
+                            }
+                        }
                     }
                     float mx = -INFINITY;
 #pragma unroll
@@ -453,6 +514,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
                         for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
                     }
+                    // Streams of one piece take turns with the exponentials: left alone they fall into step, and then both
+                    // wait for the tensor pipe and both queue at the exponential unit.
+                    if (!shared_rows) bar_sync(2 + x, 256);
                     const float ref = m == -INFINITY ? 0.0f : m;
                     float sum[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -468,14 +532,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         }
                         tmem_st32(t_s + hf * 32, pw);
                     }
+                    if (!shared_rows && (x == 0 || t + 1 < n)) bar_arrive(3 - x, 256);  // (every arrival is waited for)
                     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     // slots that nobody sees may hold anything: their values are cleared before the product
-                    const int dead_from = c.s.L - j0;
+                    const int dead_from = c.q.s.L - j0;
                     if (dead_from < TILE || (j0 < c.p.first && c.p.first > v.sinks)) {
                         const uint32_t at = g + pos_v(t, n), s = at % NS;
                         wait(full(s), at / NS);
                         const int j = j0 + row;
-                        if (j >= c.s.L || (j < c.p.first && j >= v.sinks)) {
+                        if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
 #pragma unroll
                             for (int hh = 0; hh < HALVES; hh++)
 #pragma unroll
@@ -487,6 +552,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     tmem_st_wait();
                     tc_fence_before();
                     mbar_arrive(p_ready(x));
+                    if (closing) queries_ready();
+                }
+                if (first && more) {  // (no tile in this segment: its own queries were not fetched)
+                    fetch_queries(nx);
+                    queries_ready();
                 }
                 // ---- the segment is done: store, or leave a partial result
                 const bool any = !first;
@@ -497,20 +567,23 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const bool whole = c.unit == 0 && n == c.p.units;
                 float4 *part = reinterpret_cast<float4 *>(a.parts + ((size_t)blockIdx.x * 2 + (c.unit == 0 ? 1 : 0)) * C::PART);
                 const int t_row = row / v.G;
-                const size_t out_row = (size_t)c.s.row0 + ta + t_row;
+                const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
                 const int head = c.h * v.G + row % v.G;
                 const bool both = shared_rows && n > 1;  // two streams of the same rows: stream 0 joins and stores
-                const uint32_t t_s1 = tmem + 128 + lanes, t_o1 = tmem + 256 + D + lanes;
+                const uint32_t t_o1 = tmem + 256 + D + lanes;
                 float w0 = 1.0f, w1 = 0.0f;
                 if (both) {
-                    // warps w and w + 4 reach the same lanes: stream 1 leaves its maximum and sum over its scores
-                    if (x == 1) tmem_st2(t_s1, m, l);
+                    // warps w and w + 4 reach the same lanes of tensor memory
+                    volatile float *ml = reinterpret_cast<volatile float *>(smem + C::ML_AT);
+                    if (x == 1) {
+                        ml[row] = m;
+                        ml[128 + row] = l;
+                    }
                     tc_fence_before();
                     bar_sync(1, 256);
                     tc_fence_after();
                     if (x == 0) {
-                        float m1, l1;
-                        tmem_ld2(t_s1, m1, l1);
+                        const float m1 = ml[row], l1 = ml[128 + row];
                         const float mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.0f : mm;
                         w0 = ex2(m - ref);
                         w1 = ex2(m1 - ref);
@@ -588,12 +661,14 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_
     if (row >= tok * v.G || (x == 1 && shared_rows)) return;
     auto part = [&](int i) { return a.parts + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * C::PART; };
     float mm = -INFINITY, ll = 0.0f;
+#pragma unroll 8
     for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, __ldcg(part(i) + 256 * D + r));
     const float ref = mm == -INFINITY ? 0.0f : mm;
     constexpr int CH = D / 4, PER = CH / 8;
     float4 acc[PER];
 #pragma unroll
     for (int k = 0; k < PER; k++) acc[k] = make_float4(0, 0, 0, 0);
+#pragma unroll 4
     for (int i = 0; i < n_parts; i++) {
         const float w = ex2(__ldcg(part(i) + 256 * D + r) - ref);
         ll += w * __ldcg(part(i) + 256 * (D + 1) + r);
@@ -607,7 +682,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_
         }
     }
     const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-    const size_t out_row = (size_t)c.s.row0 + c.p.ta + (x ? c.p.tok0 : 0) + row / v.G;
+    const size_t out_row = (size_t)c.q.s.row0 + c.p.ta + (x ? c.p.tok0 : 0) + row / v.G;
     const int head = c.h * v.G + row % v.G;
     uint2 *o = reinterpret_cast<uint2 *>((__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D) + (threadIdx.x >> 5) * PER;
 #pragma unroll
