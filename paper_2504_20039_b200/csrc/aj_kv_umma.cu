@@ -11,8 +11,8 @@
 //
 //   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); load the stream's queries, store results
 //   warps 8, 10     issue tcgen05.mma for stream 0 and 1: PV of a tile, then QK^T of the stream's next
-//   warp 9          (warp 11 only completes the warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
-//                   one box per lane, in the order K0 K1 V0 K2 V1 ... in which they are consumed
+//   warp 9          TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
+//                   in the order K0 K1 V0 K2 V1 ... in which they are consumed
 //
 // The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
 // CTA: causal prompts and ragged caches are balanced alike.  Items that span CTAs leave unnormalised partial results
@@ -34,16 +34,15 @@ namespace kv {
 namespace {
 
 constexpr int TILE = 128;
-constexpr int THREADS = 384;
-// Registers: launched with 168 a thread (3 x 168 = 504 per thread of a warpgroup row); the softmax warpgroups take 200
-// each and leave 104 to the third, 2 x 200 + 104 = 504.
-constexpr int REGS_SOFTMAX = 200, REGS_OTHER = 104;
+constexpr int THREADS = 352;  // 11 warps: at most 168 registers a thread
 constexpr uint32_t B_MN_MAJOR = 1u << 16;
+constexpr float P0 = 1.0f, P1 = 0.6931210160255432f, P2 = 0.2402234971523285f, P3 = 0.055921975523233414f, P4 = 0.00966636836528778f;  // see ex2_poly
+constexpr int POLY_AT = 1;  // every fourth pair of exponentials is computed on the multiply-add pipe
 
 template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
     static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BARS = 2 * STAGES + 10;
+    static constexpr int BARS = 2 * STAGES + 12;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maximum and sum of stream 1's rows
     static constexpr int PRE_AT = ML_AT + 2 * 128 * 4;
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
@@ -239,6 +238,52 @@ __device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
         ::I8(r, 0), I8(r, 8), I8(r, 16), I8(r, 24), "r"(addr)
         : "memory");
 }
+// pairs of f32 in one register pair
+__device__ inline uint64_t f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ inline float lo(uint64_t x) {
+    return __uint_as_float((uint32_t)x);
+}
+__device__ inline float hi(uint64_t x) {
+    return __uint_as_float((uint32_t)(x >> 32));
+}
+__device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ inline uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// 2^x for a pair on the multiply-add pipe, for x <= 16: x = n + f with n the nearest integer, 2^f by the polynomial
+// that interpolates it at the five Chebyshev nodes of [-1/2, 1/2] (relative error below 4e-6, and of either sign),
+// 2^n by adding to the exponent.  Arguments below -127 (masked slots) give less than 2^-126.
+__device__ inline uint64_t ex2_poly(uint64_t x) {
+    const float x0 = fmaxf(lo(x), -127.0f), x1 = fmaxf(hi(x), -127.0f);
+    const uint64_t y = f2(x0, x1);
+    const float big = 12582912.0f;  // 1.5 * 2^23: the sum's last bits are the nearest integer
+    const uint64_t t = add2(y, f2(big, big));
+    const uint64_t n = add2(t, f2(-big, -big));
+    const uint64_t f = fma2(n, f2(-1.0f, -1.0f), y);
+    uint64_t p = f2(P4, P4);
+    p = fma2(p, f, f2(P3, P3));
+    p = fma2(p, f, f2(P2, P2));
+    p = fma2(p, f, f2(P1, P1));
+    p = fma2(p, f, f2(P0, P0));
+    return f2(__int_as_float(__float_as_int(lo(p)) + (__float_as_int(lo(t)) << 23)), __int_as_float(__float_as_int(hi(p)) + (__float_as_int(hi(t)) << 23)));
+}
+
 __device__ inline uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 __device__ inline bool elect_one() {
     uint32_t p;
@@ -266,25 +311,25 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto s_full = [&](int x) { return bars + 8u * (2 * NS + x); };
-    auto p_ready = [&](int x) { return bars + 8u * (2 * NS + 2 + x); };
-    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 4 + x); };
-    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 6 + x); };
-    auto drained = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
+    auto p_ready = [&](int x, int hf) { return bars + 8u * (2 * NS + 2 + 2 * hf + x); };
+    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 6 + x); };
+    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
+    auto drained = [&](int x) { return bars + 8u * (2 * NS + 10 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *pre = reinterpret_cast<int *>(smem + C::PRE_AT);
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
             mbar_init(full(s), 1);
-            mbar_init(empty(s), 2);  // both streams, or the one that uses the tile twice
+            mbar_init(empty(s), 2);  // both streams
         }
         for (int x = 0; x < 2; x++) {
             mbar_init(s_full(x), 1);
-            mbar_init(p_ready(x), 128);
+            mbar_init(p_ready(x, 0), 128);
+            mbar_init(p_ready(x, 1), 128);
             mbar_init(o_done(x), 1);
             mbar_init(q_ready(x), 128);
             mbar_init(drained(x), 1);
@@ -307,12 +352,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 
     if (u0 < u1) {
         if (warp >= 8) {
-          asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
           Line c = seek(v, tpt, pre, u0);
           if (warp == 9) {
             // ---------------------------------------------------------------- TMA
             const unsigned long long pol = policy_evict_normal();
-            const int per_tile = TILE >> v.page_shift, boxes = per_tile * HALVES;  // at most 16
+            const int per_tile = TILE >> v.page_shift;  // pages of a tile: at most 8
             const uint32_t box_bytes = (uint32_t)v.page * 128u;
             uint32_t g = 0;
             bool ok = true;
@@ -323,22 +367,35 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     const bool is_v = i == 2 * n - 1 || (i >= 2 && (i & 1) == 0);
                     const int t = is_v ? (i == 2 * n - 1 ? n - 1 : (i - 2) >> 1) : (i == 0 ? 0 : (i + 1) >> 1);
                     const int s = g % NS;
-                    const int idx = lane % per_tile, half = lane / per_tile;
-                    const int slot = tile_of(c.p, c.unit + t) * TILE + (idx << v.page_shift);
-                    // pages past the length and pages that no row of the item sees are not fetched
-                    const bool on = lane < boxes && slot < c.q.s.L && (slot + v.page > c.p.first || slot < v.sinks);
-                    const int page = on ? page_of(v, c.b, slot) : 0;
-                    const unsigned n_on = __popc(__ballot_sync(~0u, on));
+                    // lane i looks up the tile's i-th page; one elected lane issues all copies.  Pages past the
+                    // length and pages that no row of the item sees are not fetched.
+                    const int slot0 = tile_of(c.p, c.unit + t) * TILE, slot = slot0 + (lane << v.page_shift);
+                    const bool on = lane < per_tile && slot < c.q.s.L && (slot + v.page > c.p.first || slot < v.sinks);
+                    const int row = on ? (page_of(v, c.b, slot) * v.Hkv + c.h) << v.page_shift : 0;
+                    const unsigned which = __ballot_sync(~0u, on);
                     ok = __all_sync(~0u, mbar_wait(empty(s), ((g / NS) & 1u) ^ 1u, abort_flag));
                     if (!ok) {
                         give_up();
                         break;
                     }
-                    if (lane == 0) mbar_expect_tx(full(s), n_on * box_bytes);
+                    const bool leader = elect_one();
+                    if (leader) mbar_expect_tx(full(s), __popc(which) * (uint32_t)HALVES * box_bytes);
+                    for (int p = 0; p < per_tile; p++) {
+                        const int r = __shfl_sync(~0u, row, p);
+                        if (which >> p & 1) {
+                            const uint32_t dst = ring + s * C::TILE_BYTES + (uint32_t)(p << v.page_shift) * 128u;
+                            if (leader) {
+                                if (is_v) {
+#pragma unroll
+                                    for (int hf = 0; hf < HALVES; hf++) tma_load_2d(dst + hf * 16384, &tmap_v, hf * 64, r, full(s), pol);
+                                } else {
+#pragma unroll
+                                    for (int hf = 0; hf < HALVES; hf++) tma_load_2d(dst + hf * 16384, &tmap_k, hf * 64, r, full(s), pol);
+                                }
+                            }
+                        }
+                    }
                     __syncwarp();
-                    if (on)
-                        tma_load_2d(ring + s * C::TILE_BYTES + half * 16384 + (uint32_t)(idx << v.page_shift) * 128u, is_v ? &tmap_v : &tmap_k,
-                                    half * 64, (page * v.Hkv + c.h) << v.page_shift, full(s), pol);
                     g++;
                 }
                 u += n;
@@ -370,45 +427,66 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 tc_fence_after();
                 return ok;
             };
+            // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
+            // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
             for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
                 const int n = min(c.p.units - c.unit, u1 - u);
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
-                const int step = shared_rows ? 2 : 1, t0 = shared_rows ? x : 0;
-                auto qk = [&](int t) {
+                const int ahead = shared_rows ? 2 : 1;  // K tiles in front of V tiles
+                auto mine = [&](int t) { return !shared_rows || (t & 1) == x; };
+                bool begun = false;
+                auto k_tile = [&](int t) {
                     const uint32_t at = g + pos_k(t), s = at % NS;
                     if (!wait(full(s), at / NS)) return;
-                    const unsigned long long kd = smem_desc_sw128(ring + s * C::TILE_BYTES);
-                    if (elect_one()) {
+                    if (mine(t)) {
+                        if (!begun) {
+                            if (!wait(q_ready(x), n_q)) return;
+                            n_q++;
+                        }
+                        begun = true;
+                        const unsigned long long kd = smem_desc_sw128(ring + s * C::TILE_BYTES);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < D / 16; k++)
-                            umma_bf16(t_s, qd + (k / 4) * (16384 >> 4) + 2 * (k % 4), kd + (k / 4) * (16384 >> 4) + 2 * (k % 4), idesc_s, k != 0);
-                        umma_commit(s_full(x));
-                        umma_commit(empty(s));
-                        if (shared_rows) umma_commit(empty(s));
+                            for (int k = 0; k < D / 16; k++)
+                                umma_bf16(t_s, qd + (k / 4) * (16384 >> 4) + 2 * (k % 4), kd + (k / 4) * (16384 >> 4) + 2 * (k % 4), idesc_s, k != 0);
+                            umma_commit(s_full(x));
+                            umma_commit(empty(s));
+                        }
+                    } else if (elect_one()) {
+                        mbar_arrive(empty(s));
                     }
                     __syncwarp();
                 };
-                if (t0 < n) {
-                    wait(q_ready(x), n_q);
-                    n_q++;
-                    if (ok) qk(t0);
-                }
-                for (int t = t0; ok && t < n; t += step) {
-                    if (!wait(p_ready(x), n_p)) break;
-                    n_p++;
+                auto v_tile = [&](int t) {
                     const uint32_t at = g + pos_v(t, n), s = at % NS;
-                    if (!wait(full(s), at / NS)) break;
-                    const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
-                    if (elect_one()) {
+                    if (!wait(full(s), at / NS)) return;
+                    if (mine(t)) {
+                        const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
+                        if (!wait(p_ready(x, 0), n_p)) return;
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < TILE / 16; k++)
-                            umma_ts(t_o, t_s + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, k == 0 ? t != t0 : 1);
-                        umma_commit(empty(s));
-                        if (shared_rows) umma_commit(empty(s));
-                        if (t + step >= n) umma_commit(o_done(x));
+                            for (int k = 0; k < 4; k++)
+                                umma_ts(t_o, t_s + 64 + k * 8, vd + (unsigned long long)(k + 4) * (2048 >> 4), idesc_o, k == 0 ? t >= ahead : 1);
+                        }
+                        __syncwarp();
+                        if (!wait(p_ready(x, 1), n_p)) return;
+                        n_p++;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < 4; k++)
+                                umma_ts(t_o, t_s + 96 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, 1);
+                            umma_commit(empty(s));
+                            if (t + ahead >= n) umma_commit(o_done(x));
+                        }
+                    } else if (elect_one()) {
+                        mbar_arrive(empty(s));
                     }
                     __syncwarp();
-                    if (t + step < n) qk(t + step);
+                };
+                for (int t = 0; ok && t < ahead && t < n; t++) k_tile(t);
+                for (int t = 0; ok && t < n; t++) {
+                    v_tile(t);
+                    if (ok && t + ahead < n) k_tile(t + ahead);
                 }
                 g += 2 * n;
                 u += n;
@@ -421,7 +499,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
         } else {
             // ---------------------------------------------------------------- softmax of stream x
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
             Line c = seek(v, tpt, pre, u0);
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
@@ -460,16 +537,21 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 fetch_queries(c);
                 queries_ready();
             }
-            Line nx = c;
-            for (int u = u0; u < u1; c = nx) {
+            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
                 const int n = min(c.p.units - c.unit, u1 - u);
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
                 const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
                 const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
                 const int n_rows = tok * v.G;
-                next_item(v, tpt, pre, nx);
                 if (!shared_rows && x == 1) bar_arrive(2, 256);  // stream 0 goes first
-                const bool more = u + n < u1 && has_tile(nx.p, x, min(nx.p.units, u1 - u - n));  // queries to fetch for the next item
+                auto fetch_next = [&]() {  // the next item's queries, if this stream has a tile of it
+                    if (u + n >= u1) return false;
+                    Line nx = c;
+                    next_item(v, tpt, pre, nx);
+                    if (!has_tile(nx.p, x, min(nx.p.units, u1 - u - n))) return false;
+                    fetch_queries(nx);
+                    return true;
+                };
                 const int p_first = c.q.s.L - c.q.s.nq + ta;           // slot of the stream's first token
                 const int my_p = p_first + min(row, n_rows - 1) / v.G, p_last = p_first + tok - 1;
                 float m = -INFINITY, l = 0.0f;
@@ -480,28 +562,39 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     wait(s_full(x), n_s);
                     n_s++;
                     // this stream's last product with its queries is done: fetch the next ones under the softmax
-                    const bool closing = more && t + step >= n;
-                    if (closing) fetch_queries(nx);
-                    uint32_t sr[2][64];
-                    tmem_ld64(t_s, sr[0]);
-                    tmem_ld64(t_s + 64, sr[1]);
-                    if (j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window)) {
-                        // one bit per slot of the tile; no branch per element
+                    const bool fetched = t + step >= n && fetch_next();
+                    // Scores of slots 0..63 are read for the maximum and again for their exponentials; those of slots
+                    // 64..127 stay in registers, and the weights are written over their columns.
+                    const bool masked = j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window);
+                    uint32_t bits[4];  // with masked: one bit per slot of the tile that the row sees
+                    if (masked) {
                         const int hi = my_p - j0 + 1, lo = v.window ? my_p - v.window + 1 - j0 : 0, sk = v.sinks - j0;
 #pragma unroll
-                        for (int w = 0; w < 4; w++) {
-                            const uint32_t bits = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
-#pragma unroll
-                            for (int i = 0; i < 32; i++) {
-                                uint32_t &s = sr[w >> 1][(w & 1) * 32 + i];
-                                s = bits & (1u << i) ? s : 0xff800000u;
-                            }
-                        }
+                        for (int w = 0; w < 4; w++)
+                            bits[w] = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
                     }
-                    float mx = -INFINITY;
+                    uint32_t sr[64];
+                    auto hide = [&](uint32_t b0, uint32_t b1) {
 #pragma unroll
-                    for (int i = 0; i < 128; i += 2)
-                        mx = fmaxf(mx, fmaxf(__uint_as_float(sr[i >> 6][i & 63]), __uint_as_float(sr[i >> 6][(i + 1) & 63])));
+                        for (int i = 0; i < 32; i++) {
+                            sr[i] = b0 & (1u << i) ? sr[i] : 0xff800000u;
+                            sr[32 + i] = b1 & (1u << i) ? sr[32 + i] : 0xff800000u;
+                        }
+                    };
+                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto raise_max = [&]() {
+#pragma unroll
+                        for (int i = 0; i < 64; i += 8)
+#pragma unroll
+                            for (int j = 0; j < 4; j++) mx4[j] = max3(mx4[j], __uint_as_float(sr[i + j]), __uint_as_float(sr[i + 4 + j]));
+                    };
+                    tmem_ld64(t_s, sr);
+                    if (masked) hide(bits[0], bits[1]);
+                    raise_max();
+                    tmem_ld64(t_s + 64, sr);
+                    if (masked) hide(bits[2], bits[3]);
+                    raise_max();
+                    float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                     mx *= scale;
                     const bool raise = mx > m + 8.0f;
                     if (first) {
@@ -514,29 +607,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
                         for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
                     }
-                    // Streams of one piece take turns with the exponentials: left alone they fall into step, and then both
-                    // wait for the tensor pipe and both queue at the exponential unit.
-                    if (!shared_rows) bar_sync(2 + x, 256);
-                    const float ref = m == -INFINITY ? 0.0f : m;
-                    float sum[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int hf = 0; hf < 2; hf++) {
-                        uint32_t pw[32];
-#pragma unroll
-                        for (int i = 0; i < 32; i++) {
-                            const float e0 = ex2(fmaf(__uint_as_float(sr[hf][2 * i]), scale, -ref));
-                            const float e1 = ex2(fmaf(__uint_as_float(sr[hf][2 * i + 1]), scale, -ref));
-                            sum[i & 1] += e0;
-                            sum[2 + (i & 1)] += e1;
-                            pw[i] = pack2(e0, e1);
-                        }
-                        tmem_st32(t_s + hf * 32, pw);
-                    }
-                    if (!shared_rows && (x == 0 || t + 1 < n)) bar_arrive(3 - x, 256);  // (every arrival is waited for)
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
                     // slots that nobody sees may hold anything: their values are cleared before the product
-                    const int dead_from = c.q.s.L - j0;
-                    if (dead_from < TILE || (j0 < c.p.first && c.p.first > v.sinks)) {
+                    if (c.q.s.L - j0 < TILE || (j0 < c.p.first && c.p.first > v.sinks)) {
                         const uint32_t at = g + pos_v(t, n), s = at % NS;
                         wait(full(s), at / NS);
                         const int j = j0 + row;
@@ -548,17 +620,41 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                                     *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + hh * 16384 + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
                         }
                         fence_async_shared();
+                        __syncwarp();
                     }
-                    tmem_st_wait();
-                    tc_fence_before();
-                    mbar_arrive(p_ready(x));
-                    if (closing) queries_ready();
+                    // Streams of one piece take turns with the exponentials: left alone they fall into step, and then both
+                    // wait for the tensor pipe and both queue at the exponential unit.
+                    if (!shared_rows) bar_sync(2 + x, 256);
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    const uint64_t scale2 = f2(scale, scale), ref2 = f2(-ref, -ref);
+                    uint64_t sum2[2] = {0, 0};
+#pragma unroll
+                    for (int hf = 0; hf < 2; hf++) {
+                        if (hf == 1) {
+                            tmem_ld64(t_s, sr);
+                            if (masked) hide(bits[0], bits[1]);
+                        }
+                        uint32_t pw[32];
+#pragma unroll
+                        for (int i = 0; i < 32; i++) {
+                            const uint64_t y = fma2(f2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, ref2);
+                            const uint64_t e = i % 4 == POLY_AT ? ex2_poly(y) : f2(ex2(lo(y)), ex2(hi(y)));
+                            sum2[i & 1] = add2(sum2[i & 1], e);
+                            pw[i] = pack2(lo(e), hi(e));
+                        }
+                        tmem_st32(t_s + 64 + hf * 32, pw);
+                        if (hf == 1 && !shared_rows && (x == 0 || t + 1 < n)) bar_arrive(3 - x, 256);  // (every arrival is waited for)
+                        tmem_st_wait();
+                        tc_fence_before();
+                        mbar_arrive(p_ready(x, hf));
+                    }
+                    const uint64_t sum = add2(sum2[0], sum2[1]);
+                    l += lo(sum) + hi(sum);
+                    if (fetched) queries_ready();
                 }
-                if (first && more) {  // (no tile in this segment: its own queries were not fetched)
-                    fetch_queries(nx);
-                    queries_ready();
-                }
+                if (first && fetch_next()) queries_ready();  // (no tile in this segment, and no queries were fetched for it)
                 // ---- the segment is done: store, or leave a partial result
+                if (m == -INFINITY) l = 0.0f;  // (the polynomial leaves a trace for masked slots)
                 const bool any = !first;
                 if (any) {
                     wait(o_done(x), n_o);
@@ -596,6 +692,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll
                     for (int k = 0; k < D / 32; k++) {
                         float ov[32];
+                        __syncwarp();  // (the stores below leave lanes without a row behind)
                         tmem_ld32(t_o + k * 32, ov);
                         if (both) {
                             float o1[32];
@@ -627,6 +724,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         }
                     }
                 }
+                __syncwarp();
                 tc_fence_before();
                 if (both) bar_sync(1, 256);  // stream 1's tensor memory is read
                 g += 2 * n;
@@ -634,10 +732,12 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
         }
     }
+    // the joining kernel may come up while the last CTAs store their results; it waits for the whole grid
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 8) tmem_dealloc(tmem, 512);
+    if (warp == 8) tmem_dealloc(*tmem_slot, 512);
 }
 
 // Joins the partial results of the items that span CTAs.  CTA (i, y) serves 32 rows of the item whose first

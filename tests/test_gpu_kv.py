@@ -102,6 +102,23 @@ def test_attend_large_scores_and_equal_keys(n, D):
     s.check_attend(out, lse, 0, 0, rounded_weights=True)
 
 
+@pytest.mark.parametrize("D,page", [(128, 32), (64, 16)])
+def test_attend_many_tiles_per_cta(D, page):
+    """Windows whose two streams share the rows, over enough tiles that the ring of loads wraps several times in a
+    CTA, with cold and warm caches (loads then land out of order): the same bits every time, and the right ones."""
+    import torch
+
+    s = Setup(4, [4096, 3000, 4095, 2049, 700, 4096, 1, 4096], [17] * 8, 32, 8, D, page, ragged=False)
+    h = s.handle()
+    out, lse = _attend(s, h, 0, 0)
+    flush = torch.empty(64 * 1024 * 1024, device="cuda")
+    for _ in range(30):
+        flush.zero_()
+        again, lse2 = _attend(s, h, 0, 0)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+    s.check_attend(out, lse, 0, 0, rounded_weights=True)
+
+
 @pytest.mark.parametrize("n", [1, 17])
 def test_attend_joins_many_calls_on_one_handle(n):
     """Calls of different shape back to back: the counters and partial results of one leave nothing for the next."""
