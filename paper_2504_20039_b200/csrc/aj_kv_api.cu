@@ -314,6 +314,10 @@ aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *l
     a.scale_log2 = scale * kv::LOG2E;
     a.status = h->status;
     h->last_launches = 1;
+    if (h->tensor) {
+        h->last_path = "mma";
+        return done(kv::launch_weigh_mma(a, (cudaStream_t)cuda_stream));
+    }
     h->last_path = "simt";
     return done(kv::launch_weigh_simt(a, h->dtype == AJ_BF16, (cudaStream_t)cuda_stream));
 }

@@ -71,10 +71,146 @@ __global__ void __launch_bounds__(128) append_any_kernel(AppendArgs a) {
     }
 }
 
+// ---- head sizes 64 and 128 in 16-byte pieces: E elements per lane, D / E lanes per head vector
+//
+// A warp takes one token and UNROLL x (vectors per warp) neighbouring heads: all loads are issued first, and the
+// token's cosines and sines stay in registers for all of them.  The other element of a rotated pair lies in the same
+// lane (PAIRS) or `mate` lanes away (mate = rot / 2 / E, a power of two), one shuffle per element.
+
+constexpr int UNROLL = 4, FAST_WARPS = 4;
+
+template <typename T, int D, bool PAIRS>
+__global__ void __launch_bounds__(32 * FAST_WARPS) append_vec_kernel(AppendArgs a, int chunks) {
+    constexpr int E = 16 / (int)sizeof(T), LV = D / E, VW = 32 / LV;
+    const View &v = a.v;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LV, i0 = (lane % LV) * E;
+    const long long at = (long long)blockIdx.x * FAST_WARPS + warp;
+    const int b = blockIdx.y, t = (int)(at / chunks), first = (int)(at - (long long)t * chunks) * (UNROLL * VW) + sub;
+    const Seq s = seq_of(v, b);
+    if (t >= s.nq) return;
+    const size_t row = (size_t)s.row0 + t;
+    const int slot = s.L - s.nq + t, heads = v.Hq + 2 * v.Hkv;
+    union Piece {
+        uint4 u;
+        T t[E];
+    } x[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; u++) {
+        const int hh = first + u * VW;
+        const T *src = hh < v.Hq             ? (const T *)a.q + row * a.q_stride + (size_t)hh * D
+                       : hh < v.Hq + v.Hkv   ? (const T *)a.k + row * a.k_stride + (size_t)(hh - v.Hq) * D
+                                             : (const T *)a.vv + row * a.v_stride + (size_t)(hh - v.Hq - v.Hkv) * D;
+        x[u].u = hh < heads ? __ldcs(reinterpret_cast<const uint4 *>(src + i0)) : make_uint4(0, 0, 0, 0);
+    }
+    int page = -1;
+    if (slot >= 0) {
+        page = __ldg(v.table + (size_t)b * v.width + (slot >> v.page_shift));
+        if ((unsigned)page >= (unsigned)v.n_pages) page = -1;
+    }
+    const int pos = a.positions ? __ldg(a.positions + row) : slot;
+    const int half = a.rot >> 1, mate = half / E;
+    const bool turns = i0 < a.rot, second = !PAIRS && i0 >= half;
+    float co[PAIRS ? E / 2 : E], si[PAIRS ? E / 2 : E];
+    if (turns) {
+        const float *cs = a.cos_sin + (size_t)min(max(pos, 0), a.n_pos - 1) * a.rot + (PAIRS ? i0 >> 1 : second ? i0 - half : i0);
+#pragma unroll
+        for (int e = 0; e < (PAIRS ? E / 2 : E); e += 2) {
+            const float2 c2 = __ldg(reinterpret_cast<const float2 *>(cs + e)), s2 = __ldg(reinterpret_cast<const float2 *>(cs + half + e));
+            co[e] = c2.x;
+            co[e + 1] = c2.y;
+            si[e] = s2.x;
+            si[e + 1] = s2.y;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; u++) {
+        const int hh = first + u * VW;
+        const bool is_q = hh < v.Hq, is_v = hh >= v.Hq + v.Hkv;
+        float y[E];
+#pragma unroll
+        for (int e = 0; e < E; e++) y[e] = to_f32(x[u].t[e]);
+        const float *w = is_q ? a.q_norm : a.k_norm;
+        if (a.q_norm || a.k_norm) {  // uniform; the lanes of one vector agree on w
+            float sq = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; e++) sq += y[e] * y[e];
+#pragma unroll
+            for (int o = LV / 2; o; o >>= 1) sq += __shfl_xor_sync(~0u, sq, o);
+            if (w && !is_v) {
+                const float r = rsqrtf(sq * (1.0f / D) + a.eps);
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const float4 g = __ldg(reinterpret_cast<const float4 *>(w + i0 + e));
+                    y[e] *= r * g.x;
+                    y[e + 1] *= r * g.y;
+                    y[e + 2] *= r * g.z;
+                    y[e + 3] *= r * g.w;
+                }
+            }
+        }
+        if (PAIRS) {
+            if (turns && !is_v) {
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float p = y[e], q = y[e + 1];
+                    y[e] = p * co[e / 2] - q * si[e / 2];
+                    y[e + 1] = q * co[e / 2] + p * si[e / 2];
+                }
+            }
+        } else if (a.rot) {
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const float o = __shfl_xor_sync(~0u, y[e], mate);
+                if (turns && !is_v) y[e] = second ? y[e] * co[e] + o * si[e] : y[e] * co[e] - o * si[e];
+            }
+        }
+        if (!is_v) {
+#pragma unroll
+            for (int e = 0; e < E; e++) x[u].t[e] = from_f32<T>(y[e]);
+        }
+        if (hh >= heads) continue;
+        if (is_q) {
+            *reinterpret_cast<uint4 *>((T *)a.q_out + row * a.q_out_stride + (size_t)hh * D + i0) = x[u].u;
+        } else if (slot >= 0) {
+            const int h = is_v ? hh - v.Hq - v.Hkv : hh - v.Hq;
+            if (page >= 0)
+                *reinterpret_cast<uint4 *>((T *)(is_v ? a.v_pages : a.k_pages) + (((size_t)page * v.Hkv + h) * v.page + (slot & (v.page - 1))) * D + i0) = x[u].u;
+            if (!is_v && i0 == 0) {
+                const size_t i = ((size_t)b * v.Hkv + h) * v.cap + slot;
+                if (a.slot_pos) a.slot_pos[i] = pos;
+                if (a.weight) a.weight[i] = 0.0f;
+            }
+        }
+    }
+}
+
+template <typename T, int D> cudaError_t append_vec(const AppendArgs &a, cudaStream_t s) {
+    constexpr int E = 16 / (int)sizeof(T), VW = 32 / (D / E);
+    const int heads = a.v.Hq + 2 * a.v.Hkv, chunks = (heads + UNROLL * VW - 1) / (UNROLL * VW);
+    const dim3 grid((unsigned)(((long long)a.v.n_q * chunks + FAST_WARPS - 1) / FAST_WARPS), a.v.B);
+    if (a.interleaved)
+        append_vec_kernel<T, D, true><<<grid, 32 * FAST_WARPS, 0, s>>>(a, chunks);
+    else
+        append_vec_kernel<T, D, false><<<grid, 32 * FAST_WARPS, 0, s>>>(a, chunks);
+    return cudaGetLastError();
+}
+
+// Can the vector kernel rotate by `rot` elements?  Whole pieces on both sides, and partners at a power of two.
+bool vec_rotation(int rot, int interleaved, int E) {
+    if (rot == 0) return true;
+    if (interleaved) return rot % E == 0;
+    const int mate = rot / 2 / E;
+    return rot / 2 % E == 0 && mate > 0 && (mate & (mate - 1)) == 0;
+}
+
 }  // namespace
 
 cudaError_t launch_append(const AppendArgs &a, bool bf16, cudaStream_t s) {
-    const int heads = a.v.Hq + 2 * a.v.Hkv;
+    const int heads = a.v.Hq + 2 * a.v.Hkv, D = a.v.D;
+    if ((D == 64 || D == 128) && vec_rotation(a.rot, a.interleaved, bf16 ? 8 : 4)) {
+        if (bf16) return D == 64 ? append_vec<__nv_bfloat16, 64>(a, s) : append_vec<__nv_bfloat16, 128>(a, s);
+        return D == 64 ? append_vec<float, 64>(a, s) : append_vec<float, 128>(a, s);
+    }
     const dim3 grid((unsigned)(((long long)a.v.n_q * heads + 3) / 4), a.v.B);
     if (bf16)
         append_any_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(a);

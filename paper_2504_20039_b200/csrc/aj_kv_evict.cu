@@ -5,7 +5,7 @@
 // lower slots first among equals; then move the r-th kept slot past `keep` into the r-th dropped slot below it.
 // Sources lie at or past `keep` and destinations below it, so the moves touch disjoint slots and need no order.
 //
-// A cluster of CTAs serves one (sequence, head): each selects for itself (a radix select of four 8-bit digits over
+// A cluster of CTAs serves one (sequence, head): each selects for itself (a radix select of three digits over
 // keys in shared memory reads 8 bytes per slot, from L2 but for the first) and then makes its share of the moves,
 // which are what costs: 4 * D elements read or written per moved slot.  With few (sequence, head) pairs a
 // larger cluster spreads them over the SMs.  Nothing is written before every CTA of the cluster has selected, so the
@@ -20,10 +20,11 @@ namespace {
 constexpr int THREADS = 1024, NWARP = THREADS / 32;
 constexpr int LIST = 4096;             // moves a CTA lists at a time
 constexpr int KEYS_MAX = 40 * 1024;    // slots whose keys fit in shared memory; longer ones re-read the weights
-constexpr int HIST = 8;                // copies of the histogram, so that equal digits of a warp group do not queue up
+constexpr int BINS = 2048;             // digits of 11, 11 and 10 bits: the first one is a float's sign, exponent and two
+                                       // bits of its fraction, so that weights of one magnitude do not queue up at one counter
 
 struct Shared {
-    unsigned hist[HIST][256];
+    unsigned hist[BINS];
     unsigned scan[NWARP + 1], scan2[NWARP + 1];
     int newest, need;
     unsigned prefix;
@@ -92,60 +93,57 @@ __global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned
         sh.need = keep;
     }
     __syncthreads();
+    auto weight_key = [&](float w) -> unsigned { return w != w ? 0u : ordered_image(w); };
     int newest = -0x7fffffff - 1;
-    for (int j = threadIdx.x; j < L; j += THREADS) newest = max(newest, __ldcg(p_in + j));
+#pragma unroll 8
+    for (int j = threadIdx.x; j < L; j += THREADS) {
+        newest = max(newest, __ldcg(p_in + j));
+        if (cached) keys[j] = weight_key(__ldcg(w_in + j));
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
     if (lane == 0) atomicMax(&sh.newest, newest);
     __syncthreads();
     const long long recent_from = (long long)sh.newest - a.recent;
-    auto make_key = [&](int j) -> unsigned {
+    auto fixed = [&](int j) {
         const int p = __ldcg(p_in + j);
-        const float w = __ldcg(w_in + j);
-        if (p < a.sinks || p > recent_from) return 0xffffffffu;
-        return w != w ? 0u : ordered_image(w);
+        return p < a.sinks || p > recent_from;
     };
-    auto key_at = [&](int j) -> unsigned { return cached ? keys[j] : make_key(j); };
-    if (cached) {
-        for (int j = threadIdx.x; j < L; j += THREADS) keys[j] = make_key(j);
-    }
+    auto key_at = [&](int j) -> unsigned { return cached ? keys[j] : fixed(j) ? 0xffffffffu : weight_key(__ldcg(w_in + j)); };
 
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = threadIdx.x; i < HIST * 256; i += THREADS) (&sh.hist[0][0])[i] = 0;
+    for (int digit = 0; digit < 3; digit++) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
+        for (int i = threadIdx.x; i < BINS; i += THREADS) sh.hist[i] = 0;
         __syncthreads();
-        const unsigned prefix = sh.prefix, high = shift == 24 ? 0u : ~0u << (shift + 8);
+        const unsigned prefix = sh.prefix, high = digit == 0 ? 0u : digit == 1 ? ~0u << 21 : ~0u << 10;
+#pragma unroll 8
         for (int j = threadIdx.x; j < L; j += THREADS) {
-            const unsigned k = key_at(j);
-            if (((k ^ prefix) & high) == 0) atomicAdd(&sh.hist[warp % HIST][(k >> shift) & 255], 1u);
+            unsigned k;
+            if (digit == 0 && cached) {  // the protected slots become known only now
+                k = fixed(j) ? 0xffffffffu : keys[j];
+                keys[j] = k;
+            } else {
+                k = key_at(j);
+            }
+            if (((k ^ prefix) & high) == 0) atomicAdd(&sh.hist[(k >> shift) & (bins - 1)], 1u);
         }
         __syncthreads();
-        if (warp == 0) {
-            // lane i holds digits 255 - 8 i .. 248 - 8 i, from the top
-            unsigned c[8], mine = 0;
+        // thread i holds the digits bins - 1 - 2 i and bins - 2 - 2 i, from the top
+        const int d0 = bins - 1 - 2 * (int)threadIdx.x;
+        const unsigned c0 = d0 >= 1 ? sh.hist[d0] : 0u, c1 = d0 >= 1 ? sh.hist[d0 - 1] : 0u;
+        unsigned up = c0 + c1;
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                c[i] = 0;
-#pragma unroll
-                for (int r = 0; r < HIST; r++) c[i] += sh.hist[r][255 - 8 * lane - i];
-                mine += c[i];
-            }
-            unsigned up = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned z = __shfl_up_sync(~0u, up, o);
-                if (lane >= o) up += z;
-            }
-            unsigned before = up - mine;
-            const unsigned need = (unsigned)sh.need;
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (before < need && need <= before + c[i]) {
-                    sh.prefix = prefix | ((unsigned)(255 - 8 * lane - i) << shift);
-                    sh.need = (int)(need - before);
-                }
-                before += c[i];
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned z = __shfl_up_sync(~0u, up, o);
+            if (lane >= o) up += z;
+        }
+        scan_warps(sh.scan, __shfl_sync(~0u, up, 31));
+        const unsigned before = sh.scan[warp] + up - c0 - c1, want = (unsigned)sh.need;
+        __syncthreads();
+        if (before < want && want <= before + c0 + c1) {
+            const bool one = want <= before + c0;
+            sh.prefix = prefix | ((unsigned)(one ? d0 : d0 - 1) << shift);
+            sh.need = (int)(want - before - (one ? 0 : c0));
         }
         __syncthreads();
     }
@@ -242,17 +240,23 @@ __global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned
             const int dst = list[i], src = list[LIST + i];
             a.weight_out[at + dst] = __ldcg(w_in + src);
             a.slot_pos_out[at + dst] = __ldcg(p_in + src);
+            const int page = __ldg(v.table + (size_t)b * v.width + (dst >> v.page_shift));
+            // a page that is not in the pool is never written
+            list[i] = (unsigned)page < (unsigned)v.n_pages ? (unsigned)((page * v.Hkv + h) * v.page + (dst & (v.page - 1))) : ~0u;
+            list[LIST + i] = (unsigned)page_row(v, b, h, src);
         }
+        __syncthreads();
         const int pieces = (c1 - c0) * n16;
+#pragma unroll 4
         for (int i = threadIdx.x; i < pieces; i += THREADS) {
             const int r = i / n16, c = i - r * n16;
-            const int dst = list[r], page = __ldg(v.table + (size_t)b * v.width + (dst >> v.page_shift));
-            if ((unsigned)page >= (unsigned)v.n_pages) continue;  // not in the pool: never written
-            const size_t from = page_row(v, b, h, list[LIST + r]) * n16 + c;
-            const size_t to = (((size_t)page * v.Hkv + h) * v.page + (dst & (v.page - 1))) * n16 + c;
+            const size_t from = (size_t)list[LIST + r] * n16 + c;
             const uint4 x = __ldcg((const uint4 *)a.k_pages + from), y = __ldcg((const uint4 *)a.v_pages + from);
-            ((uint4 *)a.k_pages)[to] = x;
-            ((uint4 *)a.v_pages)[to] = y;
+            if (list[r] != ~0u) {
+                const size_t to = (size_t)list[r] * n16 + c;
+                ((uint4 *)a.k_pages)[to] = x;
+                ((uint4 *)a.v_pages)[to] = y;
+            }
         }
         __syncthreads();
     }

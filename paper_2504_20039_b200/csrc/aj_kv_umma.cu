@@ -11,7 +11,7 @@
 //
 //   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); load the stream's queries, store results
 //   warps 8, 10     issue tcgen05.mma for stream 0 and 1: PV of a tile, then QK^T of the stream's next
-//   warp 9          TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
+//   warp 9          (warp 11 only completes its warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
 //                   in the order K0 K1 V0 K2 V1 ... in which they are consumed
 //
 // The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
@@ -34,10 +34,11 @@ namespace kv {
 namespace {
 
 constexpr int TILE = 128;
-constexpr int THREADS = 352;  // 11 warps: at most 168 registers a thread
+constexpr int THREADS = 384;
+// Registers: launched with 168 a thread; the two softmax warpgroups, which hold a row of 128 scores, take 200 and leave
+// 104 to the third (2 x 200 + 104 = 3 x 168).  Each branch sets its own share: before that no code is shared.
+constexpr int REGS_SOFTMAX = 200, REGS_OTHER = 104;
 constexpr uint32_t B_MN_MAJOR = 1u << 16;
-constexpr float P0 = 1.0f, P1 = 0.6931210160255432f, P2 = 0.2402234971523285f, P3 = 0.055921975523233414f, P4 = 0.00966636836528778f;  // see ex2_poly
-constexpr int POLY_AT = 1;  // every fourth pair of exponentials is computed on the multiply-add pipe
 
 template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
@@ -266,24 +267,6 @@ __device__ inline float max3(float a, float b, float c) {
     return r;
 }
 
-// 2^x for a pair on the multiply-add pipe, for x <= 16: x = n + f with n the nearest integer, 2^f by the polynomial
-// that interpolates it at the five Chebyshev nodes of [-1/2, 1/2] (relative error below 4e-6, and of either sign),
-// 2^n by adding to the exponent.  Arguments below -127 (masked slots) give less than 2^-126.
-__device__ inline uint64_t ex2_poly(uint64_t x) {
-    const float x0 = fmaxf(lo(x), -127.0f), x1 = fmaxf(hi(x), -127.0f);
-    const uint64_t y = f2(x0, x1);
-    const float big = 12582912.0f;  // 1.5 * 2^23: the sum's last bits are the nearest integer
-    const uint64_t t = add2(y, f2(big, big));
-    const uint64_t n = add2(t, f2(-big, -big));
-    const uint64_t f = fma2(n, f2(-1.0f, -1.0f), y);
-    uint64_t p = f2(P4, P4);
-    p = fma2(p, f, f2(P3, P3));
-    p = fma2(p, f, f2(P2, P2));
-    p = fma2(p, f, f2(P1, P1));
-    p = fma2(p, f, f2(P0, P0));
-    return f2(__int_as_float(__float_as_int(lo(p)) + (__float_as_int(lo(t)) << 23)), __int_as_float(__float_as_int(hi(p)) + (__float_as_int(hi(t)) << 23)));
-}
-
 __device__ inline uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 __device__ inline bool elect_one() {
     uint32_t p;
@@ -352,6 +335,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 
     if (u0 < u1) {
         if (warp >= 8) {
+          asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
           Line c = seek(v, tpt, pre, u0);
           if (warp == 9) {
             // ---------------------------------------------------------------- TMA
@@ -466,7 +450,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < 4; k++)
-                                umma_ts(t_o, t_s + 64 + k * 8, vd + (unsigned long long)(k + 4) * (2048 >> 4), idesc_o, k == 0 ? t >= ahead : 1);
+                                umma_ts(t_o, t_s + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, k == 0 ? t >= ahead : 1);
                         }
                         __syncwarp();
                         if (!wait(p_ready(x, 1), n_p)) return;
@@ -474,7 +458,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         if (elect_one()) {
 #pragma unroll
                             for (int k = 0; k < 4; k++)
-                                umma_ts(t_o, t_s + 96 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, 1);
+                                umma_ts(t_o, t_s + 32 + k * 8, vd + (unsigned long long)(k + 4) * (2048 >> 4), idesc_o, 1);
                             umma_commit(empty(s));
                             if (t + ahead >= n) umma_commit(o_done(x));
                         }
@@ -499,6 +483,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
           }
         } else {
             // ---------------------------------------------------------------- softmax of stream x
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
             Line c = seek(v, tpt, pre, u0);
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
@@ -563,37 +548,28 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     n_s++;
                     // this stream's last product with its queries is done: fetch the next ones under the softmax
                     const bool fetched = t + step >= n && fetch_next();
-                    // Scores of slots 0..63 are read for the maximum and again for their exponentials; those of slots
-                    // 64..127 stay in registers, and the weights are written over their columns.
-                    const bool masked = j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window);
-                    uint32_t bits[4];  // with masked: one bit per slot of the tile that the row sees
-                    if (masked) {
+                    uint32_t sr[2][64];
+                    tmem_ld64(t_s, sr[0]);
+                    tmem_ld64(t_s + 64, sr[1]);
+                    if (j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window)) {
+                        // one bit per slot of the tile; no branch per element
                         const int hi = my_p - j0 + 1, lo = v.window ? my_p - v.window + 1 - j0 : 0, sk = v.sinks - j0;
 #pragma unroll
-                        for (int w = 0; w < 4; w++)
-                            bits[w] = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
-                    }
-                    uint32_t sr[64];
-                    auto hide = [&](uint32_t b0, uint32_t b1) {
+                        for (int w = 0; w < 4; w++) {
+                            const uint32_t bits = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
 #pragma unroll
-                        for (int i = 0; i < 32; i++) {
-                            sr[i] = b0 & (1u << i) ? sr[i] : 0xff800000u;
-                            sr[32 + i] = b1 & (1u << i) ? sr[32 + i] : 0xff800000u;
+                            for (int i = 0; i < 32; i++) {
+                                uint32_t &s = sr[w >> 1][(w & 1) * 32 + i];
+                                s = bits & (1u << i) ? s : 0xff800000u;
+                            }
                         }
-                    };
+                    }
                     float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    auto raise_max = [&]() {
 #pragma unroll
-                        for (int i = 0; i < 64; i += 8)
+                    for (int i = 0; i < 128; i += 8)
 #pragma unroll
-                            for (int j = 0; j < 4; j++) mx4[j] = max3(mx4[j], __uint_as_float(sr[i + j]), __uint_as_float(sr[i + 4 + j]));
-                    };
-                    tmem_ld64(t_s, sr);
-                    if (masked) hide(bits[0], bits[1]);
-                    raise_max();
-                    tmem_ld64(t_s + 64, sr);
-                    if (masked) hide(bits[2], bits[3]);
-                    raise_max();
+                        for (int j = 0; j < 4; j++)
+                            mx4[j] = max3(mx4[j], __uint_as_float(sr[i >> 6][(i & 63) + j]), __uint_as_float(sr[i >> 6][(i & 63) + 4 + j]));
                     float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
                     mx *= scale;
                     const bool raise = mx > m + 8.0f;
@@ -630,19 +606,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     uint64_t sum2[2] = {0, 0};
 #pragma unroll
                     for (int hf = 0; hf < 2; hf++) {
-                        if (hf == 1) {
-                            tmem_ld64(t_s, sr);
-                            if (masked) hide(bits[0], bits[1]);
-                        }
                         uint32_t pw[32];
 #pragma unroll
                         for (int i = 0; i < 32; i++) {
-                            const uint64_t y = fma2(f2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, ref2);
-                            const uint64_t e = i % 4 == POLY_AT ? ex2_poly(y) : f2(ex2(lo(y)), ex2(hi(y)));
+                            const uint64_t y = fma2(f2(__uint_as_float(sr[hf][2 * i]), __uint_as_float(sr[hf][2 * i + 1])), scale2, ref2);
+                            const uint64_t e = f2(ex2(lo(y)), ex2(hi(y)));
                             sum2[i & 1] = add2(sum2[i & 1], e);
                             pw[i] = pack2(lo(e), hi(e));
                         }
-                        tmem_st32(t_s + 64 + hf * 32, pw);
+                        tmem_st32(t_s + hf * 32, pw);
                         if (hf == 1 && !shared_rows && (x == 0 || t + 1 < n)) bar_arrive(3 - x, 256);  // (every arrival is waited for)
                         tmem_st_wait();
                         tc_fence_before();
@@ -654,7 +626,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
                 if (first && fetch_next()) queries_ready();  // (no tile in this segment, and no queries were fetched for it)
                 // ---- the segment is done: store, or leave a partial result
-                if (m == -INFINITY) l = 0.0f;  // (the polynomial leaves a trace for masked slots)
                 const bool any = !first;
                 if (any) {
                     wait(o_done(x), n_o);
