@@ -316,7 +316,7 @@ aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *l
     h->last_launches = 1;
     if (h->tensor) {
         h->last_path = "mma";
-        return done(kv::launch_weigh_mma(a, (cudaStream_t)cuda_stream));
+        return done(kv::launch_weigh_mma(a, h->num_sms, (cudaStream_t)cuda_stream));
     }
     h->last_path = "simt";
     return done(kv::launch_weigh_simt(a, h->dtype == AJ_BF16, (cudaStream_t)cuda_stream));

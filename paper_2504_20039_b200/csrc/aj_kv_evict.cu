@@ -17,15 +17,14 @@ namespace kv {
 
 namespace {
 
-constexpr int THREADS = 1024, NWARP = THREADS / 32;
-constexpr int LIST = 4096;             // moves a CTA lists at a time
+constexpr int LIST_MAX = 4096;         // moves a CTA lists at a time
 constexpr int KEYS_MAX = 40 * 1024;    // slots whose keys fit in shared memory; longer ones re-read the weights
 constexpr int BINS = 2048;             // digits of 11, 11 and 10 bits: the first one is a float's sign, exponent and two
                                        // bits of its fraction, so that weights of one magnitude do not queue up at one counter
 
 struct Shared {
     unsigned hist[BINS];
-    unsigned scan[NWARP + 1], scan2[NWARP + 1];
+    unsigned scan[33], scan2[33];
     int newest, need;
     unsigned prefix;
 };
@@ -37,24 +36,26 @@ __device__ inline unsigned warp_sum(unsigned x) {
 }
 
 // Exclusive prefix over the warps of one value per warp; scan[NWARP] gets the total.
-__device__ inline void scan_warps(unsigned *scan, unsigned mine) {
+template <int NWARP> __device__ inline void scan_warps(unsigned *scan, unsigned mine) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) scan[warp] = mine;
     __syncthreads();
     if (warp == 0) {
-        unsigned x = scan[lane], y = x;
+        unsigned x = lane < NWARP ? scan[lane] : 0u, y = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const unsigned z = __shfl_up_sync(~0u, y, o);
             if (lane >= o) y += z;
         }
-        scan[lane] = y - x;
+        if (lane < NWARP) scan[lane] = y - x;
         if (lane == 31) scan[NWARP] = y;
     }
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int LIST) {
+    constexpr int NWARP = THREADS / 32;
     extern __shared__ __align__(16) unsigned dyn[];
     __shared__ Shared sh;
     const View &v = a.v;
@@ -128,22 +129,29 @@ __global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned
             if (((k ^ prefix) & high) == 0) atomicAdd(&sh.hist[(k >> shift) & (bins - 1)], 1u);
         }
         __syncthreads();
-        // thread i holds the digits bins - 1 - 2 i and bins - 2 - 2 i, from the top
-        const int d0 = bins - 1 - 2 * (int)threadIdx.x;
-        const unsigned c0 = d0 >= 1 ? sh.hist[d0] : 0u, c1 = d0 >= 1 ? sh.hist[d0 - 1] : 0u;
-        unsigned up = c0 + c1;
+        // thread i holds the PER digits from bins - 1 - PER * i down
+        constexpr int PER = BINS / THREADS;
+        const int d0 = bins - 1 - PER * (int)threadIdx.x;
+        unsigned c[PER], mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; i++) mine += c[i] = d0 >= 0 ? sh.hist[d0 - i] : 0u;
+        unsigned up = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const unsigned z = __shfl_up_sync(~0u, up, o);
             if (lane >= o) up += z;
         }
-        scan_warps(sh.scan, __shfl_sync(~0u, up, 31));
-        const unsigned before = sh.scan[warp] + up - c0 - c1, want = (unsigned)sh.need;
+        scan_warps<NWARP>(sh.scan, __shfl_sync(~0u, up, 31));
+        unsigned before = sh.scan[warp] + up - mine;
+        const unsigned want = (unsigned)sh.need;
         __syncthreads();
-        if (before < want && want <= before + c0 + c1) {
-            const bool one = want <= before + c0;
-            sh.prefix = prefix | ((unsigned)(one ? d0 : d0 - 1) << shift);
-            sh.need = (int)(want - before - (one ? 0 : c0));
+#pragma unroll
+        for (int i = 0; i < PER; i++) {
+            if (before < want && want <= before + c[i]) {
+                sh.prefix = prefix | ((unsigned)(d0 - i) << shift);
+                sh.need = (int)(want - before);
+            }
+            before += c[i];
         }
         __syncthreads();
     }
@@ -160,7 +168,7 @@ __global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned
         if (lane == 0) kept[w] = gt;
         eq += __popc(e);
     }
-    scan_warps(sh.scan, eq);
+    scan_warps<NWARP>(sh.scan, eq);
     unsigned rank = sh.scan[warp];
     for (int w = w0; w < w1 && rank < need; w++) {
         const int j = w * 32 + lane;
@@ -186,8 +194,8 @@ __global__ void __launch_bounds__(THREADS, 1) evict_kernel(EvictArgs a, unsigned
         holes += __popc(~kept[w] & below(w));
         movers += __popc(kept[w] & ~below(w) & valid(w));
     }
-    scan_warps(sh.scan, warp_sum(holes));
-    scan_warps(sh.scan2, warp_sum(movers));
+    scan_warps<NWARP>(sh.scan, warp_sum(holes));
+    scan_warps<NWARP>(sh.scan2, warp_sum(movers));
     const int n_moves = (int)sh.scan2[NWARP];  // as many holes as movers
     const int share = (n_moves + n_split - 1) / n_split;
     const int m0 = part * share, m1 = min(n_moves, m0 + share);
@@ -269,16 +277,22 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cu
     int n_split = 1;
     while (n_split < 8 && items * n_split * 2 <= num_sms) n_split *= 2;
     const int words = (a.v.cap + 31) / 32, keys = a.v.cap < KEYS_MAX ? a.v.cap : KEYS_MAX;
+    const int most = a.v.cap / 2 + 1, list = most < LIST_MAX ? most : LIST_MAX;  // at most half of the slots move
     // the keys share what the bit map of a very long cache leaves
-    const size_t fixed = (size_t)(2 * LIST + words) * 4;
+    const size_t fixed = (size_t)(2 * list + words) * 4;
     const size_t room = 212 * 1024 - fixed;
     const int keys_cap = (size_t)keys * 4 <= room ? keys : (int)(room / 4);
     const size_t smem = fixed + (size_t)keys_cap * 4;
-    cudaError_t e = cudaFuncSetAttribute(evict_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+    // more CTAs than SMs: two CTAs of half the threads share an SM, so that one's barriers hide behind the other
+    const bool half = items * n_split > num_sms && smem <= 96 * 1024;
+    auto kernel = half ? evict_kernel<512> : evict_kernel<1024>;
+    if (smem > 32 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(items * n_split);
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(half ? 512 : 1024);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr;
@@ -287,7 +301,7 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cu
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, evict_kernel, a, counters, n_split, keys_cap);
+    return cudaLaunchKernelEx(&cfg, kernel, a, counters, n_split, keys_cap, list);
 }
 
 }  // namespace kv

@@ -16,6 +16,7 @@
 // The running maximum is only a common reference: it is raised when a score exceeds it by more than 2^8 (one
 // vote per block instead of six shuffles), and weights up to 2^8 are as exact in bf16 and f32 as weights up to 1.
 #include "aj_kv.cuh"
+#include "aj_kv_mma.cuh"
 
 namespace aj {
 namespace kv {
@@ -23,34 +24,6 @@ namespace kv {
 namespace {
 
 constexpr int BLK = 64, WARPS = 4, STAGES = 3;
-
-__device__ inline uint32_t s_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ inline void cp16(uint32_t dst, const void *src, bool on) {
-    const int n = on ? 16 : 0;  // 0: fill with zeros
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ inline void ldsm4(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ inline void ldsm4t(uint32_t (&r)[4], uint32_t addr) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ inline void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ inline uint32_t transpose8(uint32_t x) {
-    uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-    return y;
-}
-__device__ inline uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&p);
-}
 
 // The blocks of slots that the new tokens of a sequence see: n_sink blocks from 0, then those from first_blk on.
 struct Span {
@@ -68,8 +41,8 @@ __device__ inline Span span_of(const View &v, const Seq &s) {
 
 template <int D, int NT> struct Few {
     static constexpr int STAGE = 2 * BLK * D * 2;
-    static constexpr int JOIN_FLOATS = WARPS * 8 * (D + 4);
-    static constexpr int MAX_PARTS = 320;
+    static constexpr int JOIN_FLOATS = WARPS * 8 * (D / 2 + 4);  // half a row at a time: two CTAs must fit an SM
+    static constexpr int MAX_PARTS = 296;
     static constexpr int SCRATCH = (JOIN_FLOATS > MAX_PARTS * 8 ? JOIN_FLOATS : MAX_PARTS * 8) * 4;
     static constexpr int PART = 8 * NT * (D + 2);  // floats of one partial result
 };
@@ -331,16 +304,18 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                 if (d == 0 && a.lse) a.lse[row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
             };
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
+            for (int nh = 0; nh < 2 * NT; nh++) {
+                constexpr int H = D / 2;
+                const int n = nh >> 1, hf = nh & 1;
 #pragma unroll
-                for (int k = 0; k < KS; k++)
+                for (int k = 0; k < KS / 2; k++)
 #pragma unroll
                     for (int i = 0; i < 4; i++)
-                        scratch[(warp * 8 + (lane & 3) * 2 + (i & 1)) * (D + 4) + k * 16 + (lane >> 2) + (i >> 1) * 8] = o[k][n][i];
+                        scratch[(warp * 8 + (lane & 3) * 2 + (i & 1)) * (H + 4) + k * 16 + (lane >> 2) + (i >> 1) * 8] = o[hf * (KS / 2) + k][n][i];
                 __syncthreads();
                 const int rows = min(8, n_rows - n * 8);
-                for (int i = threadIdx.x; i < rows * (D / 4); i += 32 * WARPS) {
-                    const int r = i / (D / 4), d = (i - r * (D / 4)) * 4, rr = n * 8 + r;
+                for (int i = threadIdx.x; i < rows * (H / 4); i += 32 * WARPS) {
+                    const int r = i / (H / 4), dh = (i - r * (H / 4)) * 4, d = hf * H + dh, rr = n * 8 + r;
                     float mm = -INFINITY, ll = 0.0f;
                     float4 x = make_float4(0, 0, 0, 0);
 #pragma unroll
@@ -349,7 +324,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
 #pragma unroll
                     for (int w = 0; w < WARPS; w++) {
                         const float c = ex2(sm_m[w][rr] - ref);
-                        const float4 y = *reinterpret_cast<const float4 *>(scratch + (w * 8 + r) * (D + 4) + d);
+                        const float4 y = *reinterpret_cast<const float4 *>(scratch + (w * 8 + r) * (H + 4) + dh);
                         ll += c * sm_l[w][rr];
                         x.x += c * y.x;
                         x.y += c * y.y;
@@ -425,7 +400,7 @@ template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaS
 
 }  // namespace
 
-size_t few_parts_floats(int D, int num_sms) { return (size_t)(2 * num_sms < 320 ? 2 * num_sms : 320) * 2 * 16 * (D + 2); }
+size_t few_parts_floats(int D, int num_sms) { return (size_t)(2 * num_sms < 296 ? 2 * num_sms : 296) * 2 * 16 * (D + 2); }
 
 cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s) {
     const bool one = a.v.n_q * a.v.G <= 8;
