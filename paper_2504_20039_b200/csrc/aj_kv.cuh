@@ -77,6 +77,7 @@ cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap &mk, const
 size_t umma_parts_floats(int D, int num_sms);
 int umma_max_batch(int D);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);
+cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s);
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s);
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s);
 

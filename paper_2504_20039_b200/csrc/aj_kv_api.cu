@@ -155,8 +155,8 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     h->parts_floats = (size_t)(7 * sms) * kv::SIMT_ROWS * (D + 2);
     h->tensor = dtype == AJ_BF16 && (D == 64 || D == 128) && !(flags & AJ_KV_FLAG_FORCE_SIMT);
     if (h->tensor && kv::few_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::few_parts_floats(D, sms);
-    const bool many = h->tensor && (long long)max_q * G > kv::FEW_ROWS && G <= 128;  // calls for the tcgen05 kernel
-    if (many && kv::umma_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::umma_parts_floats(D, sms);
+    const bool many = h->tensor && (long long)max_q * G > kv::FEW_ROWS;  // calls for the tcgen05 kernels
+    if (many && G <= 128 && kv::umma_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::umma_parts_floats(D, sms);
     if (many) {
         void *fn = nullptr;
         cudaDriverEntryPointQueryResult found;
@@ -314,6 +314,12 @@ aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *l
     a.scale_log2 = scale * kv::LOG2E;
     a.status = h->status;
     h->last_launches = 1;
+    if (h->tensor && n_q * a.v.G > kv::FEW_ROWS) {
+        h->last_path = "umma";
+        CUtensorMap mk;
+        if (!page_map(h, &mk, k_pages, n_pages)) return AJ_ERR_CUDA;
+        return done(kv::launch_weigh_umma(a, mk, h->num_sms, (cudaStream_t)cuda_stream));
+    }
     if (h->tensor) {
         h->last_path = "mma";
         return done(kv::launch_weigh_mma(a, h->num_sms, (cudaStream_t)cuda_stream));

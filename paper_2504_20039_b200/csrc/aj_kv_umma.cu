@@ -26,6 +26,7 @@
 // O (a round trip through tensor memory) is rare; weights up to 2^8 are as exact as weights up to 1.
 // Every wait is bounded (aj_ptx.cuh); one that runs out sets the status word and the CTA leaves by the normal way out.
 #include "aj_kv.cuh"
+#include "aj_kv_tc.cuh"
 #include "aj_ptx.cuh"
 
 namespace aj {
@@ -239,45 +240,7 @@ __device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
         ::I8(r, 0), I8(r, 8), I8(r, 16), I8(r, 24), "r"(addr)
         : "memory");
 }
-// pairs of f32 in one register pair
-__device__ inline uint64_t f2(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ inline float lo(uint64_t x) {
-    return __uint_as_float((uint32_t)x);
-}
-__device__ inline float hi(uint64_t x) {
-    return __uint_as_float((uint32_t)(x >> 32));
-}
-__device__ inline uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ inline uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ inline float max3(float a, float b, float c) {
-    float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-    return r;
-}
-
-__device__ inline uint32_t bits_below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
-__device__ inline bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
-}
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ inline void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ inline void bar_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
-__device__ inline void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
-
 __device__ inline uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&p);
