@@ -73,7 +73,9 @@ constexpr int FEW_ROWS = 16;
 cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s);
 size_t few_parts_floats(int D, int num_sms);
 // many rows: at most 128 query heads per key head; bf16, head size 64 or 128; at most umma_max_batch sequences
-cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s);
+// maps: K pages, V pages, queries in boxes of one token and of eight; q_tma: 0 if the queries have no maps, 1 if only boxes
+// of one token fit a row tile, 8 if both do
+cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s);
 size_t umma_parts_floats(int D, int num_sms);
 int umma_max_batch(int D);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);

@@ -47,6 +47,7 @@ class Guard {  // the handle's device for the duration of a call
 };
 
 bool off16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+bool on128(const void *p, long long stride_bytes = 0) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)stride_bytes) & 127) == 0; }
 
 // What every call has in common.
 aj_status check_view(aj_kv h, const void *pages, int n_pages, const int32_t *table, int width, const int32_t *lens, int B,
@@ -95,6 +96,16 @@ bool page_map(aj_kv h, CUtensorMap *m, const void *pages, int n_pages) {
     const cuuint64_t strides[1] = {(cuuint64_t)h->D * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)h->page}, one[2] = {1, 1};
     return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pages), dims, strides, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A tensor map of query rows as [rows, Hq, D], boxes of 64 elements x the heads of one key head x `tokens`.
+bool query_map(aj_kv h, CUtensorMap *m, const void *q, long long stride, long long rows, int tokens) {
+    const cuuint64_t dims[3] = {(cuuint64_t)h->D, (cuuint64_t)h->Hq, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)h->D * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(h->Hq / h->Hkv), (cuuint32_t)tokens}, one[3] = {1, 1, 1};
+    return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, one,
                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -263,11 +274,12 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
         h->last_path = "few";
         return done(kv::launch_attend_few(a, h->num_sms, (cudaStream_t)cuda_stream));
     }
-    if (h->tensor && a.v.G <= 128) {
+    if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows)
         h->last_path = "umma";
         h->last_launches = 0;
-        CUtensorMap mk, mv;
-        if (!page_map(h, &mk, k_pages, n_pages) || !page_map(h, &mv, v_pages, n_pages)) return AJ_ERR_CUDA;
+        CUtensorMap maps[4] = {};
+        if (!page_map(h, &maps[0], k_pages, n_pages) || !page_map(h, &maps[1], v_pages, n_pages)) return AJ_ERR_CUDA;
+        const int q_tma = !on128(q, q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
         const int most = kv::umma_max_batch(h->D);  // a very large batch runs in slices
         for (int b0 = 0; b0 < B; b0 += most) {
             kv::AttendArgs s = a;
@@ -282,7 +294,10 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
                 s.out = (char *)out + rows * out_stride * 2;
                 if (lse) s.lse += rows * h->Hq;
             }
-            st = done(kv::launch_attend_umma(s, mk, mv, h->num_sms, (cudaStream_t)cuda_stream));
+            // the rows that exist are known on the device only; no copy goes past a sequence's own
+            if (q_tma && (!query_map(h, &maps[2], s.q, q_stride, 1 << 30, 1) || (q_tma == 8 && !query_map(h, &maps[3], s.q, q_stride, 1 << 30, 8))))
+                return AJ_ERR_CUDA;
+            st = done(kv::launch_attend_umma(s, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
             if (st != AJ_OK) return st;
             h->last_launches += 2;
         }
@@ -314,7 +329,7 @@ aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *l
     a.scale_log2 = scale * kv::LOG2E;
     a.status = h->status;
     h->last_launches = 1;
-    if (h->tensor && n_q * a.v.G > kv::FEW_ROWS) {
+    if (h->tensor && n_q * a.v.G > kv::FEW_ROWS && on128(k_pages)) {
         h->last_path = "umma";
         CUtensorMap mk;
         if (!page_map(h, &mk, k_pages, n_pages)) return AJ_ERR_CUDA;

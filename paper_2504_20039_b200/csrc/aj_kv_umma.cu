@@ -39,12 +39,14 @@ constexpr int THREADS = 384;
 // Registers: launched with 168 a thread; the two softmax warpgroups, which hold a row of 128 scores, take 200 and leave
 // 104 to the third (2 x 200 + 104 = 3 x 168).  Each branch sets its own share: before that no code is shared.
 constexpr int REGS_SOFTMAX = 200, REGS_OTHER = 104;
+// What an item costs beside its tiles (its queries, the pipeline's start, its results), in tiles.
+constexpr int CHARGE = 2;
 constexpr uint32_t B_MN_MAJOR = 1u << 16;
 
 template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
     static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BARS = 2 * STAGES + 12;
+    static constexpr int BARS = 2 * STAGES + 18;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maximum and sum of stream 1's rows
     static constexpr int PRE_AT = ML_AT + 2 * 128 * 4;
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
@@ -62,11 +64,23 @@ struct Seqs {                     // a sequence and how its new tokens are cut i
     int n, each, more;            // pieces, spread evenly
 };
 
-struct Line {                     // position in the line of tiles
-    int b, h, qt, unit;           // sequence, key head, row piece, tile within the item
+struct Line {                     // position in the line
+    int b, h, qt, unit;           // sequence, key head, row piece, tile within the item (below 0: its charge)
     Seqs q;
     Piece p;
 };
+
+// A CTA's part of an item: `line` places of the line, of which the tiles first .. first + n - 1.
+struct Part {
+    int line, first, n;
+};
+__device__ inline Part part_of(const Line &c, int left) {
+    Part p;
+    p.line = min(c.p.units - c.unit, left);
+    p.first = max(c.unit, 0);
+    p.n = max(0, c.unit + p.line - p.first);
+    return p;
+}
 
 __device__ inline Seqs pieces_of(const View &v, int b, int tpt) {
     Seqs q;
@@ -97,14 +111,14 @@ __device__ inline int build_line(const View &v, int tpt, int *pre) {
         for (int b = threadIdx.x; b < v.B; b += blockDim.x) {
             const Seqs q = pieces_of(v, b, tpt);
             int u = 0;
-            for (int i = 0; i < q.n; i++) u += piece_of(v, q, i, tpt).units;
+            for (int i = 0; i < q.n; i++) u += CHARGE + piece_of(v, q, i, tpt).units;
             pre[b + 1] = u * v.Hkv;
         }
     } else {
         for (int b = warp; b < v.B; b += blockDim.x >> 5) {
             const Seqs q = pieces_of(v, b, tpt);
             int u = 0;
-            for (int i = lane; i < q.n; i += 32) u += piece_of(v, q, i, tpt).units;
+            for (int i = lane; i < q.n; i += 32) u += CHARGE + piece_of(v, q, i, tpt).units;
 #pragma unroll
             for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
             if (lane == 0) pre[b + 1] = u * v.Hkv;
@@ -145,7 +159,7 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
     c.h = r / per_head;
     r -= c.h * per_head;
     for (int q0 = 0;; q0 += 32) {
-        const int n = q0 + lane < c.q.n ? piece_of(v, c.q, q0 + lane, tpt).units : 0;
+        const int n = q0 + lane < c.q.n ? CHARGE + piece_of(v, c.q, q0 + lane, tpt).units : 0;
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -156,7 +170,7 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
         if (r < all) {
             const int at = __ffs(__ballot_sync(~0u, r < x)) - 1;
             c.qt = q0 + at;
-            c.unit = r - __shfl_sync(~0u, x - n, at);
+            c.unit = r - __shfl_sync(~0u, x - n, at) - CHARGE;
             break;
         }
         r -= all;
@@ -167,7 +181,7 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
 
 // To the first tile of the next item.
 __device__ inline void next_item(const View &v, int tpt, const int *pre, Line &c) {
-    c.unit = 0;
+    c.unit = -CHARGE;
     if (++c.qt == c.q.n) {
         c.qt = 0;
         if (++c.h == v.Hkv) {
@@ -240,6 +254,12 @@ __device__ inline void tmem_st32(uint32_t addr, const uint32_t (&r)[32]) {
         ::I8(r, 0), I8(r, 8), I8(r, 16), I8(r, 24), "r"(addr)
         : "memory");
 }
+__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap *tmap, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ inline uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
@@ -248,7 +268,8 @@ __device__ inline uint32_t pack2(float lo, float hi) {
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
-attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, AttendArgs a, int tpt) {
+attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_q1,
+                   const __grid_constant__ CUtensorMap tmap_q8, AttendArgs a, int tpt, int g_shift, int q_tma) {
     using C = Cfg<D>;
     constexpr int NS = C::STAGES, HALVES = D / 64;
     extern __shared__ __align__(1024) uint8_t smem[];  // swizzled tiles need 1024-byte alignment
@@ -256,11 +277,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const uint32_t q_at = base, ring = base + 2 * C::TILE_BYTES, bars = ring + NS * C::TILE_BYTES;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
-    auto s_full = [&](int x) { return bars + 8u * (2 * NS + x); };
-    auto p_ready = [&](int x, int hf) { return bars + 8u * (2 * NS + 2 + 2 * hf + x); };
-    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 6 + x); };
-    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
-    auto drained = [&](int x) { return bars + 8u * (2 * NS + 10 + x); };
+    auto s_full = [&](int x, int hf) { return bars + 8u * (2 * NS + 2 * x + hf); };
+    auto p_ready = [&](int x, int hf) { return bars + 8u * (2 * NS + 4 + 2 * x + hf); };
+    auto pv_done = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
+    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 10 + x); };
+    auto drained = [&](int x) { return bars + 8u * (2 * NS + 12 + x); };
+    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 14 + x); };
+    auto q_free = [&](int x) { return bars + 8u * (2 * NS + 16 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *pre = reinterpret_cast<int *>(smem + C::PRE_AT);
@@ -273,12 +296,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             mbar_init(empty(s), 2);  // both streams
         }
         for (int x = 0; x < 2; x++) {
-            mbar_init(s_full(x), 1);
-            mbar_init(p_ready(x, 0), 128);
-            mbar_init(p_ready(x, 1), 128);
-            mbar_init(o_done(x), 1);
-            mbar_init(q_ready(x), 128);
+            for (int hf = 0; hf < 2; hf++) {
+                mbar_init(s_full(x, hf), 1);
+                mbar_init(p_ready(x, hf), 128);
+            }
+            mbar_init(pv_done(x), 1);
+            mbar_init(q_ready(x), 1);
+            mbar_init(q_free(x), 1);
             mbar_init(drained(x), 1);
+            mbar_init(o_done(x), 1);
         }
         *abort_flag = 0;
         fence_barrier_init();
@@ -308,7 +334,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             uint32_t g = 0;
             bool ok = true;
             for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
-                const int n = min(c.p.units - c.unit, u1 - u);
+                const Part pt = part_of(c, u1 - u);
+                const int n = pt.n;
+                u += pt.line;
                 for (int i = 0; ok && i < 2 * n; i++) {
                     // position i holds K of tile t, or V of tile t
                     const bool is_v = i == 2 * n - 1 || (i >= 2 && (i & 1) == 0);
@@ -316,7 +344,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     const int s = g % NS;
                     // lane i looks up the tile's i-th page; one elected lane issues all copies.  Pages past the
                     // length and pages that no row of the item sees are not fetched.
-                    const int slot0 = tile_of(c.p, c.unit + t) * TILE, slot = slot0 + (lane << v.page_shift);
+                    const int slot0 = tile_of(c.p, pt.first + t) * TILE, slot = slot0 + (lane << v.page_shift);
                     const bool on = lane < per_tile && slot < c.q.s.L && (slot + v.page > c.p.first || slot < v.sinks);
                     const int row = on ? (page_of(v, c.b, slot) * v.Hkv + c.h) << v.page_shift : 0;
                     const unsigned which = __ballot_sync(~0u, on);
@@ -345,7 +373,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     __syncwarp();
                     g++;
                 }
-                u += n;
             }
             // Before the CTA may leave, every copy has landed (after a time-out too) and every stage has been released:
             // a commit that is still on its way must not arrive in shared memory that belongs to the next CTA.
@@ -357,11 +384,65 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     ok = false;
                 }
             }
+          } else if (warp == 11) {
+            // ---------------------------------------------------------------- queries
+            // A stream's queries of an item into the swizzled K-major layout (row = token x query heads + head), by TMA in
+            // boxes of eight tokens and of one, or with 16-byte copies if their rows do not lie on 128 bytes (that takes one warp some
+            // 10,000 cycles per item where TMA takes 1,500).  Rows past its tokens keep what they held: no other row
+            // depends on them.  The next item's come in while the softmax and the last product of this one run.
+            uint32_t n_q[2] = {0, 0};
+            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
+                const Part pt = part_of(c, u1 - u);
+                u += pt.line;
+                for (int x = 0; x < 2 && pt.n > 0; x++) {
+                    if (!has_tile(c.p, x, pt.n)) continue;
+                    if (!__all_sync(~0u, mbar_wait(q_free(x), (n_q[x]++ & 1u) ^ 1u, abort_flag))) {
+                        give_up();
+                        u = u1;
+                        break;
+                    }
+                    if (q_tma) {
+                        const bool lead = x == 0 || c.p.tok0 == c.p.n_tok;
+                        const int tok = lead ? c.p.tok0 : c.p.n_tok - c.p.tok0, r0 = c.q.s.row0 + c.p.ta + (lead ? 0 : c.p.tok0);
+                        if (elect_one()) {
+                            mbar_expect_tx(q_ready(x), (uint32_t)(tok * v.G) * 128u * HALVES);
+                            for (int t = 0; t < tok;) {
+                                const bool eight = q_tma == 8 && t + 8 <= tok;
+#pragma unroll
+                                for (int hf = 0; hf < HALVES; hf++)
+                                    tma_load_3d(q_at + x * C::TILE_BYTES + hf * 16384 + (uint32_t)(t * v.G) * 128u, eight ? &tmap_q8 : &tmap_q1, hf * 64, c.h * v.G, r0 + t, q_ready(x));
+                                t += eight ? 8 : 1;
+                            }
+                        }
+                        __syncwarp();
+                        continue;
+                    }
+                    constexpr int CPR = D / 8;
+                    const bool lead = x == 0 || c.p.tok0 == c.p.n_tok;
+                    const int n_rows = (lead ? c.p.tok0 : c.p.n_tok - c.p.tok0) * v.G;
+                    const __nv_bfloat16 *qp = (const __nv_bfloat16 *)a.q + ((size_t)c.q.s.row0 + c.p.ta + (lead ? 0 : c.p.tok0)) * a.q_stride + (size_t)c.h * v.G * D;
+#pragma unroll 4
+                    for (int i = lane; i < 128 * CPR; i += 32) {
+                        const int r = i / CPR, cc = i % CPR, t = g_shift >= 0 ? r >> g_shift : r / v.G;
+                        const uint32_t dst = q_at + x * C::TILE_BYTES + (cc >> 3) * 16384 + r * 128 + (((cc & 7) ^ (r & 7)) << 4);
+                        const int bytes = r < n_rows ? 16 : 0;
+                        const void *src = r < n_rows ? (const void *)(qp + (size_t)t * a.q_stride + (size_t)(r - t * v.G) * D + cc * 8) : a.q;
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+                    }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    fence_async_shared();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(q_ready(x));
+                }
+            }
+            int never = 0;  // every copy has landed before the CTA may leave
+            for (int x = 0; x < 2; x++)
+                if (n_q[x] > 0 && !*abort_flag) mbar_wait(q_ready(x), (n_q[x] - 1) & 1u, &never);
           } else if (warp <= 10) {
             // ---------------------------------------------------------------- MMA: warp 8 stream 0, warp 10 stream 1
             // The whole warp walks the loop and waits, one elected lane issues.
             const int x = warp == 8 ? 0 : 1;
-            constexpr uint32_t idesc_s = instr_desc(128, 128), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
+            constexpr uint32_t idesc_s = instr_desc(128, 64), idesc_o = instr_desc(128, D) | B_MN_MAJOR;
             const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * D;
             const unsigned long long qd = smem_desc_sw128(q_at + x * C::TILE_BYTES);
             uint32_t g = 0, n_p = 0, n_q = 0;
@@ -377,66 +458,81 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
             // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
             for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
-                const int n = min(c.p.units - c.unit, u1 - u);
+                const Part pt = part_of(c, u1 - u);
+                const int n = pt.n;
+                u += pt.line;
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
                 const int ahead = shared_rows ? 2 : 1;  // K tiles in front of V tiles
                 auto mine = [&](int t) { return !shared_rows || (t & 1) == x; };
                 bool begun = false;
-                auto k_tile = [&](int t) {
-                    const uint32_t at = g + pos_k(t), s = at % NS;
-                    if (!wait(full(s), at / NS)) return;
-                    if (mine(t)) {
-                        if (!begun) {
-                            if (!wait(q_ready(x), n_q)) return;
-                            n_q++;
-                        }
-                        begun = true;
-                        const unsigned long long kd = smem_desc_sw128(ring + s * C::TILE_BYTES);
-                        if (elect_one()) {
+                // QK^T of one half of tile t, into the columns of that half
+                auto qk = [&](int t, int hf) {
+                    const uint32_t s = (g + pos_k(t)) % NS;
+                    if (!begun) {
+                        if (!wait(q_ready(x), n_q)) return;
+                        n_q++;
+                    }
+                    begun = true;
+                    const unsigned long long kd = smem_desc_sw128(ring + s * C::TILE_BYTES + hf * 8192);
+                    if (elect_one()) {
 #pragma unroll
-                            for (int k = 0; k < D / 16; k++)
-                                umma_bf16(t_s, qd + (k / 4) * (16384 >> 4) + 2 * (k % 4), kd + (k / 4) * (16384 >> 4) + 2 * (k % 4), idesc_s, k != 0);
-                            umma_commit(s_full(x));
-                            umma_commit(empty(s));
-                        }
-                    } else if (elect_one()) {
-                        mbar_arrive(empty(s));
+                        for (int k = 0; k < D / 16; k++)
+                            umma_bf16(t_s + hf * 64, qd + (k / 4) * (16384 >> 4) + 2 * (k % 4), kd + (k / 4) * (16384 >> 4) + 2 * (k % 4), idesc_s, k != 0);
+                        umma_commit(s_full(x, hf));
+                        if (hf == 1) umma_commit(empty(s));
+                        if (hf == 1 && t + ahead >= n) umma_commit(q_free(x));  // the stream's last product with these queries
                     }
                     __syncwarp();
                 };
-                auto v_tile = [&](int t) {
-                    const uint32_t at = g + pos_v(t, n), s = at % NS;
-                    if (!wait(full(s), at / NS)) return;
-                    if (mine(t)) {
-                        const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES);
-                        if (!wait(p_ready(x, 0), n_p)) return;
-                        if (elect_one()) {
+                auto pv = [&](int t, int hf) {
+                    const uint32_t s = (g + pos_v(t, n)) % NS;
+                    const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES + hf * 8192);
+                    if (!wait(p_ready(x, hf), n_p)) return;
+                    if (elect_one()) {
 #pragma unroll
-                            for (int k = 0; k < 4; k++)
-                                umma_ts(t_o, t_s + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, k == 0 ? t >= ahead : 1);
-                        }
-                        __syncwarp();
-                        if (!wait(p_ready(x, 1), n_p)) return;
-                        n_p++;
-                        if (elect_one()) {
-#pragma unroll
-                            for (int k = 0; k < 4; k++)
-                                umma_ts(t_o, t_s + 32 + k * 8, vd + (unsigned long long)(k + 4) * (2048 >> 4), idesc_o, 1);
-                            umma_commit(empty(s));
-                            if (t + ahead >= n) umma_commit(o_done(x));
-                        }
-                    } else if (elect_one()) {
-                        mbar_arrive(empty(s));
+                        for (int k = 0; k < 4; k++)
+                            umma_ts(t_o, t_s + hf * 64 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, hf == 0 && k == 0 ? t >= ahead : 1);
+                        umma_commit(pv_done(x));
+                        if (hf == 1) umma_commit(empty(s));
+                        if (hf == 1 && t + ahead >= n) umma_commit(o_done(x));
                     }
                     __syncwarp();
                 };
-                for (int t = 0; ok && t < ahead && t < n; t++) k_tile(t);
+                auto arrived = [&](uint32_t at) { return wait(full(at % NS), at / NS); };
+                auto release = [&](uint32_t at) {
+                    if (elect_one()) mbar_arrive(empty(at % NS));
+                    __syncwarp();
+                };
+                for (int t = 0; ok && t < ahead && t < n; t++) {
+                    if (!arrived(g + pos_k(t))) break;
+                    if (mine(t)) {
+                        qk(t, 0);
+                        qk(t, 1);
+                    } else {
+                        release(g + pos_k(t));
+                    }
+                }
                 for (int t = 0; ok && t < n; t++) {
-                    v_tile(t);
-                    if (ok && t + ahead < n) k_tile(t + ahead);
+                    const bool more = t + ahead < n;
+                    if (!arrived(g + pos_v(t, n))) break;
+                    if (mine(t)) {
+                        pv(t, 0);
+                        if (more) {
+                            if (!ok || !arrived(g + pos_k(t + ahead))) break;
+                            qk(t + ahead, 0);
+                        }
+                        if (ok) pv(t, 1);
+                        if (ok && more) qk(t + ahead, 1);
+                        n_p++;
+                    } else {
+                        release(g + pos_v(t, n));
+                        if (more) {
+                            if (!arrived(g + pos_k(t + ahead))) break;
+                            release(g + pos_k(t + ahead));
+                        }
+                    }
                 }
                 g += 2 * n;
-                u += n;
             }
             // nothing that this warp issued is in flight when the CTA leaves, after a time-out either
             int never = 0;
@@ -451,154 +547,112 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
             const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * D + lanes;
-            uint32_t n_s = 0, n_o = 0, g = 0;
+            uint32_t n_h = 0, n_o = 0, g = 0;  // halves of tiles and segments with a tile so far; places in the ring
             bool dead = false;
             auto wait = [&](uint32_t bar, uint32_t parity) {
-                if (!dead && !__all_sync(~0u, mbar_wait(bar, parity & 1u, abort_flag))) {
+                if (!dead && !mbar_wait(bar, parity & 1u, abort_flag)) {
                     give_up();
                     dead = true;  // go through the motions, so that the barriers below stay matched
                 }
+                __syncwarp();
                 tc_fence_after();
             };
             const float scale = a.scale_log2;
-            // A stream's queries into the swizzled K-major layout, asynchronously; rows past its tokens get zeros.
-            auto fetch_queries = [&](const Line &c) {
-                constexpr int CPR = D / 8;
-                const bool lead = x == 0 || c.p.tok0 == c.p.n_tok;
-                const int n_rows = (lead ? c.p.tok0 : c.p.n_tok - c.p.tok0) * v.G;
-                const __nv_bfloat16 *qp = (const __nv_bfloat16 *)a.q + ((size_t)c.q.s.row0 + c.p.ta + (lead ? 0 : c.p.tok0)) * a.q_stride + (size_t)c.h * v.G * D;
-#pragma unroll 4
-                for (int i = 0; i < CPR; i++) {
-                    const int r = i * (128 / CPR) + row / CPR, cc = row % CPR, t = r / v.G;
-                    const uint32_t dst = q_at + x * C::TILE_BYTES + (cc >> 3) * 16384 + r * 128 + (((cc & 7) ^ (r & 7)) << 4);
-                    const int bytes = r < n_rows ? 16 : 0;
-                    const void *src = r < n_rows ? (const void *)(qp + (size_t)t * a.q_stride + (size_t)(r - t * v.G) * D + cc * 8) : a.q;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-                }
-            };
-            auto queries_ready = [&]() {
-                asm volatile("cp.async.wait_all;" ::: "memory");
-                fence_async_shared();
-                mbar_arrive(q_ready(x));
-            };
-            if (has_tile(c.p, x, min(c.p.units - c.unit, u1 - u0))) {
-                fetch_queries(c);
-                queries_ready();
-            }
+            const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31) == 0;  // rows on 32 bytes
+            auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
             for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
-                const int n = min(c.p.units - c.unit, u1 - u);
+                const Part pt = part_of(c, u1 - u);
+                const int n = pt.n;
+                u += pt.line;
+                if (n == 0) continue;
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
                 const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
                 const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
                 const int n_rows = tok * v.G;
-                if (!shared_rows && x == 1) bar_arrive(2, 256);  // stream 0 goes first
-                auto fetch_next = [&]() {  // the next item's queries, if this stream has a tile of it
-                    if (u + n >= u1) return false;
-                    Line nx = c;
-                    next_item(v, tpt, pre, nx);
-                    if (!has_tile(nx.p, x, min(nx.p.units, u1 - u - n))) return false;
-                    fetch_queries(nx);
-                    return true;
-                };
                 const int p_first = c.q.s.L - c.q.s.nq + ta;           // slot of the stream's first token
-                const int my_p = p_first + min(row, n_rows - 1) / v.G, p_last = p_first + tok - 1;
+                const int my_p = p_first + token(min(row, n_rows - 1)), p_last = p_first + tok - 1;
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
                 bool first = true;
-                for (int t = shared_rows ? x : 0; t < n; t += step, first = false) {
-                    const int j0 = tile_of(c.p, c.unit + t) * TILE;
-                    wait(s_full(x), n_s);
-                    n_s++;
-                    // this stream's last product with its queries is done: fetch the next ones under the softmax
-                    const bool fetched = t + step >= n && fetch_next();
-                    uint32_t sr[2][64];
-                    tmem_ld64(t_s, sr[0]);
-                    tmem_ld64(t_s + 64, sr[1]);
-                    if (j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window)) {
-                        // one bit per slot of the tile; no branch per element
-                        const int hi = my_p - j0 + 1, lo = v.window ? my_p - v.window + 1 - j0 : 0, sk = v.sinks - j0;
+                for (int t = shared_rows ? x : 0; t < n; t += step) {
+                    const int j0 = tile_of(c.p, pt.first + t) * TILE;
+                    const bool masked = j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window);
+#pragma unroll 1
+                    for (int hf = 0; hf < 2; hf++, n_h++) {
+                        wait(s_full(x, hf), n_h >> 1);
+                        uint32_t sr[64];
+                        tmem_ld64(t_s + hf * 64, sr);
+                        if (masked) {
+                            // one bit per slot; no branch per element
+                            const int jh = j0 + hf * 64, hi = my_p - jh + 1, lo = v.window ? my_p - v.window + 1 - jh : 0, sk = v.sinks - jh;
 #pragma unroll
-                        for (int w = 0; w < 4; w++) {
-                            const uint32_t bits = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
+                            for (int w = 0; w < 2; w++) {
+                                const uint32_t bits = bits_below(hi - 32 * w) & (~bits_below(lo - 32 * w) | bits_below(sk - 32 * w));
 #pragma unroll
-                            for (int i = 0; i < 32; i++) {
-                                uint32_t &s = sr[w >> 1][(w & 1) * 32 + i];
-                                s = bits & (1u << i) ? s : 0xff800000u;
+                                for (int i = 0; i < 32; i++) sr[w * 32 + i] = bits & (1u << i) ? sr[w * 32 + i] : 0xff800000u;
                             }
                         }
-                    }
-                    float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 128; i += 8)
+                        for (int i = 0; i < 64; i += 8)
 #pragma unroll
-                        for (int j = 0; j < 4; j++)
-                            mx4[j] = max3(mx4[j], __uint_as_float(sr[i >> 6][(i & 63) + j]), __uint_as_float(sr[i >> 6][(i & 63) + 4 + j]));
-                    float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]);
-                    mx *= scale;
-                    const bool raise = mx > m + 8.0f;
-                    if (first) {
-                        m = mx;
-                    } else if (__any_sync(~0u, raise)) {
-                        // all of this stream's products so far are done (the commit behind S followed them)
-                        const float c2 = raise ? ex2(m - mx) : 1.0f;
-                        if (raise) m = mx;
-                        l *= c2;
+                            for (int j = 0; j < 4; j++) mx4[j] = max3(mx4[j], __uint_as_float(sr[i + j]), __uint_as_float(sr[i + 4 + j]));
+                        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
+                        const bool raise = mx > m + 8.0f;
+                        if (first) {
+                            m = mx;
+                            first = false;
+                        } else if (__any_sync(~0u, raise)) {
+                            // every product into O so far: the last but one is done (this half's scores followed it), so
+                            // the one-bit phase is unambiguous
+                            wait(pv_done(x), n_h - 1);
+                            const float c2 = raise ? ex2(m - mx) : 1.0f;
+                            if (raise) m = mx;
+                            l *= c2;
 #pragma unroll 1
-                        for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
-                    }
-                    // slots that nobody sees may hold anything: their values are cleared before the product
-                    if (c.q.s.L - j0 < TILE || (j0 < c.p.first && c.p.first > v.sinks)) {
-                        const uint32_t at = g + pos_v(t, n), s = at % NS;
-                        wait(full(s), at / NS);
-                        const int j = j0 + row;
-                        if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
-#pragma unroll
-                            for (int hh = 0; hh < HALVES; hh++)
-#pragma unroll
-                                for (int i = 0; i < 8; i++)
-                                    *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + hh * 16384 + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+                            for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
                         }
-                        fence_async_shared();
-                        __syncwarp();
-                    }
-                    // Streams of one piece take turns with the exponentials: left alone they fall into step, and then both
-                    // wait for the tensor pipe and both queue at the exponential unit.
-                    if (!shared_rows) bar_sync(2 + x, 256);
-                    const float ref = m == -INFINITY ? 0.0f : m;
-                    const uint64_t scale2 = f2(scale, scale), ref2 = f2(-ref, -ref);
-                    uint64_t sum2[2] = {0, 0};
+                        // slots that nobody sees may hold anything: their values are cleared before the product
+                        if (hf == 0 && (c.q.s.L - j0 < TILE || (j0 < c.p.first && c.p.first > v.sinks))) {
+                            const uint32_t at = g + pos_v(t, n), s = at % NS;
+                            wait(full(s), at / NS);
+                            const int j = j0 + row;
+                            if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
 #pragma unroll
-                    for (int hf = 0; hf < 2; hf++) {
+                                for (int hh = 0; hh < HALVES; hh++)
+#pragma unroll
+                                    for (int i = 0; i < 8; i++)
+                                        *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + hh * 16384 + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+                            }
+                            fence_async_shared();
+                            __syncwarp();
+                        }
+                        const float ref = m == -INFINITY ? 0.0f : m;
+                        const uint64_t scale2 = f2(scale, scale), ref2 = f2(-ref, -ref);
+                        uint64_t sum2[2] = {0, 0};
                         uint32_t pw[32];
 #pragma unroll
                         for (int i = 0; i < 32; i++) {
-                            const uint64_t y = fma2(f2(__uint_as_float(sr[hf][2 * i]), __uint_as_float(sr[hf][2 * i + 1])), scale2, ref2);
+                            const uint64_t y = fma2(f2(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, ref2);
                             const uint64_t e = f2(ex2(lo(y)), ex2(hi(y)));
                             sum2[i & 1] = add2(sum2[i & 1], e);
                             pw[i] = pack2(lo(e), hi(e));
                         }
-                        tmem_st32(t_s + hf * 32, pw);
-                        if (hf == 1 && !shared_rows && (x == 0 || t + 1 < n)) bar_arrive(3 - x, 256);  // (every arrival is waited for)
+                        tmem_st32(t_s + hf * 64, pw);
+                        const uint64_t sum = add2(sum2[0], sum2[1]);
+                        l += lo(sum) + hi(sum);
                         tmem_st_wait();
                         tc_fence_before();
                         mbar_arrive(p_ready(x, hf));
                     }
-                    const uint64_t sum = add2(sum2[0], sum2[1]);
-                    l += lo(sum) + hi(sum);
-                    if (fetched) queries_ready();
                 }
-                if (first && fetch_next()) queries_ready();  // (no tile in this segment, and no queries were fetched for it)
                 // ---- the segment is done: store, or leave a partial result
-                const bool any = !first;
-                if (any) {
-                    wait(o_done(x), n_o);
-                    n_o++;
-                }
-                const bool whole = c.unit == 0 && n == c.p.units;
-                float4 *part = reinterpret_cast<float4 *>(a.parts + ((size_t)blockIdx.x * 2 + (c.unit == 0 ? 1 : 0)) * C::PART);
-                const int t_row = row / v.G;
+                if (!first) wait(o_done(x), n_o++);  // (first: no tile in this segment)
+                const bool whole = n == c.p.units;
+                float4 *part = reinterpret_cast<float4 *>(a.parts + ((size_t)blockIdx.x * 2 + (pt.first == 0 ? 1 : 0)) * C::PART);
+                const int t_row = token(row);
                 const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
-                const int head = c.h * v.G + row % v.G;
+                const int head = c.h * v.G + row - t_row * v.G;
                 const bool both = shared_rows && n > 1;  // two streams of the same rows: stream 0 joins and stores
                 const uint32_t t_o1 = tmem + 256 + D + lanes;
                 float w0 = 1.0f, w1 = 0.0f;
@@ -623,8 +677,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
                 if (!shared_rows || x == 0) {
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-                    for (int k = 0; k < D / 32; k++) {
+                    __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
+#pragma unroll 1
+                    for (int k = 0; k < D / 32; k++) {  // not unrolled: code that runs once per item mostly costs its way into the cache
                         float ov[32];
                         __syncwarp();  // (the stores below leave lanes without a row behind)
                         tmem_ld32(t_o + k * 32, ov);
@@ -636,11 +691,17 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         }
                         if (row < n_rows) {
                             if (whole) {
-                                uint4 *o = reinterpret_cast<uint4 *>((__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D + k * 32);
+                                uint32_t w[16];
 #pragma unroll
-                                for (int i = 0; i < 4; i++)
-                                    o[i] = make_uint4(pack2(ov[8 * i] * inv, ov[8 * i + 1] * inv), pack2(ov[8 * i + 2] * inv, ov[8 * i + 3] * inv),
-                                                      pack2(ov[8 * i + 4] * inv, ov[8 * i + 5] * inv), pack2(ov[8 * i + 6] * inv, ov[8 * i + 7] * inv));
+                                for (int i = 0; i < 16; i++) w[i] = pack2(ov[2 * i] * inv, ov[2 * i + 1] * inv);
+                                if (wide_out) {
+#pragma unroll
+                                    for (int i = 0; i < 16; i += 8)
+                                        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o + k * 32 + 2 * i), I8(w, i) : "memory");
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(o + k * 32 + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                                }
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 8; i++)
@@ -662,7 +723,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 tc_fence_before();
                 if (both) bar_sync(1, 256);  // stream 1's tensor memory is read
                 g += 2 * n;
-                u += n;
             }
         }
     }
@@ -686,8 +746,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (u0 >= u1 || u1 >= total) return;
     const Line c = seek(v, tpt, pre, u1 - 1);
-    const int i0 = u1 - 1 - c.unit, i1 = i0 + c.p.units;
-    if (i0 < u0 || i1 <= u1) return;  // begins in an earlier CTA, or ends in this one
+    const int i0 = u1 - 1 - c.unit, i1 = i0 + c.p.units;  // the item's tiles on the line
+    if (c.unit < 0 || i0 < u0 || i1 <= u1) return;  // only its charge is here, or it begins in an earlier CTA, or ends here
     const int n_parts = (i1 - 1) / per - (int)blockIdx.x + 1;
     const int r = blockIdx.y * 32 + (threadIdx.x & 31), x = r >> 7, row = r & 127;
     const bool shared_rows = c.p.tok0 == c.p.n_tok;
@@ -724,14 +784,17 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_
     if (threadIdx.x < 32 && a.lse) a.lse[out_row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
 }
 
-template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s) {
+template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
     using C = Cfg<D>;
     const int tpt = 128 / a.v.G;
     const int smem = C::smem(a.v.B);
     auto kernel = attend_umma_kernel<D>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<num_sms, THREADS, smem, s>>>(mk, mv, a, tpt);
+    int g_shift = -1;  // log2 of the query heads per key head, if it is a power of two
+    for (int i = 0; i < 8; i++)
+        if (a.v.G == 1 << i) g_shift = i;
+    kernel<<<num_sms, THREADS, smem, s>>>(maps[0], maps[1], maps[2], maps[3], a, tpt, g_shift, q_tma);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(num_sms, 8);
@@ -751,8 +814,8 @@ template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap &mk, co
 int umma_max_batch(int D) { return (232448 - (D == 64 ? Cfg<64>::smem(0) : Cfg<128>::smem(0))) / 4 - 1; }
 size_t umma_parts_floats(int D, int num_sms) { return (size_t)num_sms * 2 * 256 * (D + 2); }
 
-cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap &mk, const CUtensorMap &mv, int num_sms, cudaStream_t s) {
-    return a.v.D == 64 ? umma<64>(a, mk, mv, num_sms, s) : umma<128>(a, mk, mv, num_sms, s);
+cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
+    return a.v.D == 64 ? umma<64>(a, maps, q_tma, num_sms, s) : umma<128>(a, maps, q_tma, num_sms, s);
 }
 
 }  // namespace kv
