@@ -72,22 +72,36 @@ cudaError_t launch_attend_simt(const AttendArgs &a, bool bf16, int num_sms, cuda
 constexpr int FEW_ROWS = 16;
 cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s);
 size_t few_parts_floats(int D, int num_sms);
-// many rows: at most 128 query heads per key head; bf16, head size 64 or 128; at most umma_max_batch sequences
+// many rows: at most 128 query heads per key head; bf16, head size 64 or 128
 // maps: K pages, V pages, queries in boxes of one token and of eight; q_tma: 0 if the queries have no maps, 1 if only boxes
 // of one token fit a row tile, 8 if both do
 cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s);
 size_t umma_parts_floats(int D, int num_sms);
-int umma_max_batch(int D);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);
 cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s);
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s);
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s);
+
+// Once per device, before the first launch: more than 48 KB of shared memory per CTA.
+cudaError_t prepare_attend_few();
+cudaError_t prepare_attend_umma();
+cudaError_t prepare_weigh_mma();
+cudaError_t prepare_weigh_umma();
+cudaError_t prepare_evict();
 
 // Sizes of the split-attention workspace that the CUDA-core kernels can use for this handle.
 constexpr int SIMT_MAX_SPLITS = 64;
 constexpr int SIMT_ROWS = 8;  // query rows a CTA of the CUDA-core kernels handles at once
 
 #ifdef __CUDACC__
+
+// A kernel may use all of the shared memory that its own static share leaves.
+template <typename K> cudaError_t allow_shared(K kernel) {
+    cudaFuncAttributes fa;
+    const cudaError_t e = cudaFuncGetAttributes(&fa, kernel);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
+}
 
 struct Seq {
     int row0, nq, L;  // first row of q, new tokens, slots in use

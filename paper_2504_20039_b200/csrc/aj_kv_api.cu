@@ -159,6 +159,12 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     for (h->page_shift = 0; (1 << h->page_shift) < page_size;) h->page_shift++;
     h->dtype = dtype;
     h->flags = flags;
+    if (kv::prepare_attend_few() != cudaSuccess || kv::prepare_attend_umma() != cudaSuccess || kv::prepare_weigh_mma() != cudaSuccess ||
+        kv::prepare_weigh_umma() != cudaSuccess || kv::prepare_evict() != cudaSuccess) {
+        cudaGetLastError();
+        delete h;
+        return AJ_ERR_CUDA;
+    }
     // CUDA-core kernels: 6 waves of pieces, or two per item if that is more, up to 64 MB
     const int G = Hq / Hkv;
     const long long items = (long long)max_B * Hkv * (((long long)max_q * G + kv::SIMT_ROWS - 1) / kv::SIMT_ROWS);
@@ -276,32 +282,13 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     }
     if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows)
         h->last_path = "umma";
-        h->last_launches = 0;
         CUtensorMap maps[4] = {};
         if (!page_map(h, &maps[0], k_pages, n_pages) || !page_map(h, &maps[1], v_pages, n_pages)) return AJ_ERR_CUDA;
         const int q_tma = !on128(q, q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
-        const int most = kv::umma_max_batch(h->D);  // a very large batch runs in slices
-        for (int b0 = 0; b0 < B; b0 += most) {
-            kv::AttendArgs s = a;
-            s.v.B = B - b0 < most ? B - b0 : most;
-            s.v.table += (size_t)b0 * table_width;
-            s.v.lens += b0;
-            if (q_start) {
-                s.v.q_start += b0;
-            } else {
-                const size_t rows = (size_t)b0 * n_q;
-                s.q = (const char *)q + rows * q_stride * 2;
-                s.out = (char *)out + rows * out_stride * 2;
-                if (lse) s.lse += rows * h->Hq;
-            }
-            // the rows that exist are known on the device only; no copy goes past a sequence's own
-            if (q_tma && (!query_map(h, &maps[2], s.q, q_stride, 1 << 30, 1) || (q_tma == 8 && !query_map(h, &maps[3], s.q, q_stride, 1 << 30, 8))))
-                return AJ_ERR_CUDA;
-            st = done(kv::launch_attend_umma(s, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
-            if (st != AJ_OK) return st;
-            h->last_launches += 2;
-        }
-        return AJ_OK;
+        // the rows that exist are known on the device only; no copy goes past a sequence's own
+        if (q_tma && (!query_map(h, &maps[2], q, q_stride, 1 << 30, 1) || (q_tma == 8 && !query_map(h, &maps[3], q, q_stride, 1 << 30, 8)))) return AJ_ERR_CUDA;
+        h->last_launches = 2;
+        return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
     }
     h->last_path = "simt";
     return done(kv::launch_attend_simt(a, h->dtype == AJ_BF16, h->num_sms, (cudaStream_t)cuda_stream));

@@ -272,6 +272,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
 
 }  // namespace
 
+cudaError_t prepare_evict() {
+    const cudaError_t e = allow_shared(evict_kernel<512>);
+    return e == cudaSuccess ? allow_shared(evict_kernel<1024>) : e;
+}
+
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s) {
     const int items = a.v.B * a.v.Hkv;
     int n_split = 1;
@@ -286,10 +291,6 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cu
     // more CTAs than SMs: two CTAs of half the threads share an SM, so that one's barriers hide behind the other
     const bool half = items * n_split > num_sms && smem <= 96 * 1024;
     auto kernel = half ? evict_kernel<512> : evict_kernel<1024>;
-    if (smem > 32 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(items * n_split);
     cfg.blockDim = dim3(half ? 512 : 1024);

@@ -392,13 +392,18 @@ template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaS
     using C = Few<D, NT>;
     const size_t smem = (size_t)STAGES * C::STAGE + C::SCRATCH + (a.v.B + 1) * 4;
     auto kernel = attend_few_kernel<D, NT>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
     kernel<<<2 * num_sms < C::MAX_PARTS ? 2 * num_sms : C::MAX_PARTS, 32 * WARPS, smem, s>>>(a);
     return cudaGetLastError();
 }
 
 }  // namespace
+
+cudaError_t prepare_attend_few() {
+    cudaError_t e = allow_shared(attend_few_kernel<64, 1>);
+    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<64, 2>);
+    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<128, 1>);
+    return e == cudaSuccess ? allow_shared(attend_few_kernel<128, 2>) : e;
+}
 
 size_t few_parts_floats(int D, int num_sms) { return (size_t)(2 * num_sms < 296 ? 2 * num_sms : 296) * 2 * 16 * (D + 2); }
 

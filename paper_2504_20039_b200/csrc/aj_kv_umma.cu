@@ -48,9 +48,9 @@ template <int D> struct Cfg {
     static constexpr int STAGES = D == 128 ? 5 : 8;
     static constexpr int BARS = 2 * STAGES + 18;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maximum and sum of stream 1's rows
-    static constexpr int PRE_AT = ML_AT + 2 * 128 * 4;
+    static constexpr int SMEM = ML_AT + 2 * 128 * 4;
+    static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 4, "the prefix sums of the largest batch fit the ring");
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
-    static constexpr int smem(int B) { return PRE_AT + (B + 1) * 4; }
 };
 
 // The tokens of a row piece and the tiles of slots that they see.
@@ -180,7 +180,7 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
 }
 
 // To the first tile of the next item.
-__device__ inline void next_item(const View &v, int tpt, const int *pre, Line &c) {
+__device__ inline void next_item(const View &v, int tpt, Line &c) {
     c.unit = -CHARGE;
     if (++c.qt == c.q.n) {
         c.qt = 0;
@@ -188,8 +188,8 @@ __device__ inline void next_item(const View &v, int tpt, const int *pre, Line &c
             c.h = 0;
             do {
                 if (++c.b >= v.B) return;
-            } while (pre[c.b] == pre[c.b + 1]);
-            c.q = pieces_of(v, c.b, tpt);
+                c.q = pieces_of(v, c.b, tpt);
+            } while (c.q.n == 0);
         }
     }
     c.p = piece_of(v, c.q, c.qt, tpt);
@@ -301,7 +301,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto q_free = [&](int x) { return bars + 8u * (2 * NS + 16 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    int *pre = reinterpret_cast<int *>(smem + C::PRE_AT);
+    int *pre = reinterpret_cast<int *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
@@ -341,6 +341,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         if (warp >= 8) {
           asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
           Line c = seek(v, tpt, pre, u0);
+          fence_async_shared();
+          __syncthreads();  // the prefix sums are read: the ring may be filled
           if (warp == 9) {
             // ---------------------------------------------------------------- TMA
             const unsigned long long pol = policy_evict_normal();
@@ -348,7 +350,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const uint32_t box_bytes = (uint32_t)v.page * 128u;
             uint32_t g = 0;
             bool ok = true;
-            for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
+            for (int u = u0; ok && u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -406,7 +408,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // 10,000 cycles per item where TMA takes 1,500).  Rows past its tokens keep what they held: no other row
             // depends on them.  The next item's come in while the softmax and the last product of this one run.
             uint32_t n_q[2] = {0, 0};
-            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
+            for (int u = u0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 u += pt.line;
                 for (int x = 0; x < 2 && pt.n > 0; x++) {
@@ -472,7 +474,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             };
             // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
             // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
-            for (int u = u0; ok && u < u1; next_item(v, tpt, pre, c)) {
+            for (int u = u0; ok && u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -558,6 +560,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // ---------------------------------------------------------------- softmax of stream x
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
             Line c = seek(v, tpt, pre, u0);
+            fence_async_shared();
+            __syncthreads();  // the prefix sums are read
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
             const uint32_t lanes = (uint32_t)(wq * 32) << 16;
             const uint32_t t_s = tmem + x * 128 + lanes, t_o = tmem + 256 + x * D + lanes;
@@ -574,7 +578,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const float scale = a.scale_log2;
             const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31) == 0;  // rows on 32 bytes
             auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
-            for (int u = u0; u < u1; next_item(v, tpt, pre, c)) {
+            for (int u = u0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -804,15 +808,13 @@ __global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_
 template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
     using C = Cfg<D>;
     const int tpt = 128 / a.v.G;
-    const int smem = C::smem(a.v.B);
     auto kernel = attend_umma_kernel<D>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
     int g_shift = -1;  // log2 of the query heads per key head, if it is a power of two
     for (int i = 0; i < 8; i++)
         if (a.v.G == 1 << i) g_shift = i;
-    kernel<<<num_sms, THREADS, smem, s>>>(maps[0], maps[1], maps[2], maps[3], a, tpt, g_shift, q_tma);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    kernel<<<num_sms, THREADS, C::SMEM, s>>>(maps[0], maps[1], maps[2], maps[3], a, tpt, g_shift, q_tma);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(num_sms, 8);
     cfg.blockDim = dim3(256);
@@ -828,8 +830,12 @@ template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)
 
 }  // namespace
 
-int umma_max_batch(int D) { return (232448 - (D == 64 ? Cfg<64>::smem(0) : Cfg<128>::smem(0))) / 4 - 1; }
 size_t umma_parts_floats(int D, int num_sms) { return (size_t)num_sms * 2 * 256 * (D + 2); }
+
+cudaError_t prepare_attend_umma() {
+    const cudaError_t e = allow_shared(attend_umma_kernel<64>);
+    return e == cudaSuccess ? allow_shared(attend_umma_kernel<128>) : e;
+}
 
 cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
     return a.v.D == 64 ? umma<64>(a, maps, q_tma, num_sms, s) : umma<128>(a, maps, q_tma, num_sms, s);

@@ -153,11 +153,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2) weigh_kernel(WeighArgs a, int g
         const Seq &s = cur.s;
         const int j0 = cur.blk * BLK + warp * WS, h = cur.h, counted = cur.counted;
         const size_t at = ((size_t)cur.b * v.Hkv + h) * v.cap + j0 + r8;
-        float acc[MT][2];  // the slots j0 + 16 m + r8 (+ 8); lane q4 = 0 begins with the weight so far
+        float acc[MT][2] = {}, before[MT][2];  // the slots j0 + 16 m + r8 (+ 8); their weight so far, wanted last
 #pragma unroll
         for (int m = 0; m < MT; m++)
 #pragma unroll
-            for (int i = 0; i < 2; i++) acc[m][i] = q4 == 0 && j0 + 16 * m + r8 + 8 * i < s.L ? __ldg(a.weight + at + 16 * m + 8 * i) : 0.0f;
+            for (int i = 0; i < 2; i++) before[m][i] = q4 == 0 && j0 + 16 * m + r8 + 8 * i < s.L ? __ldg(a.weight + at + 16 * m + 8 * i) : 0.0f;
         // rows that can see one of this warp's slots: tokens at or after the first slot, and within the window of the last
         const int p0 = s.L - s.nq, j_end = min(j0 + WS, s.L);
         int t_hi = s.nq - 1;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) weigh_kernel(WeighArgs a, int g
                 float x = acc[m][i];
                 x += __shfl_xor_sync(~0u, x, 1);
                 x += __shfl_xor_sync(~0u, x, 2);
-                if (q4 == 0 && j0 + 16 * m + r8 + 8 * i < s.L) a.weight_out[at + 16 * m + 8 * i] = x;
+                if (q4 == 0 && j0 + 16 * m + r8 + 8 * i < s.L) a.weight_out[at + 16 * m + 8 * i] = before[m][i] + x;
             }
         if (++stage == STAGES) stage = 0;
     }
@@ -236,8 +236,6 @@ __global__ void __launch_bounds__(32 * WARPS, 2) weigh_kernel(WeighArgs a, int g
 template <int D> cudaError_t weigh(const WeighArgs &a, int num_sms, cudaStream_t s) {
     using C = Weigh<D>;
     const size_t smem = (size_t)C::STAGES * C::STAGE + (a.v.B + 1) * 8;
-    cudaError_t e = cudaFuncSetAttribute(weigh_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
     int g_shift = -1;
     for (int i = 0; i < 11; i++)
         if (a.v.G == 1 << i) g_shift = i;
@@ -246,6 +244,11 @@ template <int D> cudaError_t weigh(const WeighArgs &a, int num_sms, cudaStream_t
 }
 
 }  // namespace
+
+cudaError_t prepare_weigh_mma() {
+    const cudaError_t e = allow_shared(weigh_kernel<64>);
+    return e == cudaSuccess ? allow_shared(weigh_kernel<128>) : e;
+}
 
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s) {
     return a.v.D == 64 ? weigh<64>(a, num_sms, s) : weigh<128>(a, num_sms, s);

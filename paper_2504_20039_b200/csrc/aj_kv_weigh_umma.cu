@@ -341,13 +341,16 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
 
 template <int D> cudaError_t weigh(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s) {
     const int smem = Cfg<D>::smem(a.v.B);
-    cudaError_t e = cudaFuncSetAttribute(weigh_umma_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
     weigh_umma_kernel<D><<<num_sms, THREADS, smem, s>>>(mk, a);
     return cudaGetLastError();
 }
 
 }  // namespace
+
+cudaError_t prepare_weigh_umma() {
+    const cudaError_t e = allow_shared(weigh_umma_kernel<64>);
+    return e == cudaSuccess ? allow_shared(weigh_umma_kernel<128>) : e;
+}
 
 cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s) {
     return a.v.D == 64 ? weigh<64>(a, mk, num_sms, s) : weigh<128>(a, mk, num_sms, s);
