@@ -5,12 +5,15 @@
 // lower slots first among equals; then move the r-th kept slot past `keep` into the r-th dropped slot below it.
 // Sources lie at or past `keep` and destinations below it, so the moves touch disjoint slots and need no order.
 //
-// A cluster of CTAs serves one (sequence, head): each selects for itself (a radix select of three digits over
-// keys in shared memory reads 8 bytes per slot, from L2 but for the first) and then makes its share of the moves,
-// which are what costs: 4 * D elements read or written per moved slot.  With few (sequence, head) pairs a
-// larger cluster spreads them over the SMs.  Nothing is written before every CTA of the cluster has selected, so the
-// state arrays may be updated in place.
+// A cluster of CTAs serves one (sequence, head), each a run of its slots: with few pairs a larger cluster spreads
+// them over the SMs.  The threshold comes from a radix select of three digits: every CTA counts its own slots in shared
+// memory and adds up the counts of the cluster through distributed shared memory.  Ranks of dropped and kept slots follow
+// from prefix sums over warps and CTAs, and each rank's slots are written into the list of the CTA that makes the move, so
+// that the moves (4 * D elements read or written per moved slot, the bulk of the bytes) are shared evenly.
+// It is the chain of barriers that bounds it, not the bytes: a cluster of 8 takes some 20,000 cycles for 16,384 slots.
+// Nothing is written before the whole cluster has read the state, so the state arrays may be updated in place.
 #include "aj_kv.cuh"
+#include "aj_ptx.cuh"
 
 namespace aj {
 namespace kv {
@@ -18,15 +21,16 @@ namespace kv {
 namespace {
 
 constexpr int LIST_MAX = 4096;         // moves a CTA lists at a time
-constexpr int KEYS_MAX = 40 * 1024;    // slots whose keys fit in shared memory; longer ones re-read the weights
+constexpr int KEYS_MAX = 32 * 1024;    // slots of a CTA whose keys fit in shared memory; more re-read the weights
 constexpr int BINS = 2048;             // digits of 11, 11 and 10 bits: the first one is a float's sign, exponent and two
                                        // bits of its fraction, so that weights of one magnitude do not queue up at one counter
+constexpr int MAX_CLUSTER = 8;
 
 struct Shared {
-    unsigned hist[BINS];
+    unsigned hist[3][BINS];
     unsigned scan[33], scan2[33];
     int newest, need;
-    unsigned prefix;
+    unsigned prefix, eq, holes, movers;
 };
 
 __device__ inline unsigned warp_sum(unsigned x) {
@@ -53,8 +57,15 @@ template <int NWARP> __device__ inline void scan_warps(unsigned *scan, unsigned 
     __syncthreads();
 }
 
+// A word of another CTA's shared memory.
+__device__ inline unsigned ld_cluster(const void *p, int rank) {
+    unsigned x;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(map_to_cta(smem_u32(p), rank)) : "memory");
+    return x;
+}
+
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int LIST) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int list_len) {
     constexpr int NWARP = THREADS / 32;
     extern __shared__ __align__(16) unsigned dyn[];
     __shared__ Shared sh;
@@ -67,74 +78,102 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     const float *w_in = a.weight + at;
     const int *p_in = a.slot_pos + at;
 
-    // The new length is written once every CTA of this sequence has read the old one (they may be one array).
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const unsigned total = (unsigned)v.Hkv * n_split;
-        __threadfence();
-        if (atomicInc(counters + b, total - 1) == total - 1) a.lens_out[b] = min(L, keep);
-    }
-    if (L <= keep) {  // the same for the whole cluster
-        for (int j = part * THREADS + threadIdx.x; j < L; j += n_split * THREADS) {
-            if (a.weight_out != a.weight) a.weight_out[at + j] = w_in[j];
-            if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = p_in[j];
-        }
-        return;
-    }
-
-    const int n_words = (L + 31) >> 5;
-    unsigned *list = dyn;                  // [2][LIST] holes, movers
-    unsigned *kept = dyn + 2 * LIST;       // [ceil(cap / 32)] one bit per slot
-    unsigned *keys = kept + ((v.cap + 31) >> 5);
-    const bool cached = L <= keys_cap;
-
+    for (int i = threadIdx.x; i < 3 * BINS; i += THREADS) (&sh.hist[0][0])[i] = 0;
     if (threadIdx.x == 0) {
         sh.newest = -0x7fffffff - 1;
         sh.prefix = 0;
         sh.need = keep;
     }
     __syncthreads();
+    // The new length is written once every CTA of this sequence has read the old one (they may be one array).
+    auto leave = [&]() {
+        if (threadIdx.x == 0) {
+            const unsigned total = (unsigned)v.Hkv * n_split;
+            __threadfence();
+            if (atomicInc(counters + b, total - 1) == total - 1) a.lens_out[b] = min(L, keep);
+        }
+    };
+    if (L <= keep) {  // the same for the whole cluster
+        for (int j = part * THREADS + threadIdx.x; j < L; j += n_split * THREADS) {
+            if (a.weight_out != a.weight) a.weight_out[at + j] = w_in[j];
+            if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = p_in[j];
+        }
+        leave();
+        return;
+    }
+    auto cluster_sync = [&]() {
+        if (n_split > 1) cluster_sync_all();
+        else __syncthreads();
+    };
+
+    // this CTA's slots: words w_lo .. w_hi - 1 of 32, slots j_lo .. j_hi - 1
+    const int n_words = (L + 31) >> 5, per = (n_words + n_split - 1) / n_split;
+    const int w_lo = min(n_words, part * per), w_hi = min(n_words, w_lo + per), j_lo = w_lo * 32, j_hi = min(L, w_hi * 32);
+    unsigned *list = dyn;                      // [2][list_len] holes, movers
+    unsigned *kept = dyn + 2 * list_len;       // one bit per slot of this CTA
+    unsigned *keys = kept + (((v.cap + 31) >> 5) + n_split - 1) / n_split;
+    const bool cached = j_hi - j_lo <= keys_cap;
+
     auto weight_key = [&](float w) -> unsigned { return w != w ? 0u : ordered_image(w); };
     int newest = -0x7fffffff - 1;
-#pragma unroll 8
-    for (int j = threadIdx.x; j < L; j += THREADS) {
+#pragma unroll 4
+    for (int j = j_lo + threadIdx.x; j < j_hi; j += THREADS) {
         newest = max(newest, __ldcg(p_in + j));
-        if (cached) keys[j] = weight_key(__ldcg(w_in + j));
+        if (cached) keys[j - j_lo] = weight_key(__ldcg(w_in + j));
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
     if (lane == 0) atomicMax(&sh.newest, newest);
-    __syncthreads();
-    const long long recent_from = (long long)sh.newest - a.recent;
+    cluster_sync();
+    newest = lane < n_split ? (int)ld_cluster(&sh.newest, lane) : -0x7fffffff - 1;
+#pragma unroll
+    for (int o = 4; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
+    newest = __shfl_sync(~0u, newest, 0);
+    const long long recent_from = (long long)newest - a.recent;
     auto fixed = [&](int j) {
         const int p = __ldcg(p_in + j);
         return p < a.sinks || p > recent_from;
     };
-    auto key_at = [&](int j) -> unsigned { return cached ? keys[j] : fixed(j) ? 0xffffffffu : weight_key(__ldcg(w_in + j)); };
+    auto key_at = [&](int j) -> unsigned { return cached ? keys[j - j_lo] : fixed(j) ? 0xffffffffu : weight_key(__ldcg(w_in + j)); };
 
     for (int digit = 0; digit < 3; digit++) {
         const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
-        for (int i = threadIdx.x; i < BINS; i += THREADS) sh.hist[i] = 0;
-        __syncthreads();
-        const unsigned prefix = sh.prefix, high = digit == 0 ? 0u : digit == 1 ? ~0u << 21 : ~0u << 10;
-#pragma unroll 8
-        for (int j = threadIdx.x; j < L; j += THREADS) {
+        unsigned *hist = sh.hist[digit];
+        const unsigned prefix = sh.prefix, high = digit == 0 ? 0u : digit == 1 ? ~0u << 21 : ~0u << 10, want = (unsigned)sh.need;
+#pragma unroll 4
+        for (int j = j_lo + threadIdx.x; j < j_hi; j += THREADS) {
             unsigned k;
             if (digit == 0 && cached) {  // the protected slots become known only now
-                k = fixed(j) ? 0xffffffffu : keys[j];
-                keys[j] = k;
+                k = fixed(j) ? 0xffffffffu : keys[j - j_lo];
+                keys[j - j_lo] = k;
             } else {
                 k = key_at(j);
             }
-            if (((k ^ prefix) & high) == 0) atomicAdd(&sh.hist[(k >> shift) & (bins - 1)], 1u);
+            if (((k ^ prefix) & high) == 0) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
         }
-        __syncthreads();
-        // thread i holds the PER digits from bins - 1 - PER * i down
+        cluster_sync();
+        // thread i holds the PER digits from bins - 1 - PER * i down, summed over the cluster
         constexpr int PER = BINS / THREADS;
         const int d0 = bins - 1 - PER * (int)threadIdx.x;
-        unsigned c[PER], mine = 0;
+        unsigned c[PER] = {}, mine = 0;
+        if (d0 >= 0) {
+            if (n_split == 1) {
 #pragma unroll
-        for (int i = 0; i < PER; i++) mine += c[i] = d0 >= 0 ? sh.hist[d0 - i] : 0u;
+                for (int i = 0; i < PER; i++) c[i] = hist[d0 - i];
+            } else {
+                unsigned x[MAX_CLUSTER][PER];
+#pragma unroll
+                for (int r = 0; r < MAX_CLUSTER; r++)
+#pragma unroll
+                    for (int i = 0; i < PER; i++) x[r][i] = r < n_split ? ld_cluster(hist + d0 - i, r) : 0u;
+#pragma unroll
+                for (int r = 0; r < MAX_CLUSTER; r++)
+#pragma unroll
+                    for (int i = 0; i < PER; i++) c[i] += x[r][i];
+            }
+#pragma unroll
+            for (int i = 0; i < PER; i++) mine += c[i];
+        }
         unsigned up = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -143,8 +182,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
         }
         scan_warps<NWARP>(sh.scan, __shfl_sync(~0u, up, 31));
         unsigned before = sh.scan[warp] + up - mine;
-        const unsigned want = (unsigned)sh.need;
-        __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; i++) {
             if (before < want && want <= before + c[i]) {
@@ -157,26 +194,35 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     }
     const unsigned thr = sh.prefix, need = (unsigned)sh.need;
 
+    // what the CTAs before this one, and all of them, hold of a counter
+    auto across = [&](const unsigned *p, unsigned &all) {
+        const unsigned x = lane < n_split ? ld_cluster(p, lane) : 0u;
+        all = warp_sum(x);
+        return warp_sum(lane < part ? x : 0u);
+    };
     // one bit per slot: kept.  A warp takes a run of words; among keys equal to the threshold the lowest slots stay
-    const int run = (n_words + NWARP - 1) / NWARP;
-    const int w0 = warp * run, w1 = min(n_words, w0 + run);
+    const int run = (w_hi - w_lo + NWARP - 1) / NWARP;
+    const int w0 = min(w_hi, w_lo + warp * run), w1 = min(w_hi, w0 + run);
     unsigned eq = 0;
     for (int w = w0; w < w1; w++) {
         const int j = w * 32 + lane;
         const unsigned k = j < L ? key_at(j) : 0u;
         const unsigned gt = __ballot_sync(~0u, j < L && k > thr), e = __ballot_sync(~0u, j < L && k == thr);
-        if (lane == 0) kept[w] = gt;
+        if (lane == 0) kept[w - w_lo] = gt;
         eq += __popc(e);
     }
     scan_warps<NWARP>(sh.scan, eq);
-    unsigned rank = sh.scan[warp];
+    if (threadIdx.x == 0) sh.eq = sh.scan[NWARP];
+    cluster_sync();
+    unsigned all;
+    unsigned rank = across(&sh.eq, all) + sh.scan[warp];
     for (int w = w0; w < w1 && rank < need; w++) {
         const int j = w * 32 + lane;
         const unsigned k = j < L ? key_at(j) : 0u;
         const unsigned e = __ballot_sync(~0u, j < L && k == thr);
         const bool mine = (e >> lane & 1) && rank + __popc(e & ((1u << lane) - 1)) < need;
         const unsigned add = __ballot_sync(~0u, mine);
-        if (lane == 0) kept[w] |= add;
+        if (lane == 0) kept[w - w_lo] |= add;
         rank += __popc(e);
     }
     __syncthreads();
@@ -191,105 +237,111 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     };
     unsigned holes = 0, movers = 0;
     for (int w = w0 + lane; w < w1; w += 32) {
-        holes += __popc(~kept[w] & below(w));
-        movers += __popc(kept[w] & ~below(w) & valid(w));
+        holes += __popc(~kept[w - w_lo] & below(w));
+        movers += __popc(kept[w - w_lo] & ~below(w) & valid(w));
     }
     scan_warps<NWARP>(sh.scan, warp_sum(holes));
     scan_warps<NWARP>(sh.scan2, warp_sum(movers));
-    const int n_moves = (int)sh.scan2[NWARP];  // as many holes as movers
-    const int share = (n_moves + n_split - 1) / n_split;
-    const int m0 = part * share, m1 = min(n_moves, m0 + share);
-
-    // every CTA of the cluster is done reading the weights and positions
-    if (n_split > 1) {
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x == 0) {
+        sh.holes = sh.scan[NWARP];
+        sh.movers = sh.scan2[NWARP];
     }
+    cluster_sync();
+    unsigned n_moves;  // as many holes as movers
+    const unsigned hole0 = across(&sh.holes, n_moves) + sh.scan[warp], mover0 = across(&sh.movers, n_moves) + sh.scan2[warp];
+    const int share = min(list_len, (int)(n_moves + n_split - 1) / n_split);  // moves a CTA makes at a time
+
     if (a.weight_out != a.weight || a.slot_pos_out != a.slot_pos) {
-        for (int j = part * THREADS + threadIdx.x; j < keep; j += n_split * THREADS) {
-            if (kept[j >> 5] >> (j & 31) & 1) {
+        for (int j = j_lo + threadIdx.x; j < min(j_hi, keep); j += THREADS) {
+            if (kept[(j >> 5) - w_lo] >> (j & 31) & 1) {
                 if (a.weight_out != a.weight) a.weight_out[at + j] = __ldcg(w_in + j);
                 if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = __ldcg(p_in + j);
             }
         }
     }
     const int n16 = v.D * a.elem / 16;  // 16-byte pieces of a row
-    for (int c0 = m0; c0 < m1; c0 += LIST) {
-        const int c1 = min(m1, c0 + LIST);
-        unsigned hr = sh.scan[warp], mr = sh.scan2[warp];
-        for (int w = w0; w < w1; w += 32) {  // 32 words at a time, one per lane
-            const int wl = w + lane;
-            unsigned hb = 0, mb = 0;
-            if (wl < w1) {
-                hb = ~kept[wl] & below(wl);
-                mb = kept[wl] & ~below(wl) & valid(wl);
+    for (int c0 = 0; c0 < (int)n_moves; c0 += share * n_split) {
+        // ranks c0 + k * share .. go to CTA k of the cluster
+        unsigned hr = hole0, mr = mover0;
+        auto put = [&](unsigned bits, unsigned &r0, int slot, unsigned *to) {  // one slot per lane
+            const int r = (int)(r0 + __popc(bits & ((1u << lane) - 1))) - c0;
+            if ((bits >> lane & 1) && r >= 0 && r < share * n_split) {
+                const int k = r / share;
+                if (n_split == 1) to[r] = slot;
+                else st_shared_cluster_u32(map_to_cta(smem_u32(to + (r - k * share)), k), (unsigned)slot);
             }
-            unsigned hs = __popc(hb), ms = __popc(mb);
-            const unsigned hc = hs, mc = ms;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const unsigned x = __shfl_up_sync(~0u, hs, o), y = __shfl_up_sync(~0u, ms, o);
-                if (lane >= o) {
-                    hs += x;
-                    ms += y;
-                }
-            }
-            int r = (int)(hr + hs - hc);
-            for (; hb; hb &= hb - 1, r++)
-                if (r >= c0 && r < c1) list[r - c0] = wl * 32 + __ffs(hb) - 1;
-            r = (int)(mr + ms - mc);
-            for (; mb; mb &= mb - 1, r++)
-                if (r >= c0 && r < c1) list[LIST + r - c0] = wl * 32 + __ffs(mb) - 1;
-            hr += __shfl_sync(~0u, hs, 31);
-            mr += __shfl_sync(~0u, ms, 31);
+            r0 += __popc(bits);
+        };
+        for (int w = w0; w < w1; w++) {
+            const unsigned bits = kept[w - w_lo];
+            put(~bits & below(w), hr, w * 32 + lane, list);
+            put(bits & ~below(w) & valid(w), mr, w * 32 + lane, list + list_len);
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < c1 - c0; i += THREADS) {
-            const int dst = list[i], src = list[LIST + i];
-            a.weight_out[at + dst] = __ldcg(w_in + src);
-            a.slot_pos_out[at + dst] = __ldcg(p_in + src);
+        cluster_sync();  // the lists are complete; and the whole cluster is done reading the state below keep
+        const int count = max(0, min(share, (int)n_moves - c0 - part * share));
+        for (int i = threadIdx.x; i < count; i += THREADS) {
+            const int dst = list[i], src = list[list_len + i];
             const int page = __ldg(v.table + (size_t)b * v.width + (dst >> v.page_shift));
+            const unsigned from = (unsigned)page_row(v, b, h, src);
+            const float w = __ldcg(w_in + src);
+            const int p = __ldcg(p_in + src);
             // a page that is not in the pool is never written
             list[i] = (unsigned)page < (unsigned)v.n_pages ? (unsigned)((page * v.Hkv + h) * v.page + (dst & (v.page - 1))) : ~0u;
-            list[LIST + i] = (unsigned)page_row(v, b, h, src);
+            list[list_len + i] = from;
+            a.weight_out[at + dst] = w;
+            a.slot_pos_out[at + dst] = p;
         }
         __syncthreads();
-        const int pieces = (c1 - c0) * n16;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < pieces; i += THREADS) {
-            const int r = i / n16, c = i - r * n16;
-            const size_t from = (size_t)list[LIST + r] * n16 + c;
-            const uint4 x = __ldcg((const uint4 *)a.k_pages + from), y = __ldcg((const uint4 *)a.v_pages + from);
-            if (list[r] != ~0u) {
-                const size_t to = (size_t)list[r] * n16 + c;
-                ((uint4 *)a.k_pages)[to] = x;
-                ((uint4 *)a.v_pages)[to] = y;
+        const int pieces = count * n16;
+        constexpr int AHEAD = 4;  // loads before the first store
+        for (int i0 = threadIdx.x; i0 < pieces; i0 += AHEAD * THREADS) {
+            uint4 x[AHEAD], y[AHEAD];
+            size_t to[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++) {
+                const int i = i0 + u * THREADS, r = i / n16, c = i - r * n16;
+                to[u] = ~(size_t)0;
+                if (i < pieces && list[r] != ~0u) {
+                    const size_t from = (size_t)list[list_len + r] * n16 + c;
+                    to[u] = (size_t)list[r] * n16 + c;
+                    x[u] = __ldcg((const uint4 *)a.k_pages + from);
+                    y[u] = __ldcg((const uint4 *)a.v_pages + from);
+                }
             }
+#pragma unroll
+            for (int u = 0; u < AHEAD; u++)
+                if (to[u] != ~(size_t)0) {
+                    ((uint4 *)a.k_pages)[to[u]] = x[u];
+                    ((uint4 *)a.v_pages)[to[u]] = y[u];
+                }
         }
-        __syncthreads();
+        if (c0 + share * n_split < (int)n_moves) cluster_sync();  // the lists are free again
     }
+    if (n_moves == 0) cluster_sync();  // no CTA leaves while another may still read its counters
+    leave();
 }
 
 }  // namespace
 
 cudaError_t prepare_evict() {
-    const cudaError_t e = allow_shared(evict_kernel<512>);
+    cudaError_t e = allow_shared(evict_kernel<512>);
     return e == cudaSuccess ? allow_shared(evict_kernel<1024>) : e;
 }
 
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s) {
     const int items = a.v.B * a.v.Hkv;
-    int n_split = 1;
-    while (n_split < 8 && items * n_split * 2 <= num_sms) n_split *= 2;
-    const int words = (a.v.cap + 31) / 32, keys = a.v.cap < KEYS_MAX ? a.v.cap : KEYS_MAX;
-    const int most = a.v.cap / 2 + 1, list = most < LIST_MAX ? most : LIST_MAX;  // at most half of the slots move
+    int n_split = 1;  // as many CTAs per pair as the SMs hold
+    while (n_split < MAX_CLUSTER && items * n_split * 2 <= num_sms) n_split *= 2;
+    const int cap = (((a.v.cap + 31) / 32) + n_split - 1) / n_split * 32;  // slots of a CTA
+    const int keys_want = cap < KEYS_MAX ? cap : KEYS_MAX;
+    const int most = (a.v.cap / 2 + n_split) / n_split, list = most < LIST_MAX ? most : LIST_MAX;  // at most half of the slots move
     // the keys share what the bit map of a very long cache leaves
-    const size_t fixed = (size_t)(2 * list + words) * 4;
-    const size_t room = 212 * 1024 - fixed;
-    const int keys_cap = (size_t)keys * 4 <= room ? keys : (int)(room / 4);
+    const size_t fixed = (size_t)(2 * list + cap / 32) * 4;
+    const size_t room = 196 * 1024 - fixed;
+    const int keys_cap = (size_t)keys_want * 4 <= room ? keys_want : (int)(room / 4);
     const size_t smem = fixed + (size_t)keys_cap * 4;
     // more CTAs than SMs: two CTAs of half the threads share an SM, so that one's barriers hide behind the other
-    const bool half = items * n_split > num_sms && smem <= 96 * 1024;
+    const bool half = items * n_split > num_sms && smem <= 80 * 1024;
     auto kernel = half ? evict_kernel<512> : evict_kernel<1024>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(items * n_split);
