@@ -6,7 +6,7 @@
 // Sources lie at or past `keep` and destinations below it, so the moves touch disjoint slots and need no order.
 //
 // A cluster of CTAs serves one (sequence, head), each a run of its slots: with few pairs a larger cluster spreads
-// them over the SMs.  The threshold comes from a radix select of three digits: every CTA counts its own slots in shared
+// them over the SMs.  The threshold comes from a radix select of four digits: every CTA counts its own slots in shared
 // memory and adds up the counts of the cluster through distributed shared memory.  Ranks of dropped and kept slots follow
 // from prefix sums over warps and CTAs, and each rank's slots are written into the list of the CTA that makes the move, so
 // that the moves (4 * D elements read or written per moved slot, the bulk of the bytes) are shared evenly.
@@ -22,12 +22,13 @@ namespace {
 
 constexpr int LIST_MAX = 4096;         // moves a CTA lists at a time
 constexpr int KEYS_MAX = 32 * 1024;    // slots of a CTA whose keys fit in shared memory; more re-read the weights
-constexpr int BINS = 2048;             // digits of 11, 11 and 10 bits: the first one is a float's sign, exponent and two
-                                       // bits of its fraction, so that weights of one magnitude do not queue up at one counter
+// Digits of 9, 8, 8 and 7 bits: the first one is a float's sign and exponent, spread enough that a warp's counts do not queue
+// up at one counter; and adding up 512 counters of 8 CTAs costs less than a digit more (2048 counters: 6,000 cycles).
+constexpr int DIGITS = 4, BINS = 512;
 constexpr int MAX_CLUSTER = 8;
 
 struct Shared {
-    unsigned hist[3][BINS];
+    unsigned hist[DIGITS][BINS];
     unsigned scan[33], scan2[33];
     int newest, need;
     unsigned prefix, eq, holes, movers;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     const float *w_in = a.weight + at;
     const int *p_in = a.slot_pos + at;
 
-    for (int i = threadIdx.x; i < 3 * BINS; i += THREADS) (&sh.hist[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < DIGITS * BINS; i += THREADS) (&sh.hist[0][0])[i] = 0;
     if (threadIdx.x == 0) {
         sh.newest = -0x7fffffff - 1;
         sh.prefix = 0;
@@ -136,10 +137,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     };
     auto key_at = [&](int j) -> unsigned { return cached ? keys[j - j_lo] : fixed(j) ? 0xffffffffu : weight_key(__ldcg(w_in + j)); };
 
-    for (int digit = 0; digit < 3; digit++) {
-        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bins = digit == 2 ? 1024 : 2048;
+    for (int digit = 0; digit < DIGITS; digit++) {
+        const int shift = digit == 0 ? 23 : digit == 1 ? 15 : digit == 2 ? 7 : 0, bins = digit == 0 ? 512 : digit == 3 ? 128 : 256;
         unsigned *hist = sh.hist[digit];
-        const unsigned prefix = sh.prefix, high = digit == 0 ? 0u : digit == 1 ? ~0u << 21 : ~0u << 10, want = (unsigned)sh.need;
+        const unsigned prefix = sh.prefix, high = digit == 0 ? 0u : ~0u << (shift + (digit == 3 ? 7 : 8)), want = (unsigned)sh.need;
 #pragma unroll 4
         for (int j = j_lo + threadIdx.x; j < j_hi; j += THREADS) {
             unsigned k;
@@ -152,27 +153,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
             if (((k ^ prefix) & high) == 0) atomicAdd(&hist[(k >> shift) & (bins - 1)], 1u);
         }
         cluster_sync();
-        // thread i holds the PER digits from bins - 1 - PER * i down, summed over the cluster
-        constexpr int PER = BINS / THREADS;
-        const int d0 = bins - 1 - PER * (int)threadIdx.x;
-        unsigned c[PER] = {}, mine = 0;
-        if (d0 >= 0) {
+        // thread i holds the digit bins - 1 - i, summed over the cluster
+        const int d = bins - 1 - (int)threadIdx.x;
+        unsigned mine = 0;
+        if (d >= 0) {
             if (n_split == 1) {
-#pragma unroll
-                for (int i = 0; i < PER; i++) c[i] = hist[d0 - i];
+                mine = hist[d];
             } else {
-                unsigned x[MAX_CLUSTER][PER];
+                unsigned x[MAX_CLUSTER];
 #pragma unroll
-                for (int r = 0; r < MAX_CLUSTER; r++)
+                for (int r = 0; r < MAX_CLUSTER; r++) x[r] = r < n_split ? ld_cluster(hist + d, r) : 0u;
 #pragma unroll
-                    for (int i = 0; i < PER; i++) x[r][i] = r < n_split ? ld_cluster(hist + d0 - i, r) : 0u;
-#pragma unroll
-                for (int r = 0; r < MAX_CLUSTER; r++)
-#pragma unroll
-                    for (int i = 0; i < PER; i++) c[i] += x[r][i];
+                for (int r = 0; r < MAX_CLUSTER; r++) mine += x[r];
             }
-#pragma unroll
-            for (int i = 0; i < PER; i++) mine += c[i];
         }
         unsigned up = mine;
 #pragma unroll
@@ -181,14 +174,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
             if (lane >= o) up += z;
         }
         scan_warps<NWARP>(sh.scan, __shfl_sync(~0u, up, 31));
-        unsigned before = sh.scan[warp] + up - mine;
-#pragma unroll
-        for (int i = 0; i < PER; i++) {
-            if (before < want && want <= before + c[i]) {
-                sh.prefix = prefix | ((unsigned)(d0 - i) << shift);
-                sh.need = (int)(want - before);
-            }
-            before += c[i];
+        const unsigned before = sh.scan[warp] + up - mine;
+        if (before < want && want <= before + mine) {
+            sh.prefix = prefix | ((unsigned)d << shift);
+            sh.need = (int)(want - before);
         }
         __syncthreads();
     }
@@ -251,14 +240,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     const unsigned hole0 = across(&sh.holes, n_moves) + sh.scan[warp], mover0 = across(&sh.movers, n_moves) + sh.scan2[warp];
     const int share = min(list_len, (int)(n_moves + n_split - 1) / n_split);  // moves a CTA makes at a time
 
-    if (a.weight_out != a.weight || a.slot_pos_out != a.slot_pos) {
-        for (int j = j_lo + threadIdx.x; j < min(j_hi, keep); j += THREADS) {
-            if (kept[(j >> 5) - w_lo] >> (j & 31) & 1) {
-                if (a.weight_out != a.weight) a.weight_out[at + j] = __ldcg(w_in + j);
-                if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = __ldcg(p_in + j);
-            }
-        }
-    }
     const int n16 = v.D * a.elem / 16;  // 16-byte pieces of a row
     for (int c0 = 0; c0 < (int)n_moves; c0 += share * n_split) {
         // ranks c0 + k * share .. go to CTA k of the cluster
@@ -316,6 +297,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
                 }
         }
         if (c0 + share * n_split < (int)n_moves) cluster_sync();  // the lists are free again
+    }
+    // slots that stay where they are
+    if (a.weight_out != a.weight || a.slot_pos_out != a.slot_pos) {
+        for (int j = j_lo + threadIdx.x; j < min(j_hi, keep); j += THREADS) {
+            if (kept[(j >> 5) - w_lo] >> (j & 31) & 1) {
+                if (a.weight_out != a.weight) a.weight_out[at + j] = __ldcg(w_in + j);
+                if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = __ldcg(p_in + j);
+            }
+        }
     }
     if (n_moves == 0) cluster_sync();  // no CTA leaves while another may still read its counters
     leave();
