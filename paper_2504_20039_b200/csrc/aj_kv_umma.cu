@@ -560,6 +560,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // ---------------------------------------------------------------- softmax of stream x
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
             Line c = seek(v, tpt, pre, u0);
+            // rows of a query tile without a token stay zero (or what an item before had there): the tensor cores draw less
+            // power on zeros, and power is what limits the clock
+            for (int i = threadIdx.x; i < 2 * C::TILE_BYTES / 16; i += 256) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
             fence_async_shared();
             __syncthreads();  // the prefix sums are read
             const int x = warp >> 2, row = threadIdx.x & 127, wq = warp & 3;
@@ -592,12 +595,32 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
                 bool first = true;
+                // slots that nobody sees may hold anything: their values are cleared before the product
+                auto clear_hidden = [&](int t, int j0) {
+                    if (c.q.s.L - j0 >= TILE && (j0 >= c.p.first || c.p.first <= v.sinks)) return;
+                    const uint32_t at = g + pos_v(t, n), s = at % NS;
+                    wait(full(s), at / NS);
+                    const int j = j0 + row;
+                    if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
+#pragma unroll 1
+                        for (int i = 0; i < 8 * HALVES; i++)
+                            *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + (i >> 3) * 16384 + row * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_shared();
+                    __syncwarp();
+                };
                 for (int t = shared_rows ? x : 0; t < n; t += step) {
                     const int j0 = tile_of(c.p, pt.first + t) * TILE;
                     const bool masked = j0 + TILE > p_first + 1 || (v.window && j0 <= p_last - v.window);
 #pragma unroll 1
                     for (int hf = 0; hf < 2; hf++, n_h++) {
                         wait(s_full(x, hf), n_h >> 1);
+                        if (hf == 0) clear_hidden(t, j0);
+                        if (wq * 32 >= n_rows) {  // a warp without a row: zero queries have left zeros where its weights go
+                            first = false;
+                            mbar_arrive(p_ready(x, hf));
+                            continue;
+                        }
                         uint32_t sr[64];
                         tmem_ld64(t_s + hf * 64, sr);
                         if (masked) {
@@ -629,21 +652,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             l *= c2;
 #pragma unroll 1
                             for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
-                        }
-                        // slots that nobody sees may hold anything: their values are cleared before the product
-                        if (hf == 0 && (c.q.s.L - j0 < TILE || (j0 < c.p.first && c.p.first > v.sinks))) {
-                            const uint32_t at = g + pos_v(t, n), s = at % NS;
-                            wait(full(s), at / NS);
-                            const int j = j0 + row;
-                            if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
-#pragma unroll
-                                for (int hh = 0; hh < HALVES; hh++)
-#pragma unroll
-                                    for (int i = 0; i < 8; i++)
-                                        *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + hh * 16384 + row * 128 + i * 16) = make_uint4(0, 0, 0, 0);
-                            }
-                            fence_async_shared();
-                            __syncwarp();
                         }
                         const float ref = m == -INFINITY ? 0.0f : m;
                         const uint64_t scale2 = f2(scale, scale), ref2 = f2(-ref, -ref);
