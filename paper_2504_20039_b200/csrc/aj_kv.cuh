@@ -9,6 +9,9 @@ namespace aj {
 namespace kv {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// A running maximum (in units of log2) is left alone until a score exceeds it by this much: sums of 2^20 weights of 2^30
+// are far from the end of f32's range.
+constexpr float RAISE = 30.0f;
 
 // What a call says about the cache and its new tokens (device pointers).
 struct View {

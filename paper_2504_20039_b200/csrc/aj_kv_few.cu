@@ -13,8 +13,8 @@
 // output) are joined at the end of an item.  An item that spans CTAs leaves partial results in the workspace and the
 // CTA that arrives last joins them, in the order of the CTAs.
 //
-// The running maximum is only a common reference: it is raised when a score exceeds it by more than 2^8 (one
-// vote per block instead of six shuffles), and weights up to 2^8 are as exact in bf16 and f32 as weights up to 1.
+// The running maximum is only a common reference: it is raised when a score exceeds it by more than RAISE (one
+// vote per block instead of six shuffles), and weights far above 1 are as exact in bf16 and f32 as weights up to 1.
 #include "aj_kv.cuh"
 #include "aj_kv_mma.cuh"
 
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                     if (!sees(v, p_lo + r / v.G, j)) x = -INFINITY;
                 }
                 s[n][0][i] = x;
-                raise |= x > m[n][i & 1] + 8.0f;
+                raise |= x > m[n][i & 1] + RAISE;
             }
         if (__any_sync(~0u, raise)) {
 #pragma unroll
