@@ -83,14 +83,14 @@ size_t umma_parts_floats(int D, int num_sms);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);
 cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s);
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s);
-cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s);
+cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clusters)[4], int num_sms, cudaStream_t s);
 
 // Once per device, before the first launch: more than 48 KB of shared memory per CTA.
 cudaError_t prepare_attend_few();
 cudaError_t prepare_attend_umma();
 cudaError_t prepare_weigh_mma();
 cudaError_t prepare_weigh_umma();
-cudaError_t prepare_evict();
+cudaError_t prepare_evict(int (&clusters)[4]);
 
 // Sizes of the split-attention workspace that the CUDA-core kernels can use for this handle.
 constexpr int SIMT_MAX_SPLITS = 64;

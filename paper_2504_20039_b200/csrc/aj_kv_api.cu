@@ -11,6 +11,7 @@ using namespace aj;
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+typedef CUresult (*ReplaceAddressFn)(CUtensorMap *, void *);
 
 struct aj_kv_s {
     int device = 0, num_sms = 0;
@@ -22,7 +23,12 @@ struct aj_kv_s {
     unsigned *counters = nullptr;  // [n_counters] attention items, then [max_B] eviction
     int n_counters = 0;
     int *status = nullptr;
+    int clusters[4] = {};          // see prepare_evict
     EncodeTiledFn encode = nullptr;
+    ReplaceAddressFn replace = nullptr;
+    // tensor maps of pages, and of query rows of stride q_stride in boxes of one token and of eight: a call puts its addresses in
+    CUtensorMap pages = {}, rows1 = {}, rows8 = {};
+    long long q_stride = -1;
     int last_launches = 0;
     const char *last_path = "none";
 };
@@ -90,24 +96,29 @@ kv::View view_of(aj_kv h, int n_pages, const int32_t *table, int width, const in
     return v;
 }
 
-// A tensor map of pages as [n_pages * Hkv * page_size, D], boxes of 64 elements x one page, 128-byte swizzle.
-bool page_map(aj_kv h, CUtensorMap *m, const void *pages, int n_pages) {
-    const cuuint64_t dims[2] = {(cuuint64_t)h->D, (cuuint64_t)n_pages * h->Hkv * h->page};
+// A tensor map of pages as rows of D elements, boxes of 64 elements x one page, 128-byte swizzle.  Page numbers are checked
+// in the kernels, so the map's row count is only an upper bound; the address is put in by each call.
+bool encode_pages(aj_kv h, void *any) {
+    const cuuint64_t dims[2] = {(cuuint64_t)h->D, 0x7fffffff};
     const cuuint64_t strides[1] = {(cuuint64_t)h->D * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)h->page}, one[2] = {1, 1};
-    return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pages), dims, strides, box, one,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return h->encode(&h->pages, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, any, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// A tensor map of query rows as [rows, Hq, D], boxes of 64 elements x the heads of one key head x `tokens`.
-bool query_map(aj_kv h, CUtensorMap *m, const void *q, long long stride, long long rows, int tokens) {
-    const cuuint64_t dims[3] = {(cuuint64_t)h->D, (cuuint64_t)h->Hq, (cuuint64_t)rows};
+// A tensor map of query rows as [rows, Hq, D], boxes of 64 elements x the heads of one key head x `tokens`.  How many rows
+// exist is known on the device only; no copy goes past a sequence's own.
+bool encode_rows(aj_kv h, CUtensorMap *m, void *any, long long stride, int tokens) {
+    const cuuint64_t dims[3] = {(cuuint64_t)h->D, (cuuint64_t)h->Hq, 1u << 30};
     const cuuint64_t strides[2] = {(cuuint64_t)h->D * 2, (cuuint64_t)stride * 2};
     const cuuint32_t box[3] = {64, (cuuint32_t)(h->Hq / h->Hkv), (cuuint32_t)tokens}, one[3] = {1, 1, 1};
-    return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, one,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, any, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool at_address(aj_kv h, CUtensorMap *m, const CUtensorMap &from, const void *p) {
+    *m = from;
+    return h->replace(m, const_cast<void *>(p)) == CUDA_SUCCESS;
 }
 
 aj_status done(cudaError_t e) {
@@ -160,7 +171,7 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     h->dtype = dtype;
     h->flags = flags;
     if (kv::prepare_attend_few() != cudaSuccess || kv::prepare_attend_umma() != cudaSuccess || kv::prepare_weigh_mma() != cudaSuccess ||
-        kv::prepare_weigh_umma() != cudaSuccess || kv::prepare_evict() != cudaSuccess) {
+        kv::prepare_weigh_umma() != cudaSuccess || kv::prepare_evict(h->clusters) != cudaSuccess) {
         cudaGetLastError();
         delete h;
         return AJ_ERR_CUDA;
@@ -184,12 +195,23 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
             return AJ_ERR_CUDA;
         }
         h->encode = reinterpret_cast<EncodeTiledFn>(fn);
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapReplaceAddress", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess || !fn) {
+            cudaGetLastError();
+            delete h;
+            return AJ_ERR_CUDA;
+        }
+        h->replace = reinterpret_cast<ReplaceAddressFn>(fn);
     }
     const size_t n = (size_t)h->n_counters + max_B;
     if (cudaMalloc(&h->parts, h->parts_floats * 4) != cudaSuccess || cudaMalloc(&h->counters, n * 4) != cudaSuccess ||
         cudaMemset(h->counters, 0, n * 4) != cudaSuccess || cudaMalloc(&h->status, 256) != cudaSuccess ||
         cudaMemset(h->status, 0, 256) != cudaSuccess) {
         cudaGetLastError();
+        aj_kv_destroy(h);
+        return AJ_ERR_CUDA;
+    }
+    if (many && !encode_pages(h, h->parts)) {
         aj_kv_destroy(h);
         return AJ_ERR_CUDA;
     }
@@ -282,11 +304,15 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     }
     if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows)
         h->last_path = "umma";
-        CUtensorMap maps[4] = {};
-        if (!page_map(h, &maps[0], k_pages, n_pages) || !page_map(h, &maps[1], v_pages, n_pages)) return AJ_ERR_CUDA;
+        CUtensorMap maps[4];
+        if (!at_address(h, &maps[0], h->pages, k_pages) || !at_address(h, &maps[1], h->pages, v_pages)) return AJ_ERR_CUDA;
         const int q_tma = !on128(q, q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
-        // the rows that exist are known on the device only; no copy goes past a sequence's own
-        if (q_tma && (!query_map(h, &maps[2], q, q_stride, 1 << 30, 1) || (q_tma == 8 && !query_map(h, &maps[3], q, q_stride, 1 << 30, 8)))) return AJ_ERR_CUDA;
+        if (q_tma && q_stride != h->q_stride) {
+            h->q_stride = -1;
+            if (!encode_rows(h, &h->rows1, h->parts, q_stride, 1) || (q_tma == 8 && !encode_rows(h, &h->rows8, h->parts, q_stride, 8))) return AJ_ERR_CUDA;
+            h->q_stride = q_stride;
+        }
+        if (q_tma && (!at_address(h, &maps[2], h->rows1, q) || (q_tma == 8 && !at_address(h, &maps[3], h->rows8, q)))) return AJ_ERR_CUDA;
         h->last_launches = 2;
         return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
     }
@@ -319,7 +345,7 @@ aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *l
     if (h->tensor && n_q * a.v.G > kv::FEW_ROWS && on128(k_pages)) {
         h->last_path = "umma";
         CUtensorMap mk;
-        if (!page_map(h, &mk, k_pages, n_pages)) return AJ_ERR_CUDA;
+        if (!at_address(h, &mk, h->pages, k_pages)) return AJ_ERR_CUDA;
         return done(kv::launch_weigh_umma(a, mk, h->num_sms, (cudaStream_t)cuda_stream));
     }
     if (h->tensor) {
@@ -356,7 +382,7 @@ aj_status aj_kv_evict(aj_kv h, void *k_pages, void *v_pages, int n_pages, const 
     a.weight_out = weight_out;
     a.slot_pos_out = slot_pos_out;
     h->last_launches = 1;
-    return done(kv::launch_evict(a, h->counters + h->n_counters, h->num_sms, (cudaStream_t)cuda_stream));
+    return done(kv::launch_evict(a, h->counters + h->n_counters, h->clusters, h->num_sms, (cudaStream_t)cuda_stream));
 }
 
 aj_status aj_kv_last_status(aj_kv h) {

@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     for (int o = 16; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
     if (lane == 0) atomicMax(&sh.newest, newest);
     cluster_sync();
-    newest = lane < n_split ? (int)ld_cluster(&sh.newest, lane) : -0x7fffffff - 1;
+    newest = n_split == 1 ? sh.newest : lane < n_split ? (int)ld_cluster(&sh.newest, lane) : -0x7fffffff - 1;
 #pragma unroll
     for (int o = 4; o; o >>= 1) newest = max(newest, __shfl_xor_sync(~0u, newest, o));
     newest = __shfl_sync(~0u, newest, 0);
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
 
     // what the CTAs before this one, and all of them, hold of a counter
     auto across = [&](const unsigned *p, unsigned &all) {
-        const unsigned x = lane < n_split ? ld_cluster(p, lane) : 0u;
+        const unsigned x = n_split == 1 ? (lane == 0 ? *p : 0u) : lane < n_split ? ld_cluster(p, lane) : 0u;
         all = warp_sum(x);
         return warp_sum(lane < part ? x : 0u);
     };
@@ -313,15 +313,33 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
 
 }  // namespace
 
-cudaError_t prepare_evict() {
+// clusters[i]: how many clusters of 2^i CTAs of 1024 threads the device holds at once (a cluster stays within one GPC).
+cudaError_t prepare_evict(int (&clusters)[4]) {
     cudaError_t e = allow_shared(evict_kernel<512>);
-    return e == cudaSuccess ? allow_shared(evict_kernel<1024>) : e;
+    if (e == cudaSuccess) e = allow_shared(evict_kernel<1024>);
+    for (int i = 0; i < 4 && e == cudaSuccess; i++) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1 << i);
+        cfg.blockDim = dim3(1024);
+        cfg.dynamicSmemBytes = 96 * 1024;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1 << i;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&clusters[i], evict_kernel<1024>, &cfg);
+    }
+    return e;
 }
 
-cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cudaStream_t s) {
+cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clusters)[4], int num_sms, cudaStream_t s) {
     const int items = a.v.B * a.v.Hkv;
-    int n_split = 1;  // as many CTAs per pair as the SMs hold
-    while (n_split < MAX_CLUSTER && items * n_split * 2 <= num_sms) n_split *= 2;
+    // as many CTAs per pair as run at once, but no fewer than 1024 slots for a CTA: the barriers of a cluster cost more than
+    // the slots that it takes off a CTA's hands
+    int log_split = 0;
+    while (log_split < 3 && items <= clusters[log_split + 1] && (1024 << log_split) < a.v.cap) log_split++;
+    const int n_split = 1 << log_split;
     const int cap = (((a.v.cap + 31) / 32) + n_split - 1) / n_split * 32;  // slots of a CTA
     const int keys_want = cap < KEYS_MAX ? cap : KEYS_MAX;
     const int most = (a.v.cap / 2 + n_split) / n_split, list = most < LIST_MAX ? most : LIST_MAX;  // at most half of the slots move
@@ -330,8 +348,9 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cu
     const size_t room = 196 * 1024 - fixed;
     const int keys_cap = (size_t)keys_want * 4 <= room ? keys_want : (int)(room / 4);
     const size_t smem = fixed + (size_t)keys_cap * 4;
-    // more CTAs than SMs: two CTAs of half the threads share an SM, so that one's barriers hide behind the other
-    const bool half = items * n_split > num_sms && smem <= 80 * 1024;
+    // Half the threads where there is little to do for each, so that barriers are cheaper, and where there are more CTAs than
+    // SMs: two then share an SM, and one's barriers hide behind the other.
+    const bool half = smem <= 80 * 1024 && (items * n_split > num_sms || cap <= 2048);
     auto kernel = half ? evict_kernel<512> : evict_kernel<1024>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(items * n_split);
@@ -343,7 +362,7 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, int num_sms, cu
     attr.val.clusterDim.x = n_split;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = n_split > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a, counters, n_split, keys_cap, list);
 }
 

@@ -306,6 +306,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the joining kernel comes up as CTAs leave; it waits for the whole grid
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
             mbar_init(full(s), 1);
@@ -756,8 +757,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             }
         }
     }
-    // the joining kernel may come up while the last CTAs store their results; it waits for the whole grid
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
