@@ -179,7 +179,8 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     // CUDA-core kernels: 6 waves of pieces, or two per item if that is more, up to 64 MB
     const int G = Hq / Hkv;
     const long long items = (long long)max_B * Hkv * (((long long)max_q * G + kv::SIMT_ROWS - 1) / kv::SIMT_ROWS);
-    h->n_counters = (int)(items < 65536 ? items : 65536);  // (at least one for each of the at most 65535 key heads of a batch)
+    h->n_counters = (int)(items < 65536 ? items : 65536);
+    if (h->n_counters < 2 * sms) h->n_counters = 2 * sms;  // tcgen05 kernel: two streams of the item that spans on from a CTA
     h->parts_floats = (size_t)(7 * sms) * kv::SIMT_ROWS * (D + 2);
     h->tensor = dtype == AJ_BF16 && (D == 64 || D == 128) && !(flags & AJ_KV_FLAG_FORCE_SIMT);
     if (h->tensor && kv::few_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::few_parts_floats(D, sms);
@@ -313,7 +314,7 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
             h->q_stride = q_stride;
         }
         if (q_tma && (!at_address(h, &maps[2], h->rows1, q) || (q_tma == 8 && !at_address(h, &maps[3], h->rows8, q)))) return AJ_ERR_CUDA;
-        h->last_launches = 2;
+        h->last_launches = 1;
         return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
     }
     h->last_path = "simt";

@@ -16,7 +16,8 @@
 //
 // The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
 // CTA: causal prompts and ragged caches are balanced alike.  Items that span CTAs leave unnormalised partial results
-// (f32) in the workspace, which a second kernel, launched as a programmatic dependent, joins.
+// (f32) in the workspace, and the CTA that arrives last joins them, in the order of the CTAs (a second kernel for that cost 11
+// to 16 us a call, most of it in finding its place on the line).
 //
 // What bounds it: a window of K + 1 rows reads 512 bytes of K and V per slot and head and is bound by HBM up to about
 // 256 rows; a prompt is bound by the exponentials (16 per clock and SM: 2048 cycles per two tiles of 128 x 128)
@@ -306,7 +307,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the joining kernel comes up as CTAs leave; it waits for the whole grid
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
             mbar_init(full(s), 1);
@@ -585,7 +585,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
             for (int u = u0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
-                const int n = pt.n;
+                const int n = pt.n, unit = c.unit;
                 u += pt.line;
                 if (n == 0) continue;
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
@@ -706,9 +706,25 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         m = mm;
                     }
                 }
+                __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
+                auto store = [&](const float (&y)[32], float inv, int at) {  // 32 elements of this row
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i++) w[i] = pack2(y[2 * i] * inv, y[2 * i + 1] * inv);
+                    if (wide_out) {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 8)
+                            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o + at + 2 * i), I8(w, i) : "memory");
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(o + at + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                    }
+                };
+                auto store_lse = [&](float m, float l) {
+                    if (a.lse) a.lse[out_row * v.Hq + head] = l > 0.0f ? (m + log2f(l)) * LN2 : -INFINITY;
+                };
                 if (!shared_rows || x == 0) {
                     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-                    __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
 #pragma unroll 1
                     for (int k = 0; k < D / 32; k++) {  // not unrolled: code that runs once per item mostly costs its way into the cache
                         float ov[32];
@@ -722,17 +738,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         }
                         if (row < n_rows) {
                             if (whole) {
-                                uint32_t w[16];
-#pragma unroll
-                                for (int i = 0; i < 16; i++) w[i] = pack2(ov[2 * i] * inv, ov[2 * i + 1] * inv);
-                                if (wide_out) {
-#pragma unroll
-                                    for (int i = 0; i < 16; i += 8)
-                                        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o + k * 32 + 2 * i), I8(w, i) : "memory");
-                                } else {
-#pragma unroll
-                                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(o + k * 32 + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-                                }
+                                store(ov, inv, k * 32);
                             } else {
 #pragma unroll
                                 for (int i = 0; i < 8; i++)
@@ -742,12 +748,59 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     }
                     if (row < n_rows) {
                         if (whole) {
-                            if (a.lse) a.lse[out_row * v.Hq + head] = l > 0.0f ? (m + log2f(l)) * LN2 : -INFINITY;
+                            store_lse(m, l);
                         } else {
                             float *pm = reinterpret_cast<float *>(part) + 256 * D + x * 128 + row;
                             pm[0] = m;
                             pm[256] = l;
                         }
+                    }
+                }
+                if (!whole) {
+                    // streams of their own rows arrive and join by themselves, streams that share rows together
+                    const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
+                    const int i0 = u - pt.line - unit, cta0 = i0 / per, n_parts = (i0 + c.p.units - 1) / per - cta0 + 1;
+                    volatile uint32_t *last = tmem_slot + 2 + who;
+                    __threadfence();
+                    __syncwarp();
+                    bar_sync(id, threads);
+                    if (row == 0 && x == who) {
+                        const bool all = atomicAdd(a.counters + 2 * cta0 + who, 1u) == (unsigned)n_parts - 1;
+                        if (all) a.counters[2 * cta0 + who] = 0u;
+                        *last = all;
+                    }
+                    __syncwarp();
+                    bar_sync(id, threads);
+                    if (*last && row < n_rows) {
+                        __threadfence();
+                        auto part_at = [&](int i) { return a.parts + ((size_t)(cta0 + i) * 2 + (i == 0 ? 1 : 0)) * C::PART + who * 128 + row; };
+                        float mm = -INFINITY, ll = 0.0f;
+#pragma unroll 8
+                        for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, __ldcg(part_at(i) + 256 * D));
+                        const float ref = mm == -INFINITY ? 0.0f : mm;
+#pragma unroll 8
+                        for (int i = 0; i < n_parts; i++) ll += ex2(__ldcg(part_at(i) + 256 * D) - ref) * __ldcg(part_at(i) + 256 * (D + 1));
+                        const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+                        const int k1 = shared_rows ? (x + 1) * (D / 64) : D / 32;
+#pragma unroll 1
+                        for (int k = shared_rows ? x * (D / 64) : 0; k < k1; k++) {
+                            float y[32] = {};
+#pragma unroll 2
+                            for (int i = 0; i < n_parts; i++) {
+                                const float w = ex2(__ldcg(part_at(i) + 256 * D) - ref);
+                                const float4 *q = reinterpret_cast<const float4 *>(part_at(i) - (who * 128 + row)) + k * 8 * 256 + who * 128 + row;
+#pragma unroll
+                                for (int j = 0; j < 8; j++) {
+                                    const float4 z = __ldcg(q + j * 256);
+                                    y[4 * j] += w * z.x;
+                                    y[4 * j + 1] += w * z.y;
+                                    y[4 * j + 2] += w * z.z;
+                                    y[4 * j + 3] += w * z.w;
+                                }
+                            }
+                            store(y, inv, k * 32);
+                        }
+                        if (x == who) store_lse(mm, ll);
                     }
                 }
                 __syncwarp();
@@ -763,56 +816,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (warp == 8) tmem_dealloc(*tmem_slot, 512);
 }
 
-// Joins the partial results of the items that span CTAs.  CTA (i, y) serves 32 rows of the item whose first
-// piece is the last of attention CTA i.
-template <int D>
-__global__ void __launch_bounds__(256) join_kernel(AttendArgs a, int tpt, int n_cta) {
-    extern __shared__ int pre[];
-    using C = Cfg<D>;
-    const View &v = a.v;
-    const int total = build_line(v, tpt, pre), per = (total + n_cta - 1) / n_cta;
-    const int u1 = min(total, ((int)blockIdx.x + 1) * per), u0 = (int)blockIdx.x * per;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (u0 >= u1 || u1 >= total) return;
-    const Line c = seek(v, tpt, pre, u1 - 1);
-    const int i0 = u1 - 1 - c.unit, i1 = i0 + c.p.units;  // the item's tiles on the line
-    if (c.unit < 0 || i0 < u0 || i1 <= u1) return;  // only its charge is here, or it begins in an earlier CTA, or ends here
-    const int n_parts = (i1 - 1) / per - (int)blockIdx.x + 1;
-    const int r = blockIdx.y * 32 + (threadIdx.x & 31), x = r >> 7, row = r & 127;
-    const bool shared_rows = c.p.tok0 == c.p.n_tok;
-    const int tok = x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
-    if (row >= tok * v.G || (x == 1 && shared_rows)) return;
-    auto part = [&](int i) { return a.parts + ((size_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * C::PART; };
-    float mm = -INFINITY, ll = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, __ldcg(part(i) + 256 * D + r));
-    const float ref = mm == -INFINITY ? 0.0f : mm;
-    constexpr int CH = D / 4, PER = CH / 8;
-    float4 acc[PER];
-#pragma unroll
-    for (int k = 0; k < PER; k++) acc[k] = make_float4(0, 0, 0, 0);
-#pragma unroll 4
-    for (int i = 0; i < n_parts; i++) {
-        const float w = ex2(__ldcg(part(i) + 256 * D + r) - ref);
-        ll += w * __ldcg(part(i) + 256 * (D + 1) + r);
-#pragma unroll
-        for (int k = 0; k < PER; k++) {
-            const float4 y = __ldcg(reinterpret_cast<const float4 *>(part(i)) + ((threadIdx.x >> 5) * PER + k) * 256 + r);
-            acc[k].x += w * y.x;
-            acc[k].y += w * y.y;
-            acc[k].z += w * y.z;
-            acc[k].w += w * y.w;
-        }
-    }
-    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-    const size_t out_row = (size_t)c.q.s.row0 + c.p.ta + (x ? c.p.tok0 : 0) + row / v.G;
-    const int head = c.h * v.G + row % v.G;
-    uint2 *o = reinterpret_cast<uint2 *>((__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D) + (threadIdx.x >> 5) * PER;
-#pragma unroll
-    for (int k = 0; k < PER; k++) o[k] = make_uint2(pack2(acc[k].x * inv, acc[k].y * inv), pack2(acc[k].z * inv, acc[k].w * inv));
-    if (threadIdx.x < 32 && a.lse) a.lse[out_row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
-}
-
 template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
     using C = Cfg<D>;
     const int tpt = 128 / a.v.G;
@@ -821,19 +824,7 @@ template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)
     for (int i = 0; i < 8; i++)
         if (a.v.G == 1 << i) g_shift = i;
     kernel<<<num_sms, THREADS, C::SMEM, s>>>(maps[0], maps[1], maps[2], maps[3], a, tpt, g_shift, q_tma);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(num_sms, 8);
-    cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = (a.v.B + 1) * 4;
-    cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, join_kernel<D>, a, tpt, num_sms);
+    return cudaGetLastError();
 }
 
 }  // namespace
