@@ -49,8 +49,8 @@ template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
     static constexpr int STAGES = D == 128 ? 5 : 8;
     static constexpr int BARS = 2 * STAGES + 18;
-    static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maximum and sum of stream 1's rows
-    static constexpr int SMEM = ML_AT + 2 * 128 * 4;
+    static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maxima and sums of both streams' rows
+    static constexpr int SMEM = ML_AT + 4 * 128 * 4;
     static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 4, "the prefix sums of the largest batch fit the ring");
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
 };
@@ -332,7 +332,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const int per = (total + gridDim.x - 1) / gridDim.x;
+    // a piece of less than four tiles costs more in the join than its tiles (one window of 17 rows: 35 -> 28 us)
+    const int per = max(4, (total + (int)gridDim.x - 1) / (int)gridDim.x);
     const int u0 = min(total, (int)blockIdx.x * per), u1 = min(total, u0 + per);
     auto give_up = [&]() {
         *abort_flag = 1;
@@ -678,134 +679,145 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 }
                 // ---- the segment is done: store, or leave a partial result
                 if (m == -INFINITY) l = 0.0f;  // a row that saw nothing (the polynomial leaves a trace for masked slots)
-                if (!first) wait(o_done(x), n_o++);  // (first: no tile in this segment)
+                // Streams of their own rows store and join by themselves, streams that share rows together.
                 const bool whole = n == c.p.units;
-                float4 *part = reinterpret_cast<float4 *>(a.parts + ((size_t)blockIdx.x * 2 + (pt.first == 0 ? 1 : 0)) * C::PART);
-                const int t_row = token(row);
-                const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
-                const int head = c.h * v.G + row - t_row * v.G;
-                const bool both = shared_rows && n > 1;  // two streams of the same rows: stream 0 joins and stores
-                const uint32_t t_o1 = tmem + 256 + D + lanes;
+                const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
+                const int i0 = u - pt.line - unit, cta0 = i0 / per;  // the line's unit and the CTA where the item's tiles begin
+                const int n_parts = (i0 + c.p.units - 1) / per - cta0 + 1, mine = (int)blockIdx.x - cta0;
+                unsigned *counter = a.counters + 2 * cta0 + who;
+                volatile uint32_t *last = tmem_slot + 2 + who;  // every other part is in the workspace
+                const bool lead = row == 0 && x == who;
+                if (lead && !whole) *last = ld_acquire(counter) == (unsigned)n_parts - 1;
+                __syncwarp();
+                if (!first) wait(o_done(x), n_o++);  // (first: no tile in this segment)
                 float w0 = 1.0f, w1 = 0.0f;
-                if (both) {
-                    // warps w and w + 4 reach the same lanes of tensor memory
+                const bool both = shared_rows && n > 1;
+                if (shared_rows) {
+                    // warps w and w + 4 reach the same lanes of tensor memory: each stream stores half of the columns
                     volatile float *ml = reinterpret_cast<volatile float *>(smem + C::ML_AT);
-                    if (x == 1) {
-                        ml[row] = m;
-                        ml[128 + row] = l;
-                    }
+                    ml[x * 256 + row] = m;
+                    ml[x * 256 + 128 + row] = l;
                     tc_fence_before();
                     bar_sync(1, 256);
                     tc_fence_after();
-                    if (x == 0) {
-                        const float m1 = ml[row], l1 = ml[128 + row];
-                        const float mm = fmaxf(m, m1), ref = mm == -INFINITY ? 0.0f : mm;
-                        w0 = ex2(m - ref);
-                        w1 = ex2(m1 - ref);
-                        l = l * w0 + l1 * w1;
-                        m = mm;
-                    }
+                    const float m0 = ml[row], l0 = ml[128 + row], m1 = ml[256 + row], l1 = ml[384 + row];
+                    const float mm = fmaxf(m0, m1), ref = mm == -INFINITY ? 0.0f : mm;
+                    w0 = ex2(m0 - ref);
+                    w1 = ex2(m1 - ref);
+                    l = l0 * w0 + l1 * w1;
+                    m = mm;
+                } else if (!whole) {
+                    bar_sync(id, threads);
                 }
-                __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
-                auto store = [&](const float (&y)[32], float inv, int at) {  // 32 elements of this row
-                    uint32_t w[16];
+                const uint32_t t_o0 = tmem + 256 + who * D + lanes, t_o1 = tmem + 256 + D + lanes;
+                const int k0 = shared_rows ? x * (D / 64) : 0, k1 = wq * 32 >= n_rows ? k0 : k0 + (shared_rows ? D / 64 : D / 32);
+                auto load_o = [&](int k, float (&y)[32]) {  // 32 columns of this CTA's result
+                    __syncwarp();
+                    tmem_ld32(t_o0 + k * 32, y);
+                    if (both) {
+                        float o1[32];
+                        tmem_ld32(t_o1 + k * 32, o1);
 #pragma unroll
-                    for (int i = 0; i < 16; i++) w[i] = pack2(y[2 * i] * inv, y[2 * i + 1] * inv);
-                    if (wide_out) {
-#pragma unroll
-                        for (int i = 0; i < 16; i += 8)
-                            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o + at + 2 * i), I8(w, i) : "memory");
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(o + at + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+                        for (int i = 0; i < 32; i++) y[i] = y[i] * w0 + o1[i] * w1;
                     }
                 };
-                auto store_lse = [&](float m, float l) {
-                    if (a.lse) a.lse[out_row * v.Hq + head] = l > 0.0f ? (m + log2f(l)) * LN2 : -INFINITY;
-                };
-                if (!shared_rows || x == 0) {
-                    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                auto part_of_cta = [&](int i) { return a.parts + ((size_t)(cta0 + i) * 2 + (i == 0 ? 1 : 0)) * C::PART; };
+                const int at = who * 128 + row;
+                bool store = whole || *last;
+                if (!store) {
+                    float *part = part_of_cta(mine);
 #pragma unroll 1
-                    for (int k = 0; k < D / 32; k++) {  // not unrolled: code that runs once per item mostly costs its way into the cache
-                        float ov[32];
-                        __syncwarp();  // (the stores below leave lanes without a row behind)
-                        tmem_ld32(t_o + k * 32, ov);
-                        if (both) {
-                            float o1[32];
-                            tmem_ld32(t_o1 + k * 32, o1);
+                    for (int k = k0; k < k1; k++) {  // not unrolled: code that runs once per item mostly costs its way into the cache
+                        float y[32];
+                        load_o(k, y);
+                        if (row < n_rows) {
 #pragma unroll
-                            for (int i = 0; i < 32; i++) ov[i] = ov[i] * w0 + o1[i] * w1;
+                            for (int i = 0; i < 8; i++)
+                                reinterpret_cast<float4 *>(part)[(k * 8 + i) * 256 + at] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                        }
+                    }
+                    if (x == who && row < n_rows) {
+                        part[256 * D + at] = m;
+                        part[256 * (D + 1) + at] = l;
+                    }
+                    __syncwarp();
+                    bar_sync(id, threads);
+                    if (lead) {
+                        __threadfence();
+                        *last = atomicAdd(counter, 1u) == (unsigned)n_parts - 1;
+                        __threadfence();
+                    }
+                    __syncwarp();
+                    bar_sync(id, threads);
+                    store = *last;
+                }
+                if (store) {
+                    float mm = m, ll = l, w_mine = 1.0f, ref = 0.0f;
+                    if (!whole && row < n_rows) {
+                        for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, i == mine ? m : __ldcg(part_of_cta(i) + 256 * D + at));
+                        ref = mm == -INFINITY ? 0.0f : mm;
+                        w_mine = ex2(m - ref);
+                        ll = 0.0f;
+#pragma unroll 4
+                        for (int i = 0; i < n_parts; i++)
+                            ll += i == mine ? w_mine * l : ex2(__ldcg(part_of_cta(i) + 256 * D + at) - ref) * __ldcg(part_of_cta(i) + 256 * (D + 1) + at);
+                    }
+                    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+                    const int t_row = token(row);
+                    const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
+                    const int head = c.h * v.G + row - t_row * v.G;
+                    __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
+#pragma unroll 1
+                    for (int k = k0; k < k1; k++) {
+                        float y[32];
+                        if (whole) {
+                            load_o(k, y);
+                        } else {
+                            // in the order of the CTAs, whichever came last
+                            auto add = [&](int from, int to) {
+#pragma unroll 2
+                                for (int i = from; i < to; i++) {
+                                    const float w = ex2(__ldcg(part_of_cta(i) + 256 * D + at) - ref);
+                                    const float4 *z = reinterpret_cast<const float4 *>(part_of_cta(i)) + k * 8 * 256 + at;
+#pragma unroll
+                                    for (int j = 0; j < 8; j++) {
+                                        const float4 f = __ldcg(z + j * 256);
+                                        y[4 * j] += w * f.x;
+                                        y[4 * j + 1] += w * f.y;
+                                        y[4 * j + 2] += w * f.z;
+                                        y[4 * j + 3] += w * f.w;
+                                    }
+                                }
+                            };
+#pragma unroll
+                            for (int i = 0; i < 32; i++) y[i] = 0.0f;
+                            if (row < n_rows) add(0, mine);
+                            float own[32];
+                            load_o(k, own);
+#pragma unroll
+                            for (int i = 0; i < 32; i++) y[i] += w_mine * own[i];
+                            if (row < n_rows) add(mine + 1, n_parts);
                         }
                         if (row < n_rows) {
-                            if (whole) {
-                                store(ov, inv, k * 32);
+                            uint32_t w[16];
+#pragma unroll
+                            for (int i = 0; i < 16; i++) w[i] = pack2(y[2 * i] * inv, y[2 * i + 1] * inv);
+                            if (wide_out) {
+#pragma unroll
+                                for (int i = 0; i < 16; i += 8)
+                                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(o + k * 32 + 2 * i), I8(w, i) : "memory");
                             } else {
 #pragma unroll
-                                for (int i = 0; i < 8; i++)
-                                    part[(k * 8 + i) * 256 + x * 128 + row] = make_float4(ov[4 * i], ov[4 * i + 1], ov[4 * i + 2], ov[4 * i + 3]);
+                                for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(o + k * 32 + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
                             }
                         }
                     }
-                    if (row < n_rows) {
-                        if (whole) {
-                            store_lse(m, l);
-                        } else {
-                            float *pm = reinterpret_cast<float *>(part) + 256 * D + x * 128 + row;
-                            pm[0] = m;
-                            pm[256] = l;
-                        }
-                    }
-                }
-                if (!whole) {
-                    // streams of their own rows arrive and join by themselves, streams that share rows together
-                    const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
-                    const int i0 = u - pt.line - unit, cta0 = i0 / per, n_parts = (i0 + c.p.units - 1) / per - cta0 + 1;
-                    volatile uint32_t *last = tmem_slot + 2 + who;
-                    __threadfence();
-                    __syncwarp();
-                    bar_sync(id, threads);
-                    if (row == 0 && x == who) {
-                        const bool all = atomicAdd(a.counters + 2 * cta0 + who, 1u) == (unsigned)n_parts - 1;
-                        if (all) a.counters[2 * cta0 + who] = 0u;
-                        *last = all;
-                    }
-                    __syncwarp();
-                    bar_sync(id, threads);
-                    if (*last && row < n_rows) {
-                        __threadfence();
-                        auto part_at = [&](int i) { return a.parts + ((size_t)(cta0 + i) * 2 + (i == 0 ? 1 : 0)) * C::PART + who * 128 + row; };
-                        float mm = -INFINITY, ll = 0.0f;
-#pragma unroll 8
-                        for (int i = 0; i < n_parts; i++) mm = fmaxf(mm, __ldcg(part_at(i) + 256 * D));
-                        const float ref = mm == -INFINITY ? 0.0f : mm;
-#pragma unroll 8
-                        for (int i = 0; i < n_parts; i++) ll += ex2(__ldcg(part_at(i) + 256 * D) - ref) * __ldcg(part_at(i) + 256 * (D + 1));
-                        const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-                        const int k1 = shared_rows ? (x + 1) * (D / 64) : D / 32;
-#pragma unroll 1
-                        for (int k = shared_rows ? x * (D / 64) : 0; k < k1; k++) {
-                            float y[32] = {};
-#pragma unroll 2
-                            for (int i = 0; i < n_parts; i++) {
-                                const float w = ex2(__ldcg(part_at(i) + 256 * D) - ref);
-                                const float4 *q = reinterpret_cast<const float4 *>(part_at(i) - (who * 128 + row)) + k * 8 * 256 + who * 128 + row;
-#pragma unroll
-                                for (int j = 0; j < 8; j++) {
-                                    const float4 z = __ldcg(q + j * 256);
-                                    y[4 * j] += w * z.x;
-                                    y[4 * j + 1] += w * z.y;
-                                    y[4 * j + 2] += w * z.z;
-                                    y[4 * j + 3] += w * z.w;
-                                }
-                            }
-                            store(y, inv, k * 32);
-                        }
-                        if (x == who) store_lse(mm, ll);
-                    }
+                    if (x == who && row < n_rows && a.lse) a.lse[out_row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+                    if (lead && !whole) *counter = 0;
                 }
                 __syncwarp();
                 tc_fence_before();
-                if (both) bar_sync(1, 256);  // stream 1's tensor memory is read
+                if (shared_rows || !whole) bar_sync(id, threads);  // both streams' tensor memory and the flag are read
                 g += 2 * n;
             }
         }
