@@ -598,16 +598,20 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
                 bool first = true;
-                // slots that nobody sees may hold anything: their values are cleared before the product
-                auto clear_hidden = [&](int t, int j0) {
-                    if (c.q.s.L - j0 >= TILE && (j0 >= c.p.first || c.p.first <= v.sinks)) return;
+                // slots that nobody sees may hold anything: the values of a half's are cleared before its product, after its
+                // softmax, because the values arrive one tile behind the keys (before it: 4 us more per item)
+                auto clear_hidden = [&](int t, int j0, int hf) {
+                    const int jh = j0 + hf * 64;
+                    if (c.q.s.L - jh >= 64 && (jh >= c.p.first || jh + 64 <= v.sinks || c.p.first <= v.sinks)) return;
                     const uint32_t at = g + pos_v(t, n), s = at % NS;
                     wait(full(s), at / NS);
-                    const int j = j0 + row;
+                    const int r = hf * 64 + (row & 63), j = j0 + r;
                     if (j >= c.q.s.L || (j < c.p.first && j >= v.sinks)) {
+                        // half a row per thread; neighbouring rows begin at different 16 bytes, so they meet on no bank
 #pragma unroll 1
-                        for (int i = 0; i < 8 * HALVES; i++)
-                            *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + (i >> 3) * 16384 + row * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
+                        for (int i = 0; i < 4 * HALVES; i++)
+                            *reinterpret_cast<uint4 *>(smem + (2 + s) * C::TILE_BYTES + (HALVES == 2 ? (row >> 6) * 16384 : 0) + r * 128 +
+                                                       (HALVES == 2 ? (i + r) & 7 : ((row >> 6) * 4 + ((i + r) & 3))) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     fence_async_shared();
                     __syncwarp();
@@ -618,9 +622,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
                     for (int hf = 0; hf < 2; hf++, n_h++) {
                         wait(s_full(x, hf), n_h >> 1);
-                        if (hf == 0) clear_hidden(t, j0);
                         if (wq * 32 >= n_rows) {  // a warp without a row: zero queries have left zeros where its weights go
                             first = false;
+                            clear_hidden(t, j0, hf);
                             mbar_arrive(p_ready(x, hf));
                             continue;
                         }
@@ -672,6 +676,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         tmem_st32(t_s + hf * 64, pw);
                         const uint64_t sum = add2(sum2[0], sum2[1]);
                         l += lo(sum) + hi(sum);
+                        clear_hidden(t, j0, hf);
                         tmem_st_wait();
                         tc_fence_before();
                         mbar_arrive(p_ready(x, hf));
