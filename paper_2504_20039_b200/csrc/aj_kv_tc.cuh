@@ -1,5 +1,5 @@
 // Small pieces that the tcgen05 kernels of the key-value cache share: an elected lane, barriers of part of a CTA, the
-// fence between ordinary and asynchronous accesses to shared memory, paired f32 arithmetic.
+// fence between ordinary and asynchronous accesses to shared memory, paired f32 arithmetic, a wide read of tensor memory.
 #pragma once
 
 #include <stdint.h>
@@ -48,6 +48,19 @@ __device__ inline unsigned ld_acquire(const unsigned *p) {
     return v;
 }
 __device__ inline void bar_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
+#define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+// 64 columns of this thread's lane of tensor memory
+__device__ inline void tmem_ld64(uint32_t addr, uint32_t (&r)[64]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24), R8(r, 32), R8(r, 40), R8(r, 48), R8(r, 56)
+        : "r"(addr)
+        : "memory");
+}
 
 }  // namespace kv
 }  // namespace aj

@@ -250,6 +250,7 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
             // ---------------------------------------------------------------- queries, and the columns' sums
             const int x = warp >> 2, row = threadIdx.x & 127;
             const uint32_t t_acc = tmem + x * ROWS + ((uint32_t)((warp & 3) * 32) << 16);
+            const uint64_t scale2 = f2(a.scale_log2, a.scale_log2);
             uint32_t g = 0;
             bool dead = false;
             for (Seg c = first_seg(); c.n > 0; next_seg(c)) {
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
                         const size_t at = ((size_t)c.b * v.Hkv + c.h) * v.cap + j;
                         const float *w_from = ch == 0 ? a.weight : a.weight_out;
                         const float before = j < c.s.L ? w_from[at] : 0.0f;
-                        float sum[4] = {0, 0, 0, 0};
+                        uint64_t sum[2] = {0, 0};
                         if (on) {
                             if (!dead && !__all_sync(~0u, mbar_wait(acc_full(x), (g >> 1) & 1u, abort_flag))) {
                                 give_up();
@@ -301,33 +302,39 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
                             tc_fence_after();
                             // does every row of the chunk see every slot of the block?
                             const bool masked = p0 + r0 / v.G < j0 + BLK - 1 || (v.window && j0 <= p0 + (r0 + rows - 1) / v.G - v.window);
-                            for (int c0 = 0; c0 < rows; c0 += 32) {
-                                float sc[32];
-                                tmem_ld32(t_acc + c0, sc);
-                                if (c0 + 32 > rows) {  // columns that no product wrote
+                            auto use = [&](uint32_t (&sc)[64], int c0) {
 #pragma unroll
-                                    for (int i = 0; i < 32; i++)
-                                        if (c0 + i >= rows) sc[i] = 0.0f;
-                                }
-                                if (masked) {
+                                for (int q = 0; q < 64; q += 16) {
+                                    if (c0 + q >= rows) break;
+                                    if (c0 + q + 16 > rows) {  // columns that no product wrote
 #pragma unroll
-                                    for (int i = 0; i < 32; i++)
-                                        if (!sees(v, row_slot[(c0 + i) & (ROWS - 1)], j)) sc[i] = -INFINITY;
-                                }
+                                        for (int i = q; i < q + 16; i++)
+                                            if (c0 + i >= rows) sc[i] = 0u;
+                                    }
+                                    if (masked) {
 #pragma unroll
-                                for (int i = 0; i < 32; i += 4) {
-                                    const float4 n4 = *reinterpret_cast<const float4 *>(neg + c0 + i);
-                                    sum[0] += ex2(fmaf(sc[i], a.scale_log2, n4.x));
-                                    sum[1] += ex2(fmaf(sc[i + 1], a.scale_log2, n4.y));
-                                    sum[2] += ex2(fmaf(sc[i + 2], a.scale_log2, n4.z));
-                                    sum[3] += ex2(fmaf(sc[i + 3], a.scale_log2, n4.w));
+                                        for (int i = q; i < q + 16; i++)
+                                            if (!sees(v, row_slot[(c0 + i) & (ROWS - 1)], j)) sc[i] = 0xff800000u;
+                                    }
+#pragma unroll
+                                    for (int i = q; i < q + 16; i += 4) {
+                                        const ulonglong2 n4 = *reinterpret_cast<const ulonglong2 *>(neg + c0 + i);
+                                        const uint64_t y0 = fma2(f2(__uint_as_float(sc[i]), __uint_as_float(sc[i + 1])), scale2, n4.x), y1 = fma2(f2(__uint_as_float(sc[i + 2]), __uint_as_float(sc[i + 3])), scale2, n4.y);
+                                        sum[0] = add2(sum[0], f2(ex2(lo(y0)), ex2(hi(y0))));
+                                        sum[1] = add2(sum[1], f2(ex2(lo(y1)), ex2(hi(y1))));
+                                    }
                                 }
+                            };
+                            for (int c0 = 0; c0 < rows; c0 += 64) {
+                                uint32_t sc[64];
+                                tmem_ld64(t_acc + c0, sc);
+                                use(sc, c0);
                             }
                             tc_fence_before();
                             mbar_arrive(acc_empty(x));
                             g++;
                         }
-                        if (j < c.s.L) a.weight_out[at] = before + ((sum[0] + sum[1]) + (sum[2] + sum[3]));
+                        if (j < c.s.L) a.weight_out[at] = before + ((lo(sum[0]) + lo(sum[1])) + (hi(sum[0]) + hi(sum[1])));
                     }
                 }
             }
