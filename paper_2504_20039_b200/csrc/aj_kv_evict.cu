@@ -30,7 +30,7 @@ constexpr int MAX_CLUSTER = 8;
 struct Shared {
     unsigned hist[DIGITS][BINS];
     unsigned scan[33], scan2[33];
-    int newest, need;
+    int newest, need, ties;
     unsigned prefix, eq, holes, movers;
 };
 
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int part = blockIdx.x % n_split, item = blockIdx.x / n_split;
     const int h = item % v.Hkv, b = item / v.Hkv;
-    const int L = min(max(__ldg(v.lens + b), 0), v.cap), keep = a.keep;
+    const int L = min(max(*(const volatile int *)(v.lens + b), 0), v.cap), keep = a.keep;
     const size_t at = (size_t)item * v.cap;
     const float *w_in = a.weight + at;
     const int *p_in = a.slot_pos + at;
@@ -86,15 +86,18 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
         sh.need = keep;
     }
     __syncthreads();
-    // The new length is written once every CTA of this sequence has read the old one (they may be one array).
+    // The new length is written once every CTA of this sequence has read the old one (they may be one array).  The count goes
+    // out as soon as this CTA has, and comes back while the rows move (counted at the end: 2 us more).
+    const unsigned last = (unsigned)v.Hkv * n_split - 1;
+    unsigned others = 0;
+    auto count_in = [&]() {
+        if (threadIdx.x == 0) asm volatile("atom.acq_rel.gpu.global.inc.u32 %0, [%1], %2;" : "=r"(others) : "l"(counters + b), "r"(last) : "memory");
+    };
     auto leave = [&]() {
-        if (threadIdx.x == 0) {
-            const unsigned total = (unsigned)v.Hkv * n_split;
-            __threadfence();
-            if (atomicInc(counters + b, total - 1) == total - 1) a.lens_out[b] = min(L, keep);
-        }
+        if (threadIdx.x == 0 && others == last) a.lens_out[b] = min(L, keep);
     };
     if (L <= keep) {  // the same for the whole cluster
+        count_in();
         for (int j = part * THREADS + threadIdx.x; j < L; j += n_split * THREADS) {
             if (a.weight_out != a.weight) a.weight_out[at + j] = w_in[j];
             if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = p_in[j];
@@ -178,10 +181,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
         if (before < want && want <= before + mine) {
             sh.prefix = prefix | ((unsigned)d << shift);
             sh.need = (int)(want - before);
+            sh.ties = mine != want - before;
         }
         __syncthreads();
+        if (!sh.ties) break;  // the digit's slots all stay: the lower digits decide nothing (mostly after the third)
     }
     const unsigned thr = sh.prefix, need = (unsigned)sh.need;
+    const bool ties = sh.ties;  // more slots than places have the threshold itself as their key
 
     // what the CTAs before this one, and all of them, hold of a counter
     auto across = [&](const unsigned *p, unsigned &all) {
@@ -197,22 +203,24 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
         const int j = w * 32 + lane;
         const unsigned k = j < L ? key_at(j) : 0u;
         const unsigned gt = __ballot_sync(~0u, j < L && k > thr), e = __ballot_sync(~0u, j < L && k == thr);
-        if (lane == 0) kept[w - w_lo] = gt;
+        if (lane == 0) kept[w - w_lo] = ties ? gt : gt | e;
         eq += __popc(e);
     }
-    scan_warps<NWARP>(sh.scan, eq);
-    if (threadIdx.x == 0) sh.eq = sh.scan[NWARP];
-    cluster_sync();
-    unsigned all;
-    unsigned rank = across(&sh.eq, all) + sh.scan[warp];
-    for (int w = w0; w < w1 && rank < need; w++) {
-        const int j = w * 32 + lane;
-        const unsigned k = j < L ? key_at(j) : 0u;
-        const unsigned e = __ballot_sync(~0u, j < L && k == thr);
-        const bool mine = (e >> lane & 1) && rank + __popc(e & ((1u << lane) - 1)) < need;
-        const unsigned add = __ballot_sync(~0u, mine);
-        if (lane == 0) kept[w - w_lo] |= add;
-        rank += __popc(e);
+    if (ties) {
+        scan_warps<NWARP>(sh.scan, eq);
+        if (threadIdx.x == 0) sh.eq = sh.scan[NWARP];
+        cluster_sync();
+        unsigned all;
+        unsigned rank = across(&sh.eq, all) + sh.scan[warp];
+        for (int w = w0; w < w1 && rank < need; w++) {
+            const int j = w * 32 + lane;
+            const unsigned k = j < L ? key_at(j) : 0u;
+            const unsigned e = __ballot_sync(~0u, j < L && k == thr);
+            const bool mine = (e >> lane & 1) && rank + __popc(e & ((1u << lane) - 1)) < need;
+            const unsigned add = __ballot_sync(~0u, mine);
+            if (lane == 0) kept[w - w_lo] |= add;
+            rank += __popc(e);
+        }
     }
     __syncthreads();
 
@@ -238,6 +246,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     cluster_sync();
     unsigned n_moves;  // as many holes as movers
     const unsigned hole0 = across(&sh.holes, n_moves) + sh.scan[warp], mover0 = across(&sh.movers, n_moves) + sh.scan2[warp];
+    count_in();
     const int share = min(list_len, (int)(n_moves + n_split - 1) / n_split);  // moves a CTA makes at a time
 
     const int n16 = v.D * a.elem / 16;  // 16-byte pieces of a row
