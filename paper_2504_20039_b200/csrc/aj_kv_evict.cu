@@ -65,8 +65,9 @@ __device__ inline unsigned ld_cluster(const void *p, int rank) {
     return x;
 }
 
-template <int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int list_len) {
+// AHEAD: 16-byte pieces of K and of V that a thread has in flight while rows move; eight where the CTA has an SM to itself.
+template <int THREADS, int AHEAD>
+__global__ void __launch_bounds__(THREADS, AHEAD == 4 ? 1024 / THREADS : 1) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int list_len) {
     constexpr int NWARP = THREADS / 32;
     extern __shared__ __align__(16) unsigned dyn[];
     __shared__ Shared sh;
@@ -250,13 +251,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     const int share = min(list_len, (int)(n_moves + n_split - 1) / n_split);  // moves a CTA makes at a time
 
     const int n16 = v.D * a.elem / 16;  // 16-byte pieces of a row
+    const float per_share = 1.0f / (float)share;  // ranks stay below 8 * 4096: the quotient of r + 1/2 never rounds up to the next
     for (int c0 = 0; c0 < (int)n_moves; c0 += share * n_split) {
         // ranks c0 + k * share .. go to CTA k of the cluster
         unsigned hr = hole0, mr = mover0;
         auto put = [&](unsigned bits, unsigned &r0, int slot, unsigned *to) {  // one slot per lane
             const int r = (int)(r0 + __popc(bits & ((1u << lane) - 1))) - c0;
             if ((bits >> lane & 1) && r >= 0 && r < share * n_split) {
-                const int k = r / share;
+                const int k = (int)(((float)r + 0.5f) * per_share);
                 if (n_split == 1) to[r] = slot;
                 else st_shared_cluster_u32(map_to_cta(smem_u32(to + (r - k * share)), k), (unsigned)slot);
             }
@@ -283,7 +285,6 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
         }
         __syncthreads();
         const int pieces = count * n16;
-        constexpr int AHEAD = 4;  // loads before the first store
         for (int i0 = threadIdx.x; i0 < pieces; i0 += AHEAD * THREADS) {
             uint4 x[AHEAD], y[AHEAD];
             size_t to[AHEAD];
@@ -309,10 +310,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     }
     // slots that stay where they are
     if (a.weight_out != a.weight || a.slot_pos_out != a.slot_pos) {
-        for (int j = j_lo + threadIdx.x; j < min(j_hi, keep); j += THREADS) {
-            if (kept[(j >> 5) - w_lo] >> (j & 31) & 1) {
-                if (a.weight_out != a.weight) a.weight_out[at + j] = __ldcg(w_in + j);
-                if (a.slot_pos_out != a.slot_pos) a.slot_pos_out[at + j] = __ldcg(p_in + j);
+        const int end = min(j_hi, keep);
+        for (int j0 = j_lo + threadIdx.x; j0 < end; j0 += 4 * THREADS) {
+            float w[4];
+            int p[4];
+            bool on[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int j = j0 + u * THREADS;
+                on[u] = j < end && (kept[(j >> 5) - w_lo] >> (j & 31) & 1);
+                if (on[u]) w[u] = __ldcg(w_in + j), p[u] = __ldcg(p_in + j);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const size_t to = at + j0 + u * THREADS;
+                if (on[u] && a.weight_out != a.weight) a.weight_out[to] = w[u];
+                if (on[u] && a.slot_pos_out != a.slot_pos) a.slot_pos_out[to] = p[u];
             }
         }
     }
@@ -324,8 +337,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
 
 // clusters[i]: how many clusters of 2^i CTAs of 1024 threads the device holds at once (a cluster stays within one GPC).
 cudaError_t prepare_evict(int (&clusters)[4]) {
-    cudaError_t e = allow_shared(evict_kernel<512>);
-    if (e == cudaSuccess) e = allow_shared(evict_kernel<1024>);
+    cudaError_t e = allow_shared(evict_kernel<512, 4>);
+    if (e == cudaSuccess) e = allow_shared(evict_kernel<512, 8>);
+    if (e == cudaSuccess) e = allow_shared(evict_kernel<1024, 4>);
     for (int i = 0; i < 4 && e == cudaSuccess; i++) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(1 << i);
@@ -337,7 +351,7 @@ cudaError_t prepare_evict(int (&clusters)[4]) {
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        e = cudaOccupancyMaxActiveClusters(&clusters[i], evict_kernel<1024>, &cfg);
+        e = cudaOccupancyMaxActiveClusters(&clusters[i], evict_kernel<1024, 4>, &cfg);
     }
     return e;
 }
@@ -360,7 +374,7 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clu
     // Half the threads where there is little to do for each, so that barriers are cheaper, and where there are more CTAs than
     // SMs: two then share an SM, and one's barriers hide behind the other.
     const bool half = smem <= 80 * 1024 && (items * n_split > num_sms || cap <= 2048);
-    auto kernel = half ? evict_kernel<512> : evict_kernel<1024>;
+    auto kernel = !half ? evict_kernel<1024, 4> : items * n_split > num_sms ? evict_kernel<512, 4> : evict_kernel<512, 8>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(items * n_split);
     cfg.blockDim = dim3(half ? 512 : 1024);
