@@ -77,6 +77,9 @@ aj_status aj_kv_append(aj_kv h, const void *q, long long q_stride, const void *k
  * tensor cores the weights exp(s - max) are rounded to bf16 before they meet V.  Keys that a row does not see never
  * reach it whatever they hold; a non-finite VALUE in a slot that other rows of the call see may reach it.
  * Two runs on the same inputs give the same bits.
+ * More than 16 rows (new tokens x query heads per key head) go to the tensor cores only where k_pages and v_pages start on
+ * 128 bytes, as an allocation does, and Hq / Hkv <= 128; else the CUDA cores take them, many times slower.  Rows of q on 128
+ * bytes (pointer and stride) are loaded fastest.
  */
 aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k_pages, const void *v_pages, int n_pages,
                        const int32_t *block_table, int table_width, const int32_t *seq_lens, const int32_t *q_start,

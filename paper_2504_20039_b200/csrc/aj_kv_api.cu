@@ -303,10 +303,12 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
         h->last_path = "few";
         return done(kv::launch_attend_few(a, h->num_sms, (cudaStream_t)cuda_stream));
     }
-    if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows)
+    if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows; else the CUDA cores)
         h->last_path = "umma";
         CUtensorMap maps[4];
         if (!at_address(h, &maps[0], h->pages, k_pages) || !at_address(h, &maps[1], h->pages, v_pages)) return AJ_ERR_CUDA;
+        // queries by TMA (boxes of eight tokens where a tile has as many, and of one), or by one warp's 16-byte copies where their
+        // rows do not lie on 128 bytes: 64 windows of 33 rows 157 us and 209, a prompt of 8192 490 and 647
         const int q_tma = !on128(q, q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
         if (q_tma && q_stride != h->q_stride) {
             h->q_stride = -1;

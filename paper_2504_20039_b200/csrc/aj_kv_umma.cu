@@ -9,19 +9,28 @@
 // both streams the same rows and every other tile of 128 slots, so that in either case one stream's softmax runs
 // under the other's matrix products.  Tensor memory: S0 S1 (128 columns each), O0 O1 (D columns each).
 //
-//   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); load the stream's queries, store results
-//   warps 8, 10     issue tcgen05.mma for stream 0 and 1: PV of a tile, then QK^T of the stream's next
-//   warp 9          (warp 11 only completes its warpgroup) TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles,
-//                   in the order K0 K1 V0 K2 V1 ... in which they are consumed
+//   warps 0-3, 4-7  softmax of stream 0 and 1 (thread = row = TMEM lane); they store the results
+//   warps 8, 10     issue tcgen05.mma for stream 0 and 1: PV of half a tile, then QK^T of that half of the stream's next tile
+//   warp 9          TMA: 64-column x page-row boxes (128-byte swizzle) of the pages into a ring of K and V tiles, in the
+//                   order K0 K1 V0 K2 V1 ... in which they are consumed
+//   warp 11         the queries of both streams, by TMA where they lie on 128 bytes, else by 16-byte copies
+//
+// Scores go to the softmax in halves of 64 slots with barriers of their own: while one half is in the softmax, the other
+// half's products run.
 //
 // The tiles of all (sequence, key head, row piece) items of the batch form one line, cut into equal pieces, one per
 // CTA: causal prompts and ragged caches are balanced alike.  Items that span CTAs leave unnormalised partial results
 // (f32) in the workspace, and the CTA that arrives last joins them, in the order of the CTAs (a second kernel for that cost 11
 // to 16 us a call, most of it in finding its place on the line).
 //
-// What bounds it: a window of K + 1 rows reads 512 bytes of K and V per slot and head and is bound by HBM up to about
-// 256 rows; a prompt is bound by the exponentials (16 per clock and SM: 2048 cycles per two tiles of 128 x 128)
-// together with the tensor pipe (2048 cycles for their four products).
+// What bounds it, and what it measured (8 key heads, 32 query heads):
+//   windows of 33 rows, 64 sequences of 129 .. 4100 slots, D = 128: the stream of pages, 152 us, 4.0 TB/s; 6 us go by
+//   before the first scores, 3 us between two items, 5 us in the last join
+//   a prompt of 8192, D = 128: the exponentials (16 per clock and SM: 2048 cycles for two tiles of 128 x 128, a quarter
+//   of them on the multiply-add pipe) beside 2048 cycles of the tensor pipe for their four products; 484 us alone,
+//   1.13 PFLOP/s; back to back the card's power limit lowers the clock
+//   four prompts with a window of 1024, D = 64: half the products for as many exponentials, and ten tiles an item, two of
+//   them partly masked; 173 us
 //
 // The running maximum is a reference that is raised only when a score exceeds it by more than RAISE, so the rescaling of
 // O (a round trip through tensor memory) is rare; weights far above 1 are as exact as weights up to 1 (raised from 8 on: 192 us

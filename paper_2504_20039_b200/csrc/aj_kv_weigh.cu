@@ -11,6 +11,9 @@
 // The (sequence, key head, 128-slot block) triples of the batch form one line, measured in cost (4 for the loads of a
 // block + 1 for each group of 8 rows), and every CTA takes an equal piece of it; two CTAs per SM.
 //
+// Measured: 64 sequences of up to 4096 slots, 8 key heads of 128, 4 rows: 62 us for 306 MB back to back, 4.9 TB/s.  What
+// is missing to a copy is the begin and end of a call of this length and the state's 4-byte reads and writes.
+//
 // The order of the head's elements within a product is free, so a lane takes 16 consecutive bytes of a row where the
 // fragment layout asks for 4 x 4 bytes: both operands use the same order, and every load is 16 bytes.  The queries come
 // straight from L1 / L2, one group of rows ahead.
