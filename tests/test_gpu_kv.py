@@ -130,6 +130,22 @@ def test_attend_joins_many_calls_on_one_handle(n):
         s.check_attend(out, lse, 0, 0, rounded_weights=True)
 
 
+@pytest.mark.parametrize("n,D,window", [(17, 128, 0), (33, 128, 0), (65, 128, 0), (65, 64, 0), (17, 64, 2500), (65, 128, 4000)])
+def test_attend_joins_many_parts(n, D, window):
+    """One key head and a long cache: an item spans many CTAs, in streams that share the rows (17 x 4) and in streams of
+    their own (33 x 4, 65 x 4).  Whichever CTA arrives last, the parts are joined in one order: the same bits every time."""
+    import torch
+
+    s = Setup(n + D, [5000, n, 0, 2063], [n] * 4, 4, 1, D, 64, ragged=False)
+    h = s.handle()
+    out, lse = _attend(s, h, window, 4 if window else 0)
+    assert h.last_path() == "umma" and h.last_launch_count() == 1
+    for _ in range(20):
+        again, lse2 = _attend(s, h, window, 4 if window else 0)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+    s.check_attend(out, lse, window, 4 if window else 0, rounded_weights=True)
+
+
 WEIGH = [
     # name, lens, nq, counted rows, Hq, Hkv, D, page, dtype, window, sinks
     ("one_token", [37, 300, 0], [1, 1, 1], None, 8, 2, 128, 16, "bf16", 0, 0),
