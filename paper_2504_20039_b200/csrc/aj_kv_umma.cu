@@ -57,7 +57,7 @@ constexpr uint32_t B_MN_MAJOR = 1u << 16;
 template <int D> struct Cfg {
     static constexpr int TILE_BYTES = TILE * D * 2;            // a K or V tile, and a query tile
     static constexpr int STAGES = D == 128 ? 5 : 8;
-    static constexpr int BARS = 2 * STAGES + 18;
+    static constexpr int BARS = 2 * STAGES + 24;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maxima and sums of both streams' rows
     static constexpr int SMEM = ML_AT + 4 * 128 * 4;
     static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 4, "the prefix sums of the largest batch fit the ring");
@@ -294,11 +294,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto empty = [&](int s) { return bars + 8u * (NS + s); };
     auto s_full = [&](int x, int hf) { return bars + 8u * (2 * NS + 2 * x + hf); };
     auto p_ready = [&](int x, int hf) { return bars + 8u * (2 * NS + 4 + 2 * x + hf); };
-    auto pv_done = [&](int x) { return bars + 8u * (2 * NS + 8 + x); };
-    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 10 + x); };
-    auto drained = [&](int x) { return bars + 8u * (2 * NS + 12 + x); };
-    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 14 + x); };
-    auto q_free = [&](int x) { return bars + 8u * (2 * NS + 16 + x); };
+    auto pv_done = [&](int x, uint32_t half) { return bars + 8u * (2 * NS + 8 + 4 * x + (half & 3u)); };
+    auto q_ready = [&](int x) { return bars + 8u * (2 * NS + 16 + x); };
+    auto drained = [&](int x) { return bars + 8u * (2 * NS + 18 + x); };
+    auto o_done = [&](int x) { return bars + 8u * (2 * NS + 20 + x); };
+    auto q_free = [&](int x) { return bars + 8u * (2 * NS + 22 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
     int *pre = reinterpret_cast<int *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
@@ -315,7 +315,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 mbar_init(s_full(x, hf), 1);
                 mbar_init(p_ready(x, hf), 128);
             }
-            mbar_init(pv_done(x), 1);
+            for (uint32_t i = 0; i < 4; i++) mbar_init(pv_done(x, i), 1);
             mbar_init(q_ready(x), 1);
             mbar_init(q_free(x), 1);
             mbar_init(drained(x), 1);
@@ -503,21 +503,27 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     if (elect_one()) issue_qk(t, hf);
                     __syncwarp();
                 };
-                // P V of one half of tile t, and right behind it the scores of the stream's next tile into the same columns
+                // P V of one half of tile t, and right behind it the scores of the stream's next tile into the same columns.
+                // The softmax waits for a product by a one-bit phase when it raises its reference, so it must know that the phase
+                // before has passed.  Four barriers take turns over the halves, and this warp sees the product of two halves ago done
+                // (long since: its scores have been through the softmax) before it issues the next half: when the scores of half m
+                // are there, product m - 5, the one before m - 1 on its barrier, has been seen.
                 auto pv_qk = [&](int t, int hf, bool more) {
                     const uint32_t s = (g + pos_v(t, n)) % NS;
+                    const uint32_t half = 2 * n_p + hf;
                     const unsigned long long vd = desc_v(ring + s * C::TILE_BYTES + hf * 8192);
                     if (!wait(p_ready(x, hf), n_p)) return;
                     if (elect_one()) {
 #pragma unroll
                         for (int k = 0; k < 4; k++)
                             umma_ts(t_o, t_s + hf * 64 + k * 8, vd + (unsigned long long)k * (2048 >> 4), idesc_o, hf == 0 && k == 0 ? t >= ahead : 1);
+                        umma_commit(pv_done(x, half));  // the product alone, not the scores behind it
                         if (more) issue_qk(t + ahead, hf);
-                        umma_commit(pv_done(x));
                         if (hf == 1) umma_commit(empty(s));
                         if (hf == 1 && t + ahead >= n) umma_commit(o_done(x));
                     }
                     __syncwarp();
+                    if (half >= 2) wait(pv_done(x, half - 2), (half - 2) >> 2);
                 };
                 auto arrived = [&](uint32_t at) { return wait(full(at % NS), at / NS); };
                 auto release = [&](uint32_t at) {
@@ -556,6 +562,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             if (elect_one()) umma_commit(drained(x));
             __syncwarp();
             mbar_wait(drained(x), 0, &never);
+            for (uint32_t i = 1; ok && i <= 2 && n_p > 0; i++) mbar_wait(pv_done(x, 2 * n_p - i), ((2 * n_p - i) >> 2) & 1u, &never);
           }
         } else {
             // ---------------------------------------------------------------- softmax of stream x
@@ -649,9 +656,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             m = mx;
                             first = false;
                         } else if (__any_sync(~0u, raise)) {
-                            // every product into O so far: the last but one is done (this half's scores followed it), so
-                            // the one-bit phase is unambiguous
-                            wait(pv_done(x), n_h - 1);
+                            wait(pv_done(x, n_h - 1), (n_h - 1) >> 2);  // the last product into O
                             const float c2 = raise ? ex2(m - mx) : 1.0f;
                             if (raise) m = mx;
                             l *= c2;
