@@ -408,17 +408,18 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // boxes of eight tokens and of one, or with 16-byte copies if their rows do not lie on 128 bytes (that takes one warp some
             // 10,000 cycles per item where TMA takes 1,500).  Rows past its tokens keep what they held: no other row
             // depends on them.  The next item's come in while the softmax and the last product of this one run.
-            uint32_t n_q[2] = {0, 0};
+            uint32_t n_q[2] = {0, 0};  // items whose queries have been asked for
             for (int u = u0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 u += pt.line;
                 for (int x = 0; x < 2 && pt.n > 0; x++) {
                     if (!has_tile(c.p, x, pt.n)) continue;
-                    if (!__all_sync(~0u, mbar_wait(q_free(x), (n_q[x]++ & 1u) ^ 1u, abort_flag))) {
+                    if (!__all_sync(~0u, mbar_wait(q_free(x), (n_q[x] & 1u) ^ 1u, abort_flag))) {
                         give_up();
                         u = u1;
                         break;
                     }
+                    n_q[x]++;
                     if (q_tma) {
                         const bool lead = x == 0 || c.p.tok0 == c.p.n_tok;
                         const int tok = lead ? c.p.tok0 : c.p.n_tok - c.p.tok0, r0 = c.q.s.row0 + c.p.ta + (lead ? 0 : c.p.tok0);
@@ -453,9 +454,9 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     if (lane == 0) mbar_arrive(q_ready(x));
                 }
             }
-            int never = 0;  // every copy has landed before the CTA may leave
+            int never = 0;  // every copy has landed before the CTA may leave, after a time-out too
             for (int x = 0; x < 2; x++)
-                if (n_q[x] > 0 && !*abort_flag) mbar_wait(q_ready(x), (n_q[x] - 1) & 1u, &never);
+                if (n_q[x] > 0) mbar_wait(q_ready(x), (n_q[x] - 1) & 1u, &never);
           } else if (warp <= 10) {
             // ---------------------------------------------------------------- MMA: warp 8 stream 0, warp 10 stream 1
             // The whole warp walks the loop and waits, one elected lane issues.
