@@ -121,6 +121,18 @@ bool at_address(aj_kv h, CUtensorMap *m, const CUtensorMap &from, const void *p)
     return h->replace(m, const_cast<void *>(p)) == CUDA_SUCCESS;
 }
 
+// Zeros that are there on return, for every stream: a plain cudaMemset is queued on the default stream behind whatever the
+// caller has there, and a stream that does not wait for that one would find the memory as it was.
+cudaError_t zero_now(void *p, size_t bytes) {
+    cudaStream_t s;
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(p, 0, bytes, s);
+    const cudaError_t e2 = cudaStreamSynchronize(s);
+    cudaStreamDestroy(s);
+    return e != cudaSuccess ? e : e2;
+}
+
 aj_status done(cudaError_t e) {
     if (e == cudaSuccess) return AJ_OK;
     cudaGetLastError();
@@ -206,8 +218,8 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     }
     const size_t n = (size_t)h->n_counters + max_B;
     if (cudaMalloc(&h->parts, h->parts_floats * 4) != cudaSuccess || cudaMalloc(&h->counters, n * 4) != cudaSuccess ||
-        cudaMemset(h->counters, 0, n * 4) != cudaSuccess || cudaMalloc(&h->status, 256) != cudaSuccess ||
-        cudaMemset(h->status, 0, 256) != cudaSuccess) {
+        cudaMalloc(&h->status, 256) != cudaSuccess || zero_now(h->counters, n * 4) != cudaSuccess ||
+        zero_now(h->status, 256) != cudaSuccess) {
         cudaGetLastError();
         aj_kv_destroy(h);
         return AJ_ERR_CUDA;
@@ -396,7 +408,7 @@ aj_status aj_kv_last_status(aj_kv h) {
         cudaGetLastError();
         return AJ_ERR_CUDA;
     }
-    if (s != 0 && cudaMemset(h->status, 0, 4) != cudaSuccess) return AJ_ERR_CUDA;
+    if (s != 0 && zero_now(h->status, 4) != cudaSuccess) return AJ_ERR_CUDA;
     return s == DEV_TIMEOUT ? AJ_ERR_TIMEOUT : AJ_OK;
 }
 

@@ -56,3 +56,48 @@ def test_attend_scores_that_rise_with_every_half_tile(n, path, D, window):
     out, lse = attend(s, h, window, 4 if window else 0, times=6)
     assert h.last_path() == path
     s.check_attend(out, lse, window, 4 if window else 0, rounded_weights=True)
+
+
+@pytest.mark.parametrize("n", [1, 17])
+def test_a_fresh_handle_is_ready_for_any_stream(n):
+    """Creation leaves nothing of its own behind work that is queued on the default stream: a handle made there serves a stream that does
+    not wait for it, wherever its memory was before.  (An item that spans CTAs is stored by the part that arrives last, by a count
+    from zero; an eviction writes its lengths likewise.)"""
+    import ctypes
+
+    import torch
+
+    s = Setup(3, [5000, 3000], [n, n], 8, 2, 128, 16, ragged=False)
+    warm = s.handle()
+    out, lse = attend(s, warm)  # kernels are loaded
+    w, p = torch.rand(2, 2, s.cap, device="cuda"), torch.arange(s.cap, device="cuda", dtype=torch.int32).repeat(2, 2, 1)
+    rows = [torch.zeros_like(x) for x in (s.seq_lens, w, p)]
+    warm.evict(s.k, s.v, s.block_table, s.seq_lens, w, p, *rows, 2, 6000)
+    assert rows[0].tolist() == s.lens
+
+    # small pieces of device memory full of ones, every other one given back
+    rt = ctypes.CDLL("libcudart.so.12")
+    held = []
+    for _ in range(1024):
+        x = ctypes.c_void_p()
+        assert rt.cudaMalloc(ctypes.byref(x), 2048) == 0 and rt.cudaMemset(x, 0xFF, 2048) == 0
+        held.append(x)
+    torch.cuda.synchronize()
+    for x in held[::2]:
+        assert rt.cudaFree(x) == 0
+    side = torch.cuda.Stream()
+    o, ls, lens = torch.full_like(out, 7.0), torch.full_like(lse, 7.0), torch.full_like(s.seq_lens, -3)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400_000_000)
+    busy = torch.cuda.Event()
+    busy.record()
+    h = s.handle()
+    h.attend(s.q, s.k, s.v, s.block_table, s.seq_lens, o, 2, n, s.scale, lse=ls, stream=side.cuda_stream)
+    h.evict(s.k, s.v, s.block_table, s.seq_lens, w, p, lens, rows[1], rows[2], 2, 6000, stream=side.cuda_stream)
+    side.synchronize()
+    queued = not busy.query()
+    torch.cuda.synchronize()
+    for x in held[1::2]:
+        assert rt.cudaFree(x) == 0
+    assert torch.equal(o, out) and torch.equal(ls, lse) and lens.tolist() == s.lens
+    assert queued, "the side stream did not run beside the default stream: nothing was tested"
