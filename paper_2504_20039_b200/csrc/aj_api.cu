@@ -244,8 +244,8 @@ aj_status aj_create(aj_handle *out, int device, int max_B, int max_K, int d, int
     const size_t max_M = (size_t)max_B * (max_K + 1);
     const size_t esz = elem_size(dtype);
     bool ok = cudaMalloc(&h->keys, max_M * sizeof(unsigned long long)) == cudaSuccess &&
-              cudaMemset(h->keys, 0, max_M * sizeof(unsigned long long)) == cudaSuccess &&
-              cudaMalloc(&h->status, 256) == cudaSuccess && cudaMemset(h->status, 0, 256) == cudaSuccess &&
+              zero_now(h->keys, max_M * sizeof(unsigned long long)) == cudaSuccess &&
+              cudaMalloc(&h->status, 256) == cudaSuccess && zero_now(h->status, 256) == cudaSuccess &&
               cudaMalloc(&h->st_ht, max_M * d * esz) == cudaSuccess &&
               (d_draft == 0 || cudaMalloc(&h->st_hd, max_M * d_draft * esz) == cudaSuccess) &&
               cudaMalloc(&h->st_tok, (size_t)max_B * max_K * 4) == cudaSuccess &&
@@ -581,7 +581,7 @@ aj_status aj_last_status(aj_handle h) {
     if (cudaDeviceSynchronize() != cudaSuccess) return AJ_ERR_CUDA;
     if (cudaMemcpy(&word, h->status, sizeof word, cudaMemcpyDeviceToHost) != cudaSuccess) return AJ_ERR_CUDA;
     if (word != 0) {
-        if (cudaMemset(h->status, 0, sizeof word) != cudaSuccess) return AJ_ERR_CUDA;
+        if (zero_now(h->status, sizeof word) != cudaSuccess) return AJ_ERR_CUDA;
         h->keys_dirty = true;  // a cycle that gave up may have left partial keys behind
     }
     return word == DEV_TIMEOUT ? AJ_ERR_TIMEOUT : (word == 0 ? AJ_OK : AJ_ERR_CUDA);

@@ -8,6 +8,18 @@
 
 namespace aj {
 
+// Zeros that are there on return, for every stream: a plain cudaMemset is queued on the default stream behind whatever the
+// caller has there, and a stream that does not wait for that one would find the memory as it was.
+inline cudaError_t zero_now(void *p, size_t bytes) {
+    cudaStream_t s;
+    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(p, 0, bytes, s);
+    const cudaError_t e2 = cudaStreamSynchronize(s);
+    cudaStreamDestroy(s);
+    return e != cudaSuccess ? e : e2;
+}
+
 // ---------------------------------------------------------------- packed (max, argmax) key
 //
 // A row's best (logit, index) so far is one 64-bit word whose unsigned order is

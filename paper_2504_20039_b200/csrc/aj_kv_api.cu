@@ -121,18 +121,6 @@ bool at_address(aj_kv h, CUtensorMap *m, const CUtensorMap &from, const void *p)
     return h->replace(m, const_cast<void *>(p)) == CUDA_SUCCESS;
 }
 
-// Zeros that are there on return, for every stream: a plain cudaMemset is queued on the default stream behind whatever the
-// caller has there, and a stream that does not wait for that one would find the memory as it was.
-cudaError_t zero_now(void *p, size_t bytes) {
-    cudaStream_t s;
-    cudaError_t e = cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking);
-    if (e != cudaSuccess) return e;
-    e = cudaMemsetAsync(p, 0, bytes, s);
-    const cudaError_t e2 = cudaStreamSynchronize(s);
-    cudaStreamDestroy(s);
-    return e != cudaSuccess ? e : e2;
-}
-
 aj_status done(cudaError_t e) {
     if (e == cudaSuccess) return AJ_OK;
     cudaGetLastError();
