@@ -115,7 +115,7 @@ aj_status aj_kv_evict(aj_kv h, void *k_pages, void *v_pages, int n_pages, const 
                       void *cuda_stream);
 
 /* AJ_OK, or AJ_ERR_TIMEOUT if a bounded wait of a kernel on this handle ran out since the last call of this
- * function (outputs since then are invalid).  Synchronises the device. */
+ * function (outputs since then are invalid; after this call the handle is as new).  Synchronises the device. */
 aj_status aj_kv_last_status(aj_kv h);
 /* Kernels launched by the last call on this handle, and the name of the path the last attend / weigh took. */
 int aj_kv_last_launch_count(aj_kv h);

@@ -396,7 +396,9 @@ aj_status aj_kv_last_status(aj_kv h) {
         cudaGetLastError();
         return AJ_ERR_CUDA;
     }
-    if (s != 0 && zero_now(h->status, 4) != cudaSuccess) return AJ_ERR_CUDA;
+    // a call that gave up may have left items without their last arrival: the counts of later calls begin at zero again
+    if (s != 0 && (zero_now(h->counters, ((size_t)h->n_counters + h->max_B) * 4) != cudaSuccess || zero_now(h->status, 4) != cudaSuccess))
+        return AJ_ERR_CUDA;
     return s == DEV_TIMEOUT ? AJ_ERR_TIMEOUT : AJ_OK;
 }
 
