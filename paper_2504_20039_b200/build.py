@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libaj_verify.so")
 SOURCES = ["aj_api.cu", "aj_umma_vm.cu", "aj_umma_pair.cu", "aj_simt.cu", "aj_judge.cu", "aj_rank.cu", "aj_static.cu", "aj_lr.cu",
            "aj_kv_api.cu", "aj_kv_append.cu", "aj_kv_simt.cu", "aj_kv_few.cu", "aj_kv_umma.cu", "aj_kv_weigh.cu", "aj_kv_weigh_umma.cu", "aj_kv_evict.cu"]
 HEADERS = ["aj_internal.cuh", "aj_ptx.cuh", os.path.join("..", "..", "include", "aj_verify.h"),
-           "aj_kv.cuh", "aj_kv_mma.cuh", "aj_kv_tc.cuh", os.path.join("..", "..", "include", "aj_kv.h")]
+           "aj_kv.cuh", "aj_kv_line.cuh", "aj_kv_mma.cuh", "aj_kv_tc.cuh", os.path.join("..", "..", "include", "aj_kv.h")]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC", "-cudart", "static", "--threads", "0",

@@ -21,6 +21,10 @@ struct View {
     int window = 0, sinks = 0;
 };
 
+struct Seq {
+    int row0, nq, L;  // first row of q, new tokens, slots in use
+};
+
 struct AttendArgs {
     View v;
     const void *q = nullptr, *k = nullptr, *vv = nullptr;
@@ -108,10 +112,6 @@ template <typename K> cudaError_t allow_shared(K kernel) {
     if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
 }
-
-struct Seq {
-    int row0, nq, L;  // first row of q, new tokens, slots in use
-};
 
 __device__ inline Seq seq_of(const View &v, int b) {
     Seq s;

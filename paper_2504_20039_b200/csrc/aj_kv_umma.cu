@@ -37,6 +37,7 @@
 // for the prompts with a window, from 30 on: 183 us).
 // Every wait is bounded (aj_ptx.cuh); one that runs out sets the status word and the CTA leaves by the normal way out.
 #include "aj_kv.cuh"
+#include "aj_kv_line.cuh"
 #include "aj_kv_tc.cuh"
 #include "aj_ptx.cuh"
 
@@ -45,13 +46,10 @@ namespace kv {
 
 namespace {
 
-constexpr int TILE = 128;
 constexpr int THREADS = 384;
 // Registers: launched with 168 a thread; the two softmax warpgroups, which hold a row of 128 scores, take 200 and leave
 // 104 to the third (2 x 200 + 104 = 3 x 168).  Each branch sets its own share: before that no code is shared.
 constexpr int REGS_SOFTMAX = 200, REGS_OTHER = 104;
-// What an item costs beside its tiles (its queries, the pipeline's start, its results), in tiles.
-constexpr int CHARGE = 2;
 constexpr uint32_t B_MN_MAJOR = 1u << 16;
 
 template <int D> struct Cfg {
@@ -60,76 +58,18 @@ template <int D> struct Cfg {
     static constexpr int BARS = 2 * STAGES + 24;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maxima and sums of both streams' rows
     static constexpr int SMEM = ML_AT + 4 * 128 * 4;
-    static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 4, "the prefix sums of the largest batch fit the ring");
+    static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 8, "the prefix sums of the largest batch fit the ring");
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
 };
 
-// The tokens of a row piece and the tiles of slots that they see.
-struct Piece {
-    int ta, n_tok, tok0;          // first token, tokens, tokens of stream 0 (== n_tok: both streams share the rows)
-    int first, n_sink, first_tile, units;
-};
-
-struct Seqs {                     // a sequence and how its new tokens are cut into pieces
-    Seq s;
-    int n, each, more;            // pieces, spread evenly
-};
-
-struct Line {                     // position in the line
-    int b, h, qt, unit;           // sequence, key head, row piece, tile within the item (below 0: its charge)
-    Seqs q;
-    Piece p;
-};
-
-// A CTA's part of an item: `line` places of the line, of which the tiles first .. first + n - 1.
-struct Part {
-    int line, first, n;
-};
-__device__ inline Part part_of(const Line &c, int left) {
-    Part p;
-    p.line = min(c.p.units - c.unit, left);
-    p.first = max(c.unit, 0);
-    p.n = max(0, c.unit + p.line - p.first);
-    return p;
-}
-
-__device__ inline Seqs pieces_of(const View &v, int b, int tpt) {
-    Seqs q;
-    q.s = seq_of(v, b);
-    q.n = (q.s.nq + 2 * tpt - 1) / (2 * tpt);
-    q.each = q.n ? q.s.nq / q.n : 0;
-    q.more = q.s.nq - q.each * q.n;
-    return q;
-}
-
-__device__ inline Piece piece_of(const View &v, const Seqs &q, int qt, int tpt) {
-    Piece p;
-    p.ta = qt * q.each + min(qt, q.more);
-    p.n_tok = q.each + (qt < q.more);
-    p.tok0 = p.n_tok <= tpt ? p.n_tok : (p.n_tok + 1) >> 1;
-    const int p_lo = q.s.L - q.s.nq + p.ta, end = max(0, p_lo + p.n_tok);
-    p.first = v.window ? min(max(0, p_lo - v.window + 1), end) : 0;
-    p.first_tile = p.first / TILE;
-    p.n_sink = min((min(v.sinks, p.first) + TILE - 1) / TILE, p.first_tile);
-    p.units = max(1, p.n_sink + (end + TILE - 1) / TILE - p.first_tile);
-    return p;
-}
-
 // Prefix sums over the sequences of their tiles, by all threads; returns the total.
-__device__ inline int build_line(const View &v, int tpt, int *pre) {
+__device__ inline long long build_line(const View &v, int tpt, long long *pre) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (v.n_q <= 16 * tpt) {  // few pieces: a thread per sequence; else a warp
-        for (int b = threadIdx.x; b < v.B; b += blockDim.x) {
-            const Seqs q = pieces_of(v, b, tpt);
-            int u = 0;
-            for (int i = 0; i < q.n; i++) u += CHARGE + piece_of(v, q, i, tpt).units;
-            pre[b + 1] = u * v.Hkv;
-        }
+        for (int b = threadIdx.x; b < v.B; b += blockDim.x) pre[b + 1] = units_of(v, pieces_of(seq_of(v, b), tpt), tpt, 0, 1) * v.Hkv;
     } else {
         for (int b = warp; b < v.B; b += blockDim.x >> 5) {
-            const Seqs q = pieces_of(v, b, tpt);
-            int u = 0;
-            for (int i = lane; i < q.n; i += 32) u += CHARGE + piece_of(v, q, i, tpt).units;
+            long long u = units_of(v, pieces_of(seq_of(v, b), tpt), tpt, lane, 32);
 #pragma unroll
             for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
             if (lane == 0) pre[b + 1] = u * v.Hkv;
@@ -138,12 +78,12 @@ __device__ inline int build_line(const View &v, int tpt, int *pre) {
     if (threadIdx.x == 0) pre[0] = 0;
     __syncthreads();
     if (warp == 0) {
-        int carry = 0;
+        long long carry = 0;
         for (int b0 = 1; b0 <= v.B; b0 += 32) {
-            int x = b0 + lane <= v.B ? pre[b0 + lane] : 0;
+            long long x = b0 + lane <= v.B ? pre[b0 + lane] : 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(~0u, x, o);
+                const long long y = __shfl_up_sync(~0u, x, o);
                 if (lane >= o) x += y;
             }
             if (b0 + lane <= v.B) pre[b0 + lane] = carry + x;
@@ -155,7 +95,7 @@ __device__ inline int build_line(const View &v, int tpt, int *pre) {
 }
 
 // By a whole warp.
-__device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
+__device__ inline Line seek(const View &v, int tpt, const long long *pre, long long u) {
     Line c;
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = v.B;  // pre[lo] <= u < pre[hi]
@@ -164,10 +104,10 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
         if (pre[mid] <= u) lo = mid; else hi = mid;
     }
     c.b = lo;
-    c.q = pieces_of(v, lo, tpt);
-    const int per_head = (pre[lo + 1] - pre[lo]) / v.Hkv;
-    int r = u - pre[lo];
-    c.h = r / per_head;
+    c.q = pieces_of(seq_of(v, lo), tpt);
+    const long long per_head = (pre[lo + 1] - pre[lo]) / v.Hkv;
+    long long r = u - pre[lo];
+    c.h = (int)(r / per_head);
     r -= c.h * per_head;
     for (int q0 = 0;; q0 += 32) {
         const int n = q0 + lane < c.q.n ? CHARGE + piece_of(v, c.q, q0 + lane, tpt).units : 0;
@@ -181,7 +121,7 @@ __device__ inline Line seek(const View &v, int tpt, const int *pre, int u) {
         if (r < all) {
             const int at = __ffs(__ballot_sync(~0u, r < x)) - 1;
             c.qt = q0 + at;
-            c.unit = r - __shfl_sync(~0u, x - n, at) - CHARGE;
+            c.unit = (int)r - __shfl_sync(~0u, x - n, at) - CHARGE;
             break;
         }
         r -= all;
@@ -199,17 +139,12 @@ __device__ inline void next_item(const View &v, int tpt, Line &c) {
             c.h = 0;
             do {
                 if (++c.b >= v.B) return;
-                c.q = pieces_of(v, c.b, tpt);
+                c.q = pieces_of(seq_of(v, c.b), tpt);
             } while (c.q.n == 0);
         }
     }
     c.p = piece_of(v, c.q, c.qt, tpt);
 }
-
-// Does stream x have a tile in a segment of n tiles of this piece?
-__device__ inline bool has_tile(const Piece &p, int x, int n) { return x == 0 || p.tok0 < p.n_tok || n > 1; }
-
-__device__ inline int tile_of(const Piece &p, int unit) { return unit < p.n_sink ? unit : unit - p.n_sink + p.first_tile; }
 
 // Order of the K and V tiles of a segment of n tiles in the ring: K0 K1 V0 K2 V1 ... V(n-1).
 __device__ inline int pos_k(int t) { return t == 0 ? 0 : 2 * t - 1; }
@@ -301,7 +236,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     auto q_free = [&](int x) { return bars + 8u * (2 * NS + 22 + x); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + (2 + NS) * C::TILE_BYTES + C::BARS * 8);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    int *pre = reinterpret_cast<int *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
+    long long *pre = reinterpret_cast<long long *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
 
@@ -325,20 +260,22 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         fence_barrier_init();
     }
     if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
-    const int total = build_line(v, tpt, pre);  // synchronises the CTA
+    const long long total = build_line(v, tpt, pre);  // synchronises the CTA
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     // a piece of less than four tiles costs more in the join than its tiles (one window of 17 rows: 35 -> 28 us)
-    const int per = max(4, (total + (int)gridDim.x - 1) / (int)gridDim.x);
-    const int u0 = min(total, (int)blockIdx.x * per), u1 = min(total, u0 + per);
+    // (a CTA's places fit an int, the line's need not; see the bounds at units_of)
+    const int per = (int)max(4ll, (total + gridDim.x - 1) / gridDim.x);
+    const long long u0 = min(total, (long long)blockIdx.x * per);
+    const int u1 = (int)(min(total, u0 + per) - u0);  // from here on places are counted from u0
     auto give_up = [&]() {
         *abort_flag = 1;
         atomicCAS(a.status, DEV_OK, DEV_TIMEOUT);
     };
 
-    if (u0 < u1) {
+    if (u1 > 0) {
         if (warp >= 8) {
           asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
           Line c = seek(v, tpt, pre, u0);
@@ -351,7 +288,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const uint32_t box_bytes = (uint32_t)v.page * 128u;
             uint32_t g = 0;
             bool ok = true;
-            for (int u = u0; ok && u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; ok && u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -409,7 +346,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // 10,000 cycles per item where TMA takes 1,500).  Rows past its tokens keep what they held: no other row
             // depends on them.  The next item's come in while the softmax and the last product of this one run.
             uint32_t n_q[2] = {0, 0};  // items whose queries have been asked for
-            for (int u = u0; u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 u += pt.line;
                 for (int x = 0; x < 2 && pt.n > 0; x++) {
@@ -476,7 +413,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             };
             // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
             // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
-            for (int u = u0; ok && u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; ok && u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -590,7 +527,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const float scale = a.scale_log2;
             const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31) == 0;  // rows on 32 bytes
             auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
-            for (int u = u0; u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; u < u1; next_item(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n, unit = c.unit;
                 u += pt.line;
@@ -691,8 +628,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 // Streams of their own rows store and join by themselves, streams that share rows together.
                 const bool whole = n == c.p.units;
                 const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
-                const int i0 = u - pt.line - unit, cta0 = i0 / per;  // the line's unit and the CTA where the item's tiles begin
-                const int n_parts = (i0 + c.p.units - 1) / per - cta0 + 1, mine = (int)blockIdx.x - cta0;
+                const int i0 = u - pt.line - unit;  // the place where the item's tiles begin, from u0
+                const int mine = -floor_div(i0, per), cta0 = (int)blockIdx.x - mine, n_parts = floor_div(i0 + c.p.units - 1, per) + mine + 1;
                 unsigned *counter = a.counters + 2 * cta0 + who;
                 volatile uint32_t *last = tmem_slot + 2 + who;  // every other part is in the workspace
                 const bool lead = row == 0 && x == who;
