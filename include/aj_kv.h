@@ -73,9 +73,12 @@ aj_status aj_kv_append(aj_kv h, const void *q, long long q_stride, const void *k
  * Attention of the new tokens over the cache: out = softmax(scale * q K^T) V over the visible slots.
  * The token in slot p sees slot j iff j <= p and (window == 0, or j > p - window, or j < sinks).
  *   out [rows, Hq * D] (row stride out_stride), lse [rows, Hq] f32 optional: log of the sum of exponentials
- * A row that sees nothing gets zeros and lse = -inf.  Scores, maximum, sum and output accumulate in 32 bits.  On the
- * tensor cores the weights exp(s - max) are rounded to bf16 before they meet V.  Keys that a row does not see never
- * reach it whatever they hold; a non-finite VALUE in a slot that other rows of the call see may reach it.
+ * A row that sees nothing, or whose visible scores are all -inf, gets zeros and lse = -inf.  A NaN or +infinite score makes its
+ * row NaN, lse too.  Keys that a row does not see never reach it whatever they hold; a non-finite VALUE in a slot that other
+ * rows of the call see may reach it.
+ * Scores, maximum, sum and output accumulate in 32 bits.  On the tensor cores the weights exp(s - max) are rounded to bf16
+ * before they meet V, and above 16 rows a quarter of the exponentials are a polynomial with a relative error below 4e-6: lse
+ * is off by less than that (by 1e-6 where many slots share the weight).
  * Two runs on the same inputs give the same bits.
  * More than 16 rows (new tokens x query heads per key head) go to the tensor cores only where k_pages and v_pages start on
  * 128 bytes, as an allocation does, and Hq / Hkv <= 128; else the CUDA cores take them, many times slower.  Rows of q on 128

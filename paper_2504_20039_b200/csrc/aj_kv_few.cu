@@ -297,14 +297,14 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                     }
                 }
             auto store = [&](int r, int d, float4 x, float mm, float ll) {  // four elements of an output row
-                const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
                 const size_t row = (size_t)cur.s.row0 + r / v.G;
                 const int head = cur.h * v.G + r % v.G;
                 uint2 y;
                 y.x = pack(x.x * inv, x.y * inv);
                 y.y = pack(x.z * inv, x.w * inv);
                 *reinterpret_cast<uint2 *>((__nv_bfloat16 *)a.out + row * a.out_stride + (size_t)head * D + d) = y;
-                if (d == 0 && a.lse) a.lse[row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+                if (d == 0 && a.lse) a.lse[row * v.Hq + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * LN2;
             };
 #pragma unroll
             for (int nh = 0; nh < 2 * NT; nh++) {

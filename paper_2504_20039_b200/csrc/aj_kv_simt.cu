@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(32 * WARPS) attend_simt_kernel(AttendArgs a, i
         const int idx = rb * R + r;
         const size_t row = (size_t)s.row0 + idx / v.G;
         const int head = h * v.G + idx % v.G;
-        ((T *)a.out)[row * a.out_stride + (size_t)head * D + d] = from_f32<T>(ll > 0.0f ? x / ll : 0.0f);
-        if (d == 0 && a.lse) a.lse[row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+        ((T *)a.out)[row * a.out_stride + (size_t)head * D + d] = from_f32<T>(ll == 0.0f ? 0.0f : x / ll);  // a sum that is NaN stays one
+        if (d == 0 && a.lse) a.lse[row * v.Hq + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * LN2;
     };
     const int stride = R * (D + 2);
     float *mine = a.parts + ((size_t)item * splits + split) * stride;

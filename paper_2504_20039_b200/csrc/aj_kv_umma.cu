@@ -196,9 +196,10 @@ __device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap *tmap, int c0
         : "memory");
 }
 __device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 2^x for a pair on the multiply-add pipe, for x <= 16: x = n + f with n the nearest integer, 2^f by the polynomial
-// that interpolates it at the five Chebyshev nodes of [-1/2, 1/2] (relative error below 4e-6, of either sign), 2^n by
-// adding to the exponent.  Arguments below -127 (masked slots) give less than 2^-126.
+// 2^x for a pair on the multiply-add pipe, for x <= RAISE (which is far inside its range): x = n + f with n the nearest
+// integer, 2^f by the polynomial that interpolates it at the five Chebyshev nodes of [-1/2, 1/2] (relative error below 4e-6, of
+// either sign: a thousandth of what rounding a weight to bf16 takes, and as much in lse at most), 2^n by adding to the exponent.
+// Arguments of -127 and below (masked slots) give zero, those up to -126 less than 2^-126, NaN gives zero too.
 constexpr float P0 = 1.0f, P1 = 0.6931210527f, P2 = 0.2402234922f, P3 = 0.05592198042f, P4 = 0.009666368369f;
 __device__ inline uint64_t ex2_poly(uint64_t x) {
     const uint64_t y = f2(fmaxf(lo(x), -127.0f), fmaxf(hi(x), -127.0f));
@@ -588,7 +589,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         for (int i = 0; i < 64; i += 8)
 #pragma unroll
                             for (int j = 0; j < 4; j++) mx4[j] = max3(mx4[j], __uint_as_float(sr[i + j]), __uint_as_float(sr[i + 4 + j]));
-                        const float mx = fmaxf(max3(mx4[0], mx4[1], mx4[2]), mx4[3]) * scale;
+                        const float mx = max3(max3(mx4[0], mx4[1], mx4[2]), mx4[3], mx4[3]) * scale;  // NaN if a score is
                         const bool raise = mx > m + RAISE;
                         if (first) {
                             m = mx;
@@ -601,7 +602,8 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
 #pragma unroll 1
                             for (int k = 0; k < D / 16; k++) tmem_scale16(t_o + k * 16, c2);
                         }
-                        const float ref = m == -INFINITY ? 0.0f : m;
+                        // a score that is NaN or +infinite makes the row NaN (the polynomial would pass over it)
+                        const float ref = !(mx < INFINITY) ? __int_as_float(0x7fffffff) : m == -INFINITY ? 0.0f : m;
                         const uint64_t scale2 = f2(scale, scale), ref2 = f2(-ref, -ref);
                         uint64_t sum2[2] = {0, 0};
                         // every fourth pair of exponentials on the multiply-add pipe: both streams' other ones queue at the
@@ -624,7 +626,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     }
                 }
                 // ---- the segment is done: store, or leave a partial result
-                if (m == -INFINITY) l = 0.0f;  // a row that saw nothing (the polynomial leaves a trace for masked slots)
                 // Streams of their own rows store and join by themselves, streams that share rows together.
                 const bool whole = n == c.p.units;
                 const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
@@ -708,7 +709,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         for (int i = 0; i < n_parts; i++)
                             ll += i == mine ? w_mine * l : ex2(__ldcg(part_of_cta(i) + 256 * D + at) - ref) * __ldcg(part_of_cta(i) + 256 * (D + 1) + at);
                     }
-                    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+                    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
                     const int t_row = token(row);
                     const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
                     const int head = c.h * v.G + row - t_row * v.G;
@@ -758,7 +759,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             }
                         }
                     }
-                    if (x == who && row < n_rows && a.lse) a.lse[out_row * v.Hq + head] = ll > 0.0f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+                    if (x == who && row < n_rows && a.lse) a.lse[out_row * v.Hq + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * LN2;
                     if (lead && !whole) *counter = 0;
                 }
                 __syncwarp();

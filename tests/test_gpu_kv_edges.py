@@ -101,3 +101,70 @@ def test_a_fresh_handle_is_ready_for_any_stream(n):
         assert rt.cudaFree(x) == 0
     assert torch.equal(o, out) and torch.equal(ls, lse) and lens.tolist() == s.lens
     assert queued, "the side stream did not run beside the default stream: nothing was tested"
+
+
+PATHS = [("bf16", 1, 0, "few"), ("bf16", 4, 0, "few"), ("bf16", 17, 0, "umma"), ("bf16", 33, 0, "umma"), ("bf16", 70, 0, "umma"), ("bf16", 4, 1, "simt"), ("f32", 1, 0, "simt"),
+         ("f32", 9, 0, "simt")]
+
+
+@pytest.mark.parametrize("dtype,n,flags,path", PATHS)
+@pytest.mark.parametrize("what", ["nan_key", "inf_score", "nan_query", "nan_everywhere", "minus_inf_scores"])
+@pytest.mark.parametrize("window", [0, 150])
+def test_attend_scores_that_are_no_numbers(dtype, n, flags, path, what, window):
+    """A NaN or +infinite score of a slot that a row sees makes the row NaN, lse too, wherever the slot lies in a tile; rows that do not see the
+    slot keep their bits.  Scores of -infinity weigh nothing."""
+    import torch
+
+    B = 8
+    s = Setup(n, [700 + 37 * b for b in range(B)], [n] * B, 8, 2, 128, 32, dtype, ragged=False)
+    h = s.handle(flags)
+    sinks = 4 if window else 0
+    base, base_lse = attend(s, h, window, sinks)
+    s.check_attend(base, base_lse, window, sinks, rounded_weights=path != "simt")
+    hit = torch.zeros(s.T, s.Hq, dtype=torch.bool)
+    if what in ("nan_key", "inf_score", "minus_inf_scores"):
+        if what != "nan_key":
+            s.q.view(s.T, s.Hq, 128)[:, :, 5] = 1.0
+            base, base_lse = attend(s, h, window, sinks)
+        value = {"nan_key": float("nan"), "inf_score": float("inf"), "minus_inf_scores": -float("inf")}[what]
+        for b in range(B):  # every place in a group of eight, of either half of a tile, seen by some of the new tokens at least
+            L = s.lens[b]
+            slots = [L - n - 8 - (L - n) % 8 + b] + ([L - 1 - b % n] if n > 1 else [])
+            for j in slots:
+                s.k[int(s.table[b, j // 32]), 1, j % 32, 5] = value
+                seen = s.visible(b, window, sinks)[:, j]
+                hit[b * n : (b + 1) * n, 4:] |= seen[:, None]
+    elif what == "nan_query":
+        for b in range(B):
+            t, i = b * n + b % n, b % 8
+            s.q[t, i * 128 + 7 * b] = float("nan")
+            hit[t, i] = True
+    else:
+        for b in range(B):
+            p = torch.from_numpy(s.table[b, : -(-s.lens[b] // 32)])
+            s.k[p, 1] = float("nan")
+        hit[:, 4:] = True
+    out, lse = attend(s, h, window, sinks)
+    assert h.last_path() == path
+    out, base = out.view(s.T, s.Hq, 128).cpu(), base.view(s.T, s.Hq, 128).cpu()
+    lse, base_lse = lse.cpu(), base_lse.cpu()
+    assert hit.any()
+    if what == "minus_inf_scores":
+        s.check_attend(out.reshape(s.T, -1), lse, window, sinks, rounded_weights=path != "simt")
+    else:
+        assert torch.isnan(out[hit]).all() and torch.isnan(lse[hit]).all()
+    assert torch.equal(out[~hit], base[~hit]) and torch.equal(lse[~hit], base_lse[~hit])
+
+
+@pytest.mark.parametrize("dtype,n,flags,path", PATHS)
+def test_attend_rows_whose_every_score_is_minus_infinity(dtype, n, flags, path):
+    """Nothing is left of a row whose every visible score is -infinity: zeros and lse = -inf, as for a row that sees nothing."""
+    import torch
+
+    s = Setup(n, [300, 100], [n] * 2, 8, 2, 128, 32, dtype, ragged=False)
+    s.k[..., 5] = torch.where(torch.isnan(s.k[..., 5]), s.k[..., 5], -float("inf"))
+    s.q.view(s.T, s.Hq, 128)[:, :, 5] = 1.0
+    h = s.handle(flags)
+    out, lse = attend(s, h)
+    assert h.last_path() == path
+    assert (out == 0).all() and (lse == -float("inf")).all()
