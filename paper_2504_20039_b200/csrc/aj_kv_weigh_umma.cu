@@ -23,6 +23,10 @@ namespace {
 
 constexpr int BLK = 128, ROWS = 256, THREADS = 320;
 
+template <bool X> struct Const {
+    static constexpr bool value = X;
+};
+
 template <int D> struct Cfg {
     static constexpr int TILE = BLK * D * 2, QB = ROWS * D * 2;
     static constexpr int STAGES = D == 128 ? 4 : 8;
@@ -304,7 +308,7 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
                             tc_fence_after();
                             // does every row of the chunk see every slot of the block?
                             const bool masked = p0 + r0 / v.G < j0 + BLK - 1 || (v.window && j0 <= p0 + (r0 + rows - 1) / v.G - v.window);
-                            auto use = [&](uint32_t (&sc)[64], int c0) {
+                            auto use = [&](uint32_t (&sc)[64], int c0, auto is_masked) {
 #pragma unroll
                                 for (int q = 0; q < 64; q += 16) {
                                     if (c0 + q >= rows) break;
@@ -313,24 +317,36 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
                                         for (int i = q; i < q + 16; i++)
                                             if (c0 + i >= rows) sc[i] = 0u;
                                     }
-                                    if (masked) {
+                                    // one bit per row that sees this slot; the others' exponentials count as zero, whatever
+                                    // their lse is (a NaN there is no business of a slot that the row does not see)
+                                    uint32_t seen = 0;
+                                    if (is_masked.value) {
 #pragma unroll
-                                        for (int i = q; i < q + 16; i++)
-                                            if (!sees(v, row_slot[(c0 + i) & (ROWS - 1)], j)) sc[i] = 0xff800000u;
+                                        for (int i = 0; i < 16; i++)
+                                            if (sees(v, row_slot[(c0 + q + i) & (ROWS - 1)], j)) seen |= 1u << i;
                                     }
+                                    auto pair = [&](uint64_t y, int i) {
+                                        float a = ex2(lo(y)), b = ex2(hi(y));
+                                        if (is_masked.value) {
+                                            a = seen >> (i - q) & 1 ? a : 0.0f;
+                                            b = seen >> (i - q + 1) & 1 ? b : 0.0f;
+                                        }
+                                        return f2(a, b);
+                                    };
 #pragma unroll
                                     for (int i = q; i < q + 16; i += 4) {
                                         const ulonglong2 n4 = *reinterpret_cast<const ulonglong2 *>(neg + c0 + i);
                                         const uint64_t y0 = fma2(f2(__uint_as_float(sc[i]), __uint_as_float(sc[i + 1])), scale2, n4.x), y1 = fma2(f2(__uint_as_float(sc[i + 2]), __uint_as_float(sc[i + 3])), scale2, n4.y);
-                                        sum[0] = add2(sum[0], f2(ex2(lo(y0)), ex2(hi(y0))));
-                                        sum[1] = add2(sum[1], f2(ex2(lo(y1)), ex2(hi(y1))));
+                                        sum[0] = add2(sum[0], pair(y0, i));
+                                        sum[1] = add2(sum[1], pair(y1, i + 2));
                                     }
                                 }
                             };
                             for (int c0 = 0; c0 < rows; c0 += 64) {
                                 uint32_t sc[64];
                                 tmem_ld64(t_acc + c0, sc);
-                                use(sc, c0);
+                                if (masked) use(sc, c0, Const<true>());
+                                else use(sc, c0, Const<false>());
                             }
                             tc_fence_before();
                             mbar_arrive(acc_empty(x));

@@ -168,3 +168,54 @@ def test_attend_rows_whose_every_score_is_minus_infinity(dtype, n, flags, path):
     out, lse = attend(s, h)
     assert h.last_path() == path
     assert (out == 0).all() and (lse == -float("inf")).all()
+
+
+@pytest.mark.parametrize("dtype,n,flags,path", [("bf16", 1, 0, "mma"), ("bf16", 4, 0, "mma"), ("bf16", 17, 0, "umma"), ("bf16", 33, 0, "umma"), ("bf16", 70, 0, "umma"),
+                                                ("bf16", 9, 1, "simt"), ("f32", 9, 0, "simt")])
+@pytest.mark.parametrize("what", ["nan_lse", "nan_query", "nan_key"])
+@pytest.mark.parametrize("window", [0, 150])
+def test_weigh_keeps_a_nan_to_the_slots_that_see_it(dtype, n, flags, path, what, window):
+    """A NaN in a row's lse or query reaches the slots that the row sees and no others, a NaN key its own slot if a counted row sees it;
+    every other weight keeps its bits."""
+    import torch
+
+    s = Setup(n, [300 + 61 * b for b in range(4)], [n] * 4, 8, 2, 128, 32, dtype, ragged=False)
+    h = s.handle(flags)
+    sinks = 4 if window else 0
+    lse = attend(s, h, window, sinks)[1].clone()
+    before = torch.rand(s.B, s.Hkv, s.cap, device="cuda")
+    rows = torch.tensor([n, max(1, n // 2), n, n], dtype=torch.int32, device="cuda")
+
+    def weigh():
+        out = s.guard(torch.full((s.B, s.Hkv, s.cap), -3.0), "weight_out")
+        h.weigh(s.q, lse, s.k, s.block_table, s.seq_lens, before, out, s.B, n, s.scale, n_rows=rows, window=window, sinks=sinks)
+        torch.cuda.synchronize()
+        assert h.last_status() == 0 and h.last_path() == path
+        return out.cpu()
+
+    base = weigh()
+    assert not torch.isnan(base).any()
+    hit = torch.zeros(s.B, s.Hkv, s.cap, dtype=torch.bool)
+    for b, L in enumerate(s.lens):
+        m = int(rows[b])
+        seen = s.visible(b, window, sinks)[:m]
+        if what == "nan_key":
+            for j in (5, L // 2, L - n + n // 3, L - 1):
+                s.k[int(s.table[b, j // 32]), 1, j % 32, 9] = float("nan")
+                hit[b, 1, j] = seen[:, j].any()
+        else:
+            t, i = (0 if b % 2 else m // 2), 1 + 2 * b  # a row that counts
+            if what == "nan_lse":
+                lse[b * n + t, i] = float("nan")
+            else:
+                s.q[b * n + t, i * 128 + 3] = float("nan")
+            hit[b, i // 4, :L] |= seen[t]
+            if m < n:  # and one that does not
+                if what == "nan_lse":
+                    lse[b * n + n - 1, i] = float("nan")
+                else:
+                    s.q[b * n + n - 1, i * 128 + 3] = float("nan")
+    got = weigh()
+    s.check_guards()
+    assert hit.any() and torch.isnan(got[hit]).all()
+    assert torch.equal(got[~hit], base[~hit])
