@@ -91,8 +91,9 @@ kv::View view_of(aj_kv h, int n_pages, const int32_t *table, int width, const in
     v.D = h->D;
     v.page = h->page;
     v.page_shift = h->page_shift;
-    v.window = window;
-    v.sinks = sinks;
+    // a window as long as the cache hides nothing (positions minus a window must not wrap, below a first slot either)
+    v.window = window < v.cap ? window : 0;
+    v.sinks = sinks < v.cap ? sinks : v.cap;
     return v;
 }
 

@@ -219,3 +219,27 @@ def test_weigh_keeps_a_nan_to_the_slots_that_see_it(dtype, n, flags, path, what,
     s.check_guards()
     assert hit.any() and torch.isnan(got[hit]).all()
     assert torch.equal(got[~hit], base[~hit])
+
+
+@pytest.mark.parametrize("dtype,n,flags,path", PATHS)
+@pytest.mark.parametrize("window,sinks", [(2**31 - 1, 0), (2**31 - 1, 2**31 - 1), (7, 2**31 - 1), (1000, 2**30)])
+def test_windows_and_sinks_as_large_as_an_int(dtype, n, flags, path, window, sinks):
+    """A window or sinks of no limit, with sequences that have fewer slots than new tokens: the bits of the call without a window."""
+    import torch
+
+    s = Setup(n, [3, 500, 1, 0, n + 2, 5, 77, 300], [n] * 8, 8, 2, 128, 32, dtype, ragged=False)
+    h = s.handle(flags)
+    base, base_lse = attend(s, h)
+    s.check_attend(base, base_lse, 0, 0, rounded_weights=path != "simt")
+    out, lse = attend(s, h, window, sinks)
+    assert h.last_path() == path
+    s.check_attend(out, lse, 0, 0, rounded_weights=path != "simt")
+    if window >= s.cap:
+        assert torch.equal(out, base) and torch.equal(lse, base_lse)
+    before = torch.rand(s.B, s.Hkv, s.cap, device="cuda")
+    weights = [s.guard(torch.full((s.B, s.Hkv, s.cap), -3.0), "weight_out") for _ in range(2)]
+    for w, (win, snk) in zip(weights, [(0, 0), (window, sinks)]):
+        h.weigh(s.q, base_lse, s.k, s.block_table, s.seq_lens, before, w, s.B, n, s.scale, window=win, sinks=snk)
+    torch.cuda.synchronize()
+    s.check_guards()
+    assert torch.equal(weights[0], weights[1])
