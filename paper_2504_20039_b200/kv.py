@@ -7,7 +7,7 @@ from __future__ import annotations
 import ctypes
 
 from . import binding
-from .binding import AJ_BF16, AJ_OK, AjError
+from .binding import AJ_BF16, AJ_ERR_INVALID_ARG, AJ_OK, AjError
 
 AJ_KV_FLAG_FORCE_SIMT = 1
 
@@ -71,6 +71,10 @@ class KvHandle:
 
         cos_sin [n_pos, rot_dim] f32 holds rot_dim / 2 cosines, then as many sines, of each position."""
         n_pos, width = cos_sin.shape if cos_sin is not None else (0, 0)
+        if cos_sin is not None and rot_dim not in (None, width, 0):  # the library takes rot_dim for the length of the table's rows
+            if check:
+                raise AjError(AJ_ERR_INVALID_ARG, "aj_kv_append")
+            return AJ_ERR_INVALID_ARG
         st = self._append(self._h, q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _p(q_norm), _p(k_norm),
                           eps, _p(cos_sin), n_pos, width if rot_dim is None else rot_dim, interleaved, _p(positions), k_pages.data_ptr(),
                           v_pages.data_ptr(), k_pages.shape[0], block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(), _p(q_start),
