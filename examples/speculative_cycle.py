@@ -38,7 +38,7 @@ class ToyModel:
         ang = torch.arange(4 * max_tokens, device="cuda")[:, None] * 10000.0 ** (-torch.arange(0, D, 2, device="cuda") / D)
         self.cos_sin = torch.cat([ang.cos(), ang.sin()], 1).float().contiguous()
         self.q_norm, self.k_norm = torch.ones(D, device="cuda"), torch.ones(D, device="cuda")
-        self.h = aj.KvHandle(torch.cuda.current_device(), B, max_q, Hq, Hkv, D, page)
+        self.h = aj.KvHandle(torch.cuda.current_device(), B, max_q, Hq, Hkv, D, page, strict=True)
 
     def forward(self, tokens, row_seq, positions, n_q, q_start=None):
         """Hidden states [rows, d] of new tokens; leaves the queries and lse of the call for `weigh`."""
