@@ -630,7 +630,12 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const bool whole = n == c.p.units;
                 const int who = shared_rows ? 0 : x, id = shared_rows ? 1 : 2 + x, threads = shared_rows ? 256 : 128;
                 const int i0 = u - pt.line - unit;  // the place where the item's tiles begin, from u0
-                const int mine = -floor_div(i0, per), cta0 = (int)blockIdx.x - mine, n_parts = floor_div(i0 + c.p.units - 1, per) + mine + 1;
+                int mine = 0, n_parts = 1;
+                if (!whole) {
+                    mine = -floor_div(i0, per);
+                    n_parts = floor_div(i0 + c.p.units - 1, per) + mine + 1;
+                }
+                const int cta0 = (int)blockIdx.x - mine;
                 unsigned *counter = a.counters + 2 * cta0 + who;
                 volatile uint32_t *last = tmem_slot + 2 + who;  // every other part is in the workspace
                 const bool lead = row == 0 && x == who;
