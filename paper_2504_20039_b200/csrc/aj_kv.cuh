@@ -92,7 +92,7 @@ cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s);
 cudaError_t launch_evict(const EvictArgs &a, unsigned *counters, const int (&clusters)[4], int num_sms, cudaStream_t s);
 
-// Once per device, before the first launch: more than 48 KB of shared memory per CTA.
+// For every handle, on its device: more than 48 KB of shared memory per CTA, and what eviction may ask for (a handle takes 0.6 ms).
 cudaError_t prepare_attend_few();
 cudaError_t prepare_attend_umma();
 cudaError_t prepare_weigh_mma();
