@@ -24,17 +24,20 @@
 // to 16 us a call, most of it in finding its place on the line).
 //
 // What bounds it, and what it measured (8 key heads, 32 query heads):
-//   windows of 33 rows, 64 sequences of 129 .. 4100 slots, D = 128: the stream of pages, 152 us, 4.0 TB/s; 6 us go by
-//   before the first scores, 3 us between two items, 5 us in the last join
-//   a prompt of 8192, D = 128: the exponentials (16 per clock and SM: 2048 cycles for two tiles of 128 x 128, a quarter
-//   of them on the multiply-add pipe) beside 2048 cycles of the tensor pipe for their four products; 484 us alone,
-//   1.13 PFLOP/s; back to back the card's power limit lowers the clock
+//   windows of 33 rows, 64 sequences of 129 .. 4100 slots, D = 128: 162 us, 3.8 TB/s; 6 us go by before the first scores, 3 us
+//   between two items, 5 us in the last join.  132 rows, four more than a tile holds, make two tiles of 68 and 64: their
+//   products keep the tensor pipe 47 % busy in what should be a stream of pages
+//   a prompt of 8192, D = 128: 510 us alone, 1.08 PFLOP/s; back to back the card's power limit lowers the clock (570 us)
 //   four prompts with a window of 1024, D = 64: half the products for as many exponentials, and ten tiles an item, two of
-//   them partly masked; 173 us
+//   them partly masked; 174 us
+//   In both, a pair of tiles (256 x 128 scores) takes some 3500 cycles, where its exponentials take 1536 of their unit (16 per
+//   clock and SM, a quarter of them on the multiply-add pipe) and its four products 2048 (D = 128) or 1024 of the
+//   tensor pipe: with two softmax warps per scheduler it is their latencies that are left over (an instruction in 35 to 47 % of the
+//   issue slots; waits for tensor memory first, then for results of fixed latency, then for instructions)
 //
 // The running maximum is a reference that is raised only when a score exceeds it by more than RAISE, so the rescaling of
 // O (a round trip through tensor memory) is rare; weights far above 1 are as exact as weights up to 1 (raised from 8 on: 192 us
-// for the prompts with a window, from 30 on: 183 us).
+// for the prompts with a window, from 30 on: 183 us, at that stage).
 // Every wait is bounded (aj_ptx.cuh); one that runs out sets the status word and the CTA leaves by the normal way out.
 #include "aj_kv.cuh"
 #include "aj_kv_line.cuh"
