@@ -174,3 +174,54 @@ def test_evict_where_keys_and_moves_do_not_fit(lens, Hkv, keep, inplace):
             k0[to[0], hh, to[1]], v0[to[0], hh, to[1]] = k0[fro[0], hh, fro[1]], v0[fro[0], hh, fro[1]]
     for got, want in ((s.k.cpu(), k0), (s.v.cpu(), v0)):
         assert torch.equal(torch.nan_to_num(got, nan=99.0), torch.nan_to_num(want, nan=99.0))
+
+
+@pytest.mark.parametrize("n,D", [(3, 128), (9, 64)])
+def test_more_query_heads_than_a_row_tile(n, D):
+    """200 query heads on one key head: attention goes to the CUDA cores, weights stay on the tensor cores."""
+    s = Setup(n, [300, 2, 129], [n] * 3, 200, 1, D, 32, ragged=False)
+    h = s.handle()
+    out, lse = attend(s, h, 100, 3)
+    assert h.last_path() == "simt"
+    s.check_attend(out, lse, 100, 3, rounded_weights=False)
+    weigh_and_check(s, h, [n, 1, 2], 100, 3)
+    assert h.last_path() == "umma"
+
+
+@pytest.mark.parametrize("n,D,paths", [(1, 128, ("few", "mma")), (17, 128, ("simt", "mma")), (33, 64, ("simt", "mma"))])
+@pytest.mark.parametrize("window", [0, 150])
+def test_pages_off_128_bytes(n, D, paths, window):
+    """Pages that start on 16 bytes but not on 128, as a slice of a larger tensor may."""
+    import torch
+
+    s = Setup(n, [700, 64, 333, 1], [n] * 4, 8, 2, D, 16, ragged=False)
+    for name in ("k", "v"):
+        t = getattr(s, name)
+        room = s.guard(torch.zeros(t.numel() + 8, dtype=t.dtype), name + "_off")
+        moved = room[8:].view(t.shape)
+        moved.copy_(t)
+        assert moved.data_ptr() % 128 == 16
+        setattr(s, name, moved)
+    h = s.handle()
+    out, lse = attend(s, h, window, 4 if window else 0, times=2)
+    assert h.last_path() == paths[0]
+    s.check_attend(out, lse, window, 4 if window else 0, rounded_weights=paths[0] != "simt")
+    weigh_and_check(s, h, None, window, 4 if window else 0)
+    assert h.last_path() == paths[1]
+
+
+@pytest.mark.parametrize("n", [1, 17, 130])
+@pytest.mark.parametrize("off", [8, 64])
+def test_query_rows_off_128_bytes(n, off):
+    """Query rows that do not start on 128 bytes are copied by a warp; on 128 bytes they come by TMA: the same bits."""
+    import torch
+
+    s = Setup(n, [700, 333], [n] * 2, 8, 2, 128, 16, ragged=False)
+    h = s.handle()
+    out, lse = attend(s, h)
+    room = torch.zeros(s.T, s.Hq * s.D + 128, dtype=s.dt, device="cuda")
+    rows = room[:, off : off + s.Hq * s.D]
+    rows.copy_(s.q)
+    s.q = rows
+    again, lse2 = attend(s, h)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)
