@@ -5,3 +5,4 @@ from .binding import (  # noqa: F401
     AjError, Handle, lib, status_string, version, verify_static, AJ_STATIC_MAX_ROWS, pair_schedule, shard_exchange_bytes, shard_exchange_alloc, shard_exchange_free, shard_range, ipc_export, ipc_import, ipc_close, lr_fit, lr_release,
 )
 from .kv import AJ_KV_FLAG_FORCE_SIMT, KvHandle  # noqa: F401
+from .score import AJ_E4M3, AJ_SCORE_FLAG_FORCE_SIMT, AJ_SCORE_MAX_TOKENS, AJ_SCORE_MAX_TOP, ScoreHandle, add_norm  # noqa: F401

@@ -1,0 +1,59 @@
+// Declarations shared by the scoring kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include "aj_internal.cuh"
+
+namespace aj {
+namespace score {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+enum { BF16 = 0, F32 = 1, E4M3 = 2 };  // aj_dtype and AJ_E4M3
+
+// Rows whose logits the workspace holds at once: ten row tiles of the two-SM kernel, 1.3 GB at 128,256 entries.
+constexpr int GROUP_ROWS = 2560;
+
+// One group of rows on its way through a call.
+struct Args {
+    const void *h = nullptr, *W = nullptr;
+    const float *h_scale = nullptr, *w_scale = nullptr;
+    const int *tokens = nullptr;
+    long long h_stride = 0;
+    int rows = 0, d = 0, V = 0, n_tok = 0, n_top = 0, dtype = 0;
+    float inv_t = 1.0f;
+    float *logprob = nullptr, *lse = nullptr, *entropy = nullptr, *top_logprob = nullptr;
+    int *top_id = nullptr;
+    // workspace
+    float *logits = nullptr;   // [rows][ld]
+    float4 *parts = nullptr;   // [rows][n_v]: a tile's largest logit, S = sum 2^d and T = sum d 2^d, d = (logit - largest) * c
+    long long ld = 0;
+    int tile = 0, n_v = 0;     // entries per tile, tiles
+    int *status = nullptr;
+};
+
+cudaError_t launch_simt(const Args &a, cudaStream_t s);
+cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s);
+cudaError_t prepare_finish();
+// The finishing kernel keeps a key per tile and AJ_SCORE_MAX_TOP tiles of logits in shared memory (64 + 128 KB at most).
+constexpr int MAX_TILES = 8192, MAX_V = MAX_TILES * 256;
+
+#ifdef __CUDACC__
+
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ inline float max_nan(float a, float b) {  // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+#endif
+
+}  // namespace score
+}  // namespace aj
