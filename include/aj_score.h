@@ -69,7 +69,7 @@ aj_status aj_score_destroy(aj_score h);
  *   top_id [rows, n_top] int32, top_logprob [rows, n_top] f32 (n_top 0: both NULL; top_logprob optional)
  * Logits, maxima and sums are in 32 bits.  A row with a NaN or an infinite largest logit gets NaN in every f32 output, and
  * alternatives in [0, V) of no meaning.  Two runs on the same inputs give the same bits.  rows may be 0.
- * The tensor cores take AJ_BF16 and AJ_E4M3 where h and W start on 16 bytes and their rows are whole 16-byte pieces; all else
+ * The tensor cores take AJ_BF16 and AJ_E4M3 where h, W and w_scale start on 16 bytes and rows are whole 16-byte pieces; all else
  * goes to the CUDA cores, many times slower.
  * Errors: AJ_ERR_INVALID_ARG, AJ_ERR_WORKSPACE (rows or n_top above the handle's), AJ_ERR_CUDA.
  */

@@ -34,6 +34,17 @@ struct Args {
     int *status = nullptr;
 };
 
+// How the tcgen05 kernel cuts a group of rows.
+struct Plan {
+    bool pair = false;         // two SMs per tile
+    int tile = 0, n_v = 0, n_m = 0;  // entries per tile, tiles of entries, tiles of rows
+    int box_rows = 0, num_kb = 0, stages = 0, grid = 0;
+};
+cudaError_t prepare_umma(int num_sms, int *max_pairs);
+int one_sm_tile(int V, int num_sms);
+Plan plan_umma(int rows, int d, int V, int dtype, int tile, int num_sms, int max_pairs);
+// maps: h in boxes of box_rows, W in boxes of a CTA's share of a tile, both 128 bytes wide with 128-byte swizzle
+cudaError_t launch_umma(const CUtensorMap &mh, const CUtensorMap &mw, const Args &a, const Plan &p, cudaStream_t s);
 cudaError_t launch_simt(const Args &a, cudaStream_t s);
 cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s);
 cudaError_t prepare_finish();

@@ -9,12 +9,23 @@
 
 using namespace aj;
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+typedef CUresult (*ReplaceAddressFn)(CUtensorMap *, void *);
+
 struct aj_score_s {
-    int device = 0, num_sms = 0;
+    int device = 0, num_sms = 0, max_pairs = 0;
     int max_rows = 0, group = 0, d = 0, V = 0, dtype = 0, max_top = 0;
     unsigned flags = 0;
-    int tile = 0, n_v = 0;   // entries per tile of the workspace's layout, tiles
-    long long ld = 0;        // entries of a row of the workspace
+    int tile = 0;            // entries per tile of the one-SM kernel
+    bool tensor = false;     // a type and a width that the tensor-core kernels take
+    EncodeTiledFn encode = nullptr;
+    ReplaceAddressFn replace = nullptr;
+    // tensor maps of W for tiles of both kernels, and of the last call's shape of h: a call puts its addresses in
+    CUtensorMap w_one = {}, w_pair = {}, rows = {};
+    long long rows_stride = -1;
+    int rows_n = 0, rows_box = 0;
     float *logits = nullptr;
     float4 *parts = nullptr;
     int *status = nullptr;
@@ -48,6 +59,30 @@ aj_status done(cudaError_t e) {
     if (e == cudaSuccess) return AJ_OK;
     cudaGetLastError();
     return AJ_ERR_CUDA;
+}
+
+// A tensor map of n rows of the handle's width, boxes of 128 bytes x box rows, 128-byte swizzle; zeros past the last row and column.
+bool encode(aj_score h, CUtensorMap *m, void *any, long long n, long long stride, int box_rows) {
+    const int e = h->dtype == AJ_BF16 ? 2 : 1;
+    const cuuint64_t dims[2] = {(cuuint64_t)h->d, (cuuint64_t)n};
+    const cuuint64_t strides[1] = {(cuuint64_t)stride * e};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / e), (cuuint32_t)box_rows}, one[2] = {1, 1};
+    return h->encode(m, e == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, any, dims, strides, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool at_address(aj_score h, CUtensorMap *m, const CUtensorMap &from, const void *p) {
+    *m = from;
+    return h->replace(m, const_cast<void *>(p)) == CUDA_SUCCESS;
+}
+
+template <typename F> bool driver_entry(const char *name, F *out) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion(name, &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess || !fn) return false;
+    *out = reinterpret_cast<F>(fn);
+    return true;
 }
 
 int elem(int dtype) { return dtype == AJ_BF16 ? 2 : dtype == AJ_F32 ? 4 : 1; }
@@ -116,7 +151,8 @@ aj_status aj_score_create(aj_score *out, int device, int max_rows, int d, int V,
     if (major != 10) return AJ_ERR_NOT_SM100;
     Guard guard(device);
     if (!guard.ok()) return AJ_ERR_CUDA;
-    if (score::prepare_finish() != cudaSuccess) {
+    int max_pairs = 0;
+    if (score::prepare_finish() != cudaSuccess || score::prepare_umma(sms, &max_pairs) != cudaSuccess) {
         cudaGetLastError();
         return AJ_ERR_CUDA;
     }
@@ -131,12 +167,24 @@ aj_status aj_score_create(aj_score *out, int device, int max_rows, int d, int V,
     h->dtype = dtype;
     h->max_top = max_top;
     h->flags = flags;
-    h->tile = 256;
-    h->n_v = (V + h->tile - 1) / h->tile;
-    h->ld = (long long)h->n_v * h->tile;
-    if (cudaMalloc(&h->logits, (size_t)h->group * h->ld * 4) != cudaSuccess || cudaMalloc(&h->parts, (size_t)h->group * h->n_v * 16) != cudaSuccess ||
+    h->max_pairs = max_pairs;
+    h->tile = score::one_sm_tile(V, sms);
+    h->tensor = dtype != AJ_F32 && (long long)d * elem(dtype) % 16 == 0 && !(flags & AJ_SCORE_FLAG_FORCE_SIMT);
+    if (h->tensor && (!driver_entry("cuTensorMapEncodeTiled", &h->encode) || !driver_entry("cuTensorMapReplaceAddress", &h->replace))) {
+        cudaGetLastError();
+        delete h;
+        return AJ_ERR_CUDA;
+    }
+    // up to 128 rows in the one-SM kernel's tiles, or all of a group in tiles of 256: a row is whole tiles, so less than one more than V
+    const size_t few = h->group < 128 ? h->group : 128, n_one = (V + h->tile - 1) / h->tile, n_wide = (V + 255) / 256;
+    const size_t parts = few * n_one > h->group * n_wide ? few * n_one : h->group * n_wide;
+    if (cudaMalloc(&h->logits, (size_t)h->group * (V + 255) * 4) != cudaSuccess || cudaMalloc(&h->parts, parts * 16) != cudaSuccess ||
         cudaMalloc(&h->status, 256) != cudaSuccess || zero_now(h->status, 256) != cudaSuccess) {
         cudaGetLastError();
+        aj_score_destroy(h);
+        return AJ_ERR_CUDA;
+    }
+    if (h->tensor && (!encode(h, &h->w_one, h->logits, V, d, h->tile) || !encode(h, &h->w_pair, h->logits, V, d, 128))) {
         aj_score_destroy(h);
         return AJ_ERR_CUDA;
     }
@@ -170,6 +218,7 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
     Guard guard(h->device);
     if (!guard.ok()) return AJ_ERR_CUDA;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const bool tensor = h->tensor && !off(hidden, 16) && !off(W, 16) && (rows == 1 || h_stride * e % 16 == 0) && !off(w_scale, 16);
     // groups of rows, evenly
     const int n_groups = (rows + h->group - 1) / h->group, each = (rows + n_groups - 1) / n_groups;
     for (int r0 = 0; r0 < rows; r0 += each) {
@@ -194,15 +243,33 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
         a.top_logprob = n_top && top_logprob ? top_logprob + (size_t)r0 * n_top : nullptr;
         a.logits = h->logits;
         a.parts = h->parts;
-        a.ld = h->ld;
-        a.tile = h->tile;
-        a.n_v = h->n_v;
         a.status = h->status;
-        h->last_path = "simt";
-        cudaError_t err = score::launch_simt(a, s);
-        if (err == cudaSuccess) err = score::launch_finish(a, false, s);
+        cudaError_t err;
+        if (tensor) {
+            const score::Plan p = score::plan_umma(a.rows, h->d, h->V, h->dtype, h->tile, h->num_sms, h->max_pairs);
+            a.tile = p.tile;
+            a.n_v = p.n_v;
+            a.ld = (long long)p.n_v * p.tile;
+            if (h->rows_stride != h_stride || h->rows_n != a.rows || h->rows_box != p.box_rows) {
+                h->rows_stride = -1;
+                if (!encode(h, &h->rows, h->logits, a.rows, a.rows > 1 ? h_stride : h->d, p.box_rows)) return AJ_ERR_CUDA;
+                h->rows_stride = h_stride, h->rows_n = a.rows, h->rows_box = p.box_rows;
+            }
+            CUtensorMap mh, mw;
+            if (!at_address(h, &mh, h->rows, a.h) || !at_address(h, &mw, p.pair ? h->w_pair : h->w_one, W)) return AJ_ERR_CUDA;
+            h->last_path = p.pair ? "umma_two_sm" : "umma_one_sm";
+            err = score::launch_umma(mh, mw, a, p, s);
+            h->last_launches += 2;
+        } else {
+            a.tile = 256;
+            a.n_v = (h->V + 255) / 256;
+            a.ld = (long long)a.n_v * a.tile;
+            h->last_path = "simt";
+            err = score::launch_simt(a, s);
+            h->last_launches += 3;
+        }
+        if (err == cudaSuccess) err = score::launch_finish(a, tensor, s);
         if (err != cudaSuccess) return done(err);
-        h->last_launches += 3;
     }
     return AJ_OK;
 }
