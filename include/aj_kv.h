@@ -94,6 +94,28 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
                        void *cuda_stream);
 
 /*
+ * Attention of a batch whose sequences share their first slots (few-shot examples, a system prompt, a document), which are
+ * read once for all of them instead of once for each.  The result is that of aj_kv_attend with window 0, up to the order in
+ * which the sums are added:
+ *   m = max(m1, m2),  out = (e^(m1 - m) O1 + e^(m2 - m) O2) / (e^(m1 - m) l1 + e^(m2 - m) l2)
+ * with O, l, m the weighted values, their sum and the maximum over the shared slots (1) and over a sequence's others (2), f32.
+ *   shared        slots 0 .. shared - 1 of the sequences hold the same tokens (whole tiles of 128 of them are used together)
+ *   shared_table  [shared / page_size, rounded up] int32: their pages
+ * A sequence with at least `shared` slots before its new tokens is taken to share them.  Any other (a shorter one, one
+ * of a padded batch) is attended by its own table alone; block_table names every page of a sequence, the shared ones too.
+ * aj_kv_reserve_shared(h, max_rows) sets aside a workspace for max_rows new tokens of a call ((D + 2) * Hq * 4 bytes each), frees an
+ * earlier one and may wait for the device; 0 frees.  Sequences of a ragged call whose tokens lie past max_rows are attended alone.
+ * f32, head sizes other than 64 and 128, Hq / Hkv > 128, pages off 128 bytes, one sequence, or less than 128 shared
+ * slots: aj_kv_attend's kernels do the whole call, nothing is shared and nothing need be reserved.
+ * Errors: as aj_kv_attend; AJ_ERR_WORKSPACE also for B * n_q rows above max_rows.
+ */
+aj_status aj_kv_reserve_shared(aj_kv h, int max_rows);
+aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const void *k_pages, const void *v_pages, int n_pages,
+                              const int32_t *shared_table, int shared, const int32_t *block_table, int table_width,
+                              const int32_t *seq_lens, const int32_t *q_start, int B, int n_q, float scale, void *out,
+                              long long out_stride, float *lse, void *cuda_stream);
+
+/*
  * Accumulated attention weight: weight_out[b, h, j] = weight[b, h, j] + sum over the counted new tokens t that see
  * slot j, and the query heads of key head h, of exp(scale * q k_j - lse).
  *   lse [rows, Hq]: what aj_kv_attend gave for the same q, window and sinks

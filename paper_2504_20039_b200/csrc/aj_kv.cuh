@@ -19,10 +19,14 @@ struct View {
     int B = 0, n_q = 0, width = 0, n_pages = 0, cap = 0;
     int Hq = 0, Hkv = 0, G = 0, D = 0, page = 0, page_shift = 0;
     int window = 0, sinks = 0;
+    // A batch that shares its first slots (whole tiles of 128) is attended in two passes.  The prefix pass takes the new tokens of
+    // all n_seq sequences as one sequence's, whose tokens see all of the shared slots; the second pass leaves those slots out.
+    int shared = 0, prefix = 0, n_seq = 0, total = 0, pre_rows = 0;  // total: rows without q_start; pre_rows: rows that the results have room for
 };
 
 struct Seq {
     int row0, nq, L;  // first row of q, new tokens, slots in use
+    int first = 0;    // slots below this one are the prefix pass's
 };
 
 struct AttendArgs {
@@ -32,6 +36,7 @@ struct AttendArgs {
     float *lse = nullptr;
     long long q_stride = 0, out_stride = 0;
     float scale_log2 = 0;        // scale * log2(e): scores are kept in units of log2
+    float *pre = nullptr;        // the prefix pass's results, see pre_o
     float *parts = nullptr;      // partial results (unnormalised output, maximum, sum)
     unsigned *counters = nullptr;  // zero between launches: splits of an item that have arrived
     size_t parts_floats = 0;
@@ -113,8 +118,36 @@ template <typename K> cudaError_t allow_shared(K kernel) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
 }
 
+// The rows that the prefix pass takes: those of all sequences, as far as its results have room.
+struct Rows {
+    int base, n;
+};
+__device__ inline Rows rows_of(const View &v) {
+    Rows r;
+    r.base = v.q_start ? __ldg(v.q_start) : 0;
+    r.n = min(max(v.q_start ? __ldg(v.q_start + v.n_seq) - r.base : v.total, 0), v.pre_rows);
+    return r;
+}
+// Place of a row's (h, query head g of the key head) results of the prefix pass: element d at pre_o(.., d), for d a multiple of
+// four; maximum and sum behind them.  Rows are neighbours, so threads that own rows read and write whole lines.
+__device__ inline float *pre_o(const AttendArgs &a, int h, int row, int g, int d) {
+    const size_t rg = (size_t)a.v.pre_rows * a.v.G;
+    return a.pre + (((size_t)h * (a.v.D >> 2) + (d >> 2)) * rg + (size_t)row * a.v.G + g) * 4;
+}
+__device__ inline float *pre_ml(const AttendArgs &a, int h, int row, int g) {
+    const size_t rg = (size_t)a.v.pre_rows * a.v.G;
+    return a.pre + ((size_t)a.v.Hkv * a.v.D * rg) + ((size_t)h * rg + (size_t)row * a.v.G + g) * 2;
+}
+
 __device__ inline Seq seq_of(const View &v, int b) {
     Seq s;
+    if (v.prefix) {
+        const Rows r = rows_of(v);
+        s.row0 = r.base;
+        s.nq = r.n;
+        s.L = v.shared;
+        return s;
+    }
     s.L = min(max(__ldg(v.lens + b), 0), v.cap);
     if (v.q_start) {
         s.row0 = __ldg(v.q_start + b);
@@ -122,6 +155,10 @@ __device__ inline Seq seq_of(const View &v, int b) {
     } else {
         s.row0 = b * v.n_q;
         s.nq = v.n_q;
+    }
+    if (v.shared) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
+        const Rows r = rows_of(v);
+        if (s.L - s.nq >= v.shared && s.row0 >= r.base && s.nq <= r.n && s.row0 - r.base <= r.n - s.nq) s.first = v.shared;
     }
     return s;
 }

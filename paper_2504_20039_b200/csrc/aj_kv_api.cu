@@ -23,6 +23,8 @@ struct aj_kv_s {
     unsigned *counters = nullptr;  // [n_counters] attention items, then [max_B] eviction
     int n_counters = 0;
     int *status = nullptr;
+    float *pre = nullptr;          // aj_kv_reserve_shared: the prefix pass's results, and its own partial results where the handle had no room
+    int pre_rows = 0;
     int clusters[4] = {};          // see prepare_evict
     EncodeTiledFn encode = nullptr;
     ReplaceAddressFn replace = nullptr;
@@ -122,6 +124,54 @@ bool at_address(aj_kv h, CUtensorMap *m, const CUtensorMap &from, const void *p)
     return h->replace(m, const_cast<void *>(p)) == CUDA_SUCCESS;
 }
 
+kv::AttendArgs attend_args(aj_kv h, const void *q, long long q_stride, const void *k_pages, const void *v_pages, float scale, void *out,
+                           long long out_stride, float *lse) {
+    kv::AttendArgs a;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.k = k_pages;
+    a.vv = v_pages;
+    a.out = out;
+    a.out_stride = out_stride;
+    a.lse = lse;
+    a.scale_log2 = scale * kv::LOG2E;
+    a.parts = h->parts;
+    a.parts_floats = h->parts_floats;
+    a.counters = h->counters;
+    a.n_counters = h->n_counters;
+    a.status = h->status;
+    return a;
+}
+
+// The tensor maps of a call of the tcgen05 kernel.
+bool attend_maps(aj_kv h, const kv::AttendArgs &a, CUtensorMap (&maps)[4], int *q_tma) {
+    if (!at_address(h, &maps[0], h->pages, a.k) || !at_address(h, &maps[1], h->pages, a.vv)) return false;
+    // queries by TMA (boxes of eight tokens where a tile has as many, and of one), or by one warp's 16-byte copies where their
+    // rows do not lie on 128 bytes: 64 windows of 33 rows 157 us and 209, a prompt of 8192 490 and 647
+    const int tma = *q_tma = !on128(a.q, a.q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
+    if (tma && a.q_stride != h->q_stride) {
+        h->q_stride = -1;
+        if (!encode_rows(h, &h->rows1, h->parts, a.q_stride, 1) || (tma == 8 && !encode_rows(h, &h->rows8, h->parts, a.q_stride, 8))) return false;
+        h->q_stride = a.q_stride;
+    }
+    return !tma || (at_address(h, &maps[2], h->rows1, a.q) && (tma != 8 || at_address(h, &maps[3], h->rows8, a.q)));
+}
+
+// What the tcgen05 kernels need beside the handle's workspace.
+bool prepare_maps(aj_kv h) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess || !fn)
+        return false;
+    h->encode = reinterpret_cast<EncodeTiledFn>(fn);
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapReplaceAddress", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess || !fn)
+        return false;
+    h->replace = reinterpret_cast<ReplaceAddressFn>(fn);
+    return true;
+}
+
 aj_status done(cudaError_t e) {
     if (e == cudaSuccess) return AJ_OK;
     cudaGetLastError();
@@ -187,23 +237,10 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     if (h->tensor && kv::few_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::few_parts_floats(D, sms);
     const bool many = h->tensor && (long long)max_q * G > kv::FEW_ROWS;  // calls for the tcgen05 kernels
     if (many && G <= 128 && kv::umma_parts_floats(D, sms) > h->parts_floats) h->parts_floats = kv::umma_parts_floats(D, sms);
-    if (many) {
-        void *fn = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess || !fn) {
-            cudaGetLastError();
-            delete h;
-            return AJ_ERR_CUDA;
-        }
-        h->encode = reinterpret_cast<EncodeTiledFn>(fn);
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapReplaceAddress", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess || !fn) {
-            cudaGetLastError();
-            delete h;
-            return AJ_ERR_CUDA;
-        }
-        h->replace = reinterpret_cast<ReplaceAddressFn>(fn);
+    if (many && !prepare_maps(h)) {
+        cudaGetLastError();
+        delete h;
+        return AJ_ERR_CUDA;
     }
     const size_t n = (size_t)h->n_counters + max_B;
     if (cudaMalloc(&h->parts, h->parts_floats * 4) != cudaSuccess || cudaMalloc(&h->counters, n * 4) != cudaSuccess ||
@@ -227,6 +264,7 @@ aj_status aj_kv_destroy(aj_kv h) {
     cudaFree(h->parts);
     cudaFree(h->counters);
     cudaFree(h->status);
+    cudaFree(h->pre);
     delete h;
     return AJ_OK;
 }
@@ -284,21 +322,8 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     if (off16(v_pages)) return AJ_ERR_UNSUPPORTED;
     Guard guard(h->device);
     if (!guard.ok()) return AJ_ERR_CUDA;
-    kv::AttendArgs a;
+    kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
     a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, window, sinks);
-    a.q = q;
-    a.q_stride = q_stride;
-    a.k = k_pages;
-    a.vv = v_pages;
-    a.out = out;
-    a.out_stride = out_stride;
-    a.lse = lse;
-    a.scale_log2 = scale * kv::LOG2E;
-    a.parts = h->parts;
-    a.parts_floats = h->parts_floats;
-    a.counters = h->counters;
-    a.n_counters = h->n_counters;
-    a.status = h->status;
     h->last_launches = 1;
     if (h->tensor && n_q * a.v.G <= kv::FEW_ROWS) {
         h->last_path = "few";
@@ -307,21 +332,95 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     if (h->tensor && a.v.G <= 128 && on128(k_pages) && on128(v_pages)) {  // (swizzled boxes want 128-byte rows; else the CUDA cores)
         h->last_path = "umma";
         CUtensorMap maps[4];
-        if (!at_address(h, &maps[0], h->pages, k_pages) || !at_address(h, &maps[1], h->pages, v_pages)) return AJ_ERR_CUDA;
-        // queries by TMA (boxes of eight tokens where a tile has as many, and of one), or by one warp's 16-byte copies where their
-        // rows do not lie on 128 bytes: 64 windows of 33 rows 157 us and 209, a prompt of 8192 490 and 647
-        const int q_tma = !on128(q, q_stride * 2) ? 0 : 128 / a.v.G >= 8 ? 8 : 1;
-        if (q_tma && q_stride != h->q_stride) {
-            h->q_stride = -1;
-            if (!encode_rows(h, &h->rows1, h->parts, q_stride, 1) || (q_tma == 8 && !encode_rows(h, &h->rows8, h->parts, q_stride, 8))) return AJ_ERR_CUDA;
-            h->q_stride = q_stride;
-        }
-        if (q_tma && (!at_address(h, &maps[2], h->rows1, q) || (q_tma == 8 && !at_address(h, &maps[3], h->rows8, q)))) return AJ_ERR_CUDA;
-        h->last_launches = 1;
+        int q_tma;
+        if (!attend_maps(h, a, maps, &q_tma)) return AJ_ERR_CUDA;
         return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, (cudaStream_t)cuda_stream));
     }
     h->last_path = "simt";
     return done(kv::launch_attend_simt(a, h->dtype == AJ_BF16, h->num_sms, (cudaStream_t)cuda_stream));
+}
+
+aj_status aj_kv_reserve_shared(aj_kv h, int max_rows) {
+    if (!h || max_rows < 0 || (long long)max_rows * h->Hq > (1ll << 30)) return AJ_ERR_INVALID_ARG;
+    Guard guard(h->device);
+    if (!guard.ok()) return AJ_ERR_CUDA;
+    if (!h->tensor || h->Hq / h->Hkv > 128 || max_rows == 0) {  // nothing to reserve: calls attend sequence by sequence
+        cudaFree(h->pre);
+        h->pre = nullptr;
+        h->pre_rows = 0;
+        return AJ_OK;
+    }
+    // the prefix pass always runs on the tcgen05 kernel, which a handle for single tokens was not made for
+    if (!h->encode) {
+        if (!prepare_maps(h) || !encode_pages(h, h->parts)) {
+            h->encode = nullptr;
+            cudaGetLastError();
+            return AJ_ERR_CUDA;
+        }
+    }
+    float *pre = nullptr, *parts = nullptr;
+    const size_t rows = (size_t)max_rows * h->Hq, need = kv::umma_parts_floats(h->D, h->num_sms);
+    if (cudaMalloc(&pre, rows * (h->D + 2) * 4) != cudaSuccess || (need > h->parts_floats && cudaMalloc(&parts, need * 4) != cudaSuccess)) {
+        cudaGetLastError();
+        cudaFree(pre);
+        return AJ_ERR_CUDA;
+    }
+    cudaFree(h->pre);
+    h->pre = pre;
+    h->pre_rows = max_rows;
+    if (parts) {
+        cudaFree(h->parts);
+        h->parts = parts;
+        h->parts_floats = need;
+    }
+    return AJ_OK;
+}
+
+aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const void *k_pages, const void *v_pages, int n_pages,
+                              const int32_t *shared_table, int shared, const int32_t *block_table, int table_width, const int32_t *seq_lens,
+                              const int32_t *q_start, int B, int n_q, float scale, void *out, long long out_stride, float *lse,
+                              void *cuda_stream) {
+    aj_status st = check_view(h, k_pages, n_pages, block_table, table_width, seq_lens, B, n_q);
+    if (st != AJ_OK) return st;
+    if (shared < 0 || shared > (long long)table_width * h->page || (shared > 0 && !shared_table)) return AJ_ERR_INVALID_ARG;
+    const int whole = shared / 128 * 128;  // tiles that are shared to their end
+    if (!h->tensor || h->Hq / h->Hkv > 128 || !on128(k_pages) || !on128(v_pages) || whole == 0 || B == 1)
+        return aj_kv_attend(h, q, q_stride, k_pages, v_pages, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, scale, 0, 0, out, out_stride,
+                            lse, cuda_stream);
+    if (!v_pages || !(scale > 0.0f) || !(scale < 1e30f)) return AJ_ERR_INVALID_ARG;
+    if ((st = check_rows(h, q, q_stride, h->Hq)) != AJ_OK || (st = check_rows(h, out, out_stride, h->Hq)) != AJ_OK) return st;
+    if (h->pre_rows == 0 || (!q_start && (long long)B * n_q > h->pre_rows)) return AJ_ERR_WORKSPACE;
+    Guard guard(h->device);
+    if (!guard.ok()) return AJ_ERR_CUDA;
+    kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
+    a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, 0, 0);
+    a.v.shared = whole;
+    a.v.n_seq = B;
+    a.v.total = B * n_q;
+    a.v.pre_rows = h->pre_rows;
+    a.pre = h->pre;
+    CUtensorMap maps[4];
+    int q_tma;
+    if (!attend_maps(h, a, maps, &q_tma)) return AJ_ERR_CUDA;
+    kv::AttendArgs p = a;
+    p.v.prefix = 1;
+    p.v.B = 1;
+    p.v.n_q = a.v.total < h->pre_rows ? a.v.total : h->pre_rows;
+    p.v.table = shared_table;
+    p.v.width = (shared + h->page - 1) / h->page;
+    p.v.cap = p.v.width * h->page;
+    p.out = nullptr;
+    p.lse = nullptr;
+    h->last_launches = 2;
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const cudaError_t e = kv::launch_attend_umma(p, maps, q_tma, h->num_sms, s);
+    if (e != cudaSuccess) return done(e);
+    if (n_q * a.v.G <= kv::FEW_ROWS) {
+        h->last_path = "shared_few";
+        return done(kv::launch_attend_few(a, h->num_sms, s));
+    }
+    h->last_path = "shared_umma";
+    return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, s));
 }
 
 aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *lse, const void *k_pages, int n_pages,

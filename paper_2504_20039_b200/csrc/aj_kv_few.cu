@@ -34,7 +34,7 @@ struct Span {
 };
 __device__ inline Span span_of(const View &v, const Seq &s) {
     Span r;
-    r.first = v.window ? max(0, s.L - s.nq - v.window + 1) : 0;
+    r.first = v.window ? max(0, s.L - s.nq - v.window + 1) : s.first;
     r.first = min(r.first, s.L);
     r.first_blk = r.first / BLK;
     r.n_sink = min((min(v.sinks, r.first) + BLK - 1) / BLK, r.first_blk);
@@ -297,6 +297,18 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                     }
                 }
             auto store = [&](int r, int d, float4 x, float mm, float ll) {  // four elements of an output row
+                if (v.shared && cur.s.first) {  // the prefix's part
+                    const int at = cur.s.row0 - rows_of(v).base + r / v.G, g = r % v.G;
+                    const float2 ml = *reinterpret_cast<const float2 *>(pre_ml(a, cur.h, at, g));
+                    const float4 y = *reinterpret_cast<const float4 *>(pre_o(a, cur.h, at, g, d));
+                    const float top = fmaxf(mm, ml.x), ref = top == -INFINITY ? 0.0f : top, c0 = ex2(mm - ref), c1 = ex2(ml.x - ref);
+                    x.x = c0 * x.x + c1 * y.x;
+                    x.y = c0 * x.y + c1 * y.y;
+                    x.z = c0 * x.z + c1 * y.z;
+                    x.w = c0 * x.w + c1 * y.w;
+                    ll = c0 * ll + c1 * ml.y;
+                    mm = top;
+                }
                 const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
                 const size_t row = (size_t)cur.s.row0 + r / v.G;
                 const int head = cur.h * v.G + r % v.G;

@@ -11,7 +11,7 @@ from .binding import AJ_BF16, AJ_ERR_INVALID_ARG, AJ_OK, AjError
 
 AJ_KV_FLAG_FORCE_SIMT = 1
 
-EXPORTS = ("aj_kv_create", "aj_kv_destroy", "aj_kv_append", "aj_kv_attend", "aj_kv_weigh", "aj_kv_evict", "aj_kv_last_status",
+EXPORTS = ("aj_kv_create", "aj_kv_destroy", "aj_kv_append", "aj_kv_attend", "aj_kv_reserve_shared", "aj_kv_attend_shared", "aj_kv_weigh", "aj_kv_evict", "aj_kv_last_status",
            "aj_kv_last_launch_count", "aj_kv_last_path")
 
 _vp, _ci, _cf, _cl, _cu = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_longlong, ctypes.c_uint
@@ -21,6 +21,8 @@ _ARGS = {
     "aj_kv_append": [_vp, _vp, _cl, _vp, _cl, _vp, _cl, _vp, _vp, _cf, _vp, _ci, _ci, _ci, _vp, _vp, _vp, _ci, _vp, _ci, _vp, _vp, _ci,
                      _ci, _vp, _cl, _vp, _vp, _vp],
     "aj_kv_attend": [_vp, _vp, _cl, _vp, _vp, _ci, _vp, _ci, _vp, _vp, _ci, _ci, _cf, _ci, _ci, _vp, _cl, _vp, _vp],
+    "aj_kv_reserve_shared": [_vp, _ci],
+    "aj_kv_attend_shared": [_vp, _vp, _cl, _vp, _vp, _ci, _vp, _ci, _vp, _ci, _vp, _vp, _ci, _ci, _cf, _vp, _cl, _vp, _vp],
     "aj_kv_weigh": [_vp, _vp, _cl, _vp, _vp, _ci, _vp, _ci, _vp, _vp, _vp, _ci, _ci, _cf, _ci, _ci, _vp, _vp, _vp],
     "aj_kv_evict": [_vp, _vp, _vp, _ci, _vp, _ci, _vp, _ci, _ci, _ci, _ci, _vp, _vp, _vp, _vp, _vp, _vp],
     "aj_kv_last_status": [_vp],
@@ -69,6 +71,7 @@ class KvHandle:
             self._h = _vp()
             raise AjError(st, "aj_kv_create")
         self._append, self._attend, self._weigh, self._evict = (f["aj_kv_" + n] for n in ("append", "attend", "weigh", "evict"))
+        self._attend_shared = f["aj_kv_attend_shared"]
         self._take(device, max_B, max_q, Hq, Hkv, D, page_size, dtype, strict)
 
     def _take(self, device, max_B, max_q, Hq, Hkv, D, page_size, dtype, strict):
@@ -144,6 +147,34 @@ class KvHandle:
                               out.data_ptr(), os[0], None if lse is None else lse.data_ptr(), stream or None)
         if check and st != AJ_OK:
             raise AjError(st, "aj_kv_attend")
+        return st
+
+    def reserve_shared(self, max_rows: int, check: bool = True) -> int:
+        """aj_kv_reserve_shared: room for max_rows new tokens of an attend_shared call."""
+        st = _lib()["aj_kv_reserve_shared"](self._h, max_rows)
+        if check and st != AJ_OK:
+            raise AjError(st, "aj_kv_reserve_shared")
+        return st
+
+    def attend_shared(self, q, k_pages, v_pages, shared_table, shared: int, block_table, seq_lens, out, B: int, n_q: int, scale: float,
+                      q_start=None, lse=None, stream: int = 0, check: bool = True) -> int:
+        """aj_kv_attend_shared: attend() for a batch whose first `shared` slots are the pages of shared_table [n] int32 for every sequence."""
+        dt, i32 = self._dtype, self._i32
+        qs, os = q.stride(), out.stride()
+        if (q.dtype is not dt or out.dtype is not dt or k_pages.dtype is not dt or v_pages.dtype is not dt or block_table.dtype is not i32
+                or seq_lens.dtype is not i32 or qs[-1] != 1 or os[-1] != 1 or not k_pages.is_contiguous() or not v_pages.is_contiguous()
+                or shared_table is not None and (shared_table.dtype is not i32 or not shared_table.is_contiguous() or shared_table.numel() * self._page < shared)
+                or lse is not None and (lse.dtype is not self._f32 or not lse.is_contiguous()) or q_start is not None and q_start.dtype is not i32
+                or self._strict and not self._fits(B, n_q, (k_pages, v_pages), block_table, ((q, self._Hq), (out, self._Hq)), q_start, ((lse, self._Hq),),
+                                                   (seq_lens,), tables=((shared_table, 0),))):
+            st = AJ_ERR_INVALID_ARG
+        else:
+            st = self._attend_shared(self._h, q.data_ptr(), qs[0], k_pages.data_ptr(), v_pages.data_ptr(), k_pages.shape[0],
+                                     None if shared_table is None else shared_table.data_ptr(), shared, block_table.data_ptr(), block_table.shape[1],
+                                     seq_lens.data_ptr(), None if q_start is None else q_start.data_ptr(), B, n_q, scale, out.data_ptr(), os[0],
+                                     None if lse is None else lse.data_ptr(), stream or None)
+        if check and st != AJ_OK:
+            raise AjError(st, "aj_kv_attend_shared")
         return st
 
     def weigh(self, q, lse, k_pages, block_table, seq_lens, weight, weight_out, B: int, n_q: int, scale: float, q_start=None, n_rows=None,
