@@ -32,8 +32,9 @@ extern "C" {
 
 typedef struct aj_kv_s *aj_kv;
 
-/* Comparison switch for tests and measurements: keep aj_kv_attend and aj_kv_weigh on the CUDA-core kernels. */
-enum { AJ_KV_FLAG_FORCE_SIMT = 1u };
+/* Comparison switches for tests and measurements: keep aj_kv_attend and aj_kv_weigh on the CUDA-core kernels; let
+ * aj_kv_attend_shared attend the shared slots together even where that is slower. */
+enum { AJ_KV_FLAG_FORCE_SIMT = 1u, AJ_KV_FLAG_FORCE_SHARED = 4u };
 
 /*
  * Create a handle for fixed head counts on CUDA device `device`.
@@ -95,7 +96,7 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
 
 /*
  * Attention of a batch whose sequences share their first slots (few-shot examples, a system prompt, a document), which are
- * read once for all of them instead of once for each.  The result is that of aj_kv_attend with window 0, up to the order in
+ * attended once for all of them instead of once for each, where that pays.  The result is that of aj_kv_attend with window 0, up to the order in
  * which the sums are added:
  *   m = max(m1, m2),  out = (e^(m1 - m) O1 + e^(m2 - m) O2) / (e^(m1 - m) l1 + e^(m2 - m) l2)
  * with O, l, m the weighted values, their sum and the maximum over the shared slots (1) and over a sequence's others (2), f32.

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libaj_verify.so")
 SOURCES = ["aj_api.cu", "aj_umma_vm.cu", "aj_umma_pair.cu", "aj_simt.cu", "aj_judge.cu", "aj_rank.cu", "aj_static.cu", "aj_lr.cu",
-           "aj_kv_api.cu", "aj_kv_append.cu", "aj_kv_simt.cu", "aj_kv_few.cu", "aj_kv_umma.cu", "aj_kv_weigh.cu", "aj_kv_weigh_umma.cu", "aj_kv_evict.cu",
+           "aj_kv_api.cu", "aj_kv_append.cu", "aj_kv_simt.cu", "aj_kv_few.cu", "aj_kv_umma.cu", "aj_kv_weigh.cu", "aj_kv_weigh_umma.cu", "aj_kv_evict.cu", "aj_kv_join.cu",
            "aj_score_api.cu", "aj_score_simt.cu", "aj_score_finish.cu", "aj_score_umma.cu", "aj_norm.cu"]
 HEADERS = ["aj_internal.cuh", "aj_ptx.cuh", os.path.join("..", "..", "include", "aj_verify.h"),
            "aj_kv.cuh", "aj_kv_line.cuh", "aj_kv_mma.cuh", "aj_kv_tc.cuh", os.path.join("..", "..", "include", "aj_kv.h"),

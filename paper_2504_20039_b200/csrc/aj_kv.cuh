@@ -13,20 +13,27 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // are far from the end of f32's range.
 constexpr float RAISE = 30.0f;
 
+constexpr int MAX_CHUNKS = 16;  // of the slots that a batch shares
+
 // What a call says about the cache and its new tokens (device pointers).
 struct View {
     const int *table = nullptr, *lens = nullptr, *q_start = nullptr;
     int B = 0, n_q = 0, width = 0, n_pages = 0, cap = 0;
     int Hq = 0, Hkv = 0, G = 0, D = 0, page = 0, page_shift = 0;
     int window = 0, sinks = 0;
-    // A batch that shares its first slots (whole tiles of 128) is attended in two passes.  The prefix pass takes the new tokens of
-    // all n_seq sequences as one sequence's, whose tokens see all of the shared slots; the second pass leaves those slots out.
-    int shared = 0, prefix = 0, n_seq = 0, total = 0, pre_rows = 0;  // total: rows without q_start; pre_rows: rows that the results have room for
+    // A batch that shares its first slots (whole tiles of 128): the shared slots are cut into chunks, and `lead` chunks come before
+    // the sequences, as sequences whose new tokens are those of the whole batch and see all of the chunk.  The sequences themselves
+    // then begin behind the shared slots.  Each leaves its unnormalised results, for aj_kv_join.cu.
+    int shared = 0, lead = 0, chunk = 0, n_chunks = 0;
+    const int *lead_table = nullptr;
+    int align = 0;  // places of the line that a CTA's share is a multiple of; 0: any
+    int n_seq = 0, total = 0, pre_rows = 0;  // sequences; rows without q_start; rows that the results have room for
 };
 
 struct Seq {
     int row0, nq, L;  // first row of q, new tokens, slots in use
-    int first = 0;    // slots below this one are the prefix pass's
+    int first = 0;    // slots below this one are left out
+    int ahead = 0;    // new tokens sit this much further on than in the last nq slots
 };
 
 struct AttendArgs {
@@ -36,7 +43,9 @@ struct AttendArgs {
     float *lse = nullptr;
     long long q_stride = 0, out_stride = 0;
     float scale_log2 = 0;        // scale * log2(e): scores are kept in units of log2
-    float *pre = nullptr;        // the prefix pass's results, see pre_o
+    float *pre = nullptr;        // unnormalised results of a shared call: [n_chunks + 1][Hkv][pre_rows * G][D], the last the sequences' own
+    float2 *pre_ml = nullptr;    // their maxima and sums, [n_chunks][Hkv][pre_rows * G]
+    float2 *own_ml = nullptr;    // the sequences' own, [rows][Hq]: a sum of -1 where a row has none
     float *parts = nullptr;      // partial results (unnormalised output, maximum, sum)
     unsigned *counters = nullptr;  // zero between launches: splits of an item that have arrived
     size_t parts_floats = 0;
@@ -85,13 +94,16 @@ cudaError_t launch_attend_simt(const AttendArgs &a, bool bf16, int num_sms, cuda
 // lengths); 20 rows and more pass the registers of the first.  Accumulating the weight: 4 rows 74 and 82 us, 16 rows 85 and
 // 87, 20 rows 90 and 88, 132 rows (8 sequences) 70 and 34.
 constexpr int FEW_ROWS = 16;
-cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap = false);
 size_t few_parts_floats(int D, int num_sms);
 // many rows: at most 128 query heads per key head; bf16, head size 64 or 128
 // maps: K pages, V pages, queries in boxes of one token and of eight; q_tma: 0 if the queries have no maps, 1 if only boxes
 // of one token fit a row tile, 8 if both do
 cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s);
 size_t umma_parts_floats(int D, int num_sms);
+// joins the results of a shared call, as a programmatic dependent of the kernel before it
+cudaError_t mark_now(float2 *own_ml, size_t n);
+cudaError_t launch_join(const AttendArgs &a, cudaStream_t s);
 cudaError_t launch_weigh_simt(const WeighArgs &a, bool bf16, cudaStream_t s);
 cudaError_t launch_weigh_umma(const WeighArgs &a, const CUtensorMap &mk, int num_sms, cudaStream_t s);
 cudaError_t launch_weigh_mma(const WeighArgs &a, int num_sms, cudaStream_t s);
@@ -118,7 +130,7 @@ template <typename K> cudaError_t allow_shared(K kernel) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
 }
 
-// The rows that the prefix pass takes: those of all sequences, as far as its results have room.
+// The rows of a shared call: those of all sequences, as far as the results have room.
 struct Rows {
     int base, n;
 };
@@ -128,26 +140,25 @@ __device__ inline Rows rows_of(const View &v) {
     r.n = min(max(v.q_start ? __ldg(v.q_start + v.n_seq) - r.base : v.total, 0), v.pre_rows);
     return r;
 }
-// Place of a row's (h, query head g of the key head) results of the prefix pass: element d at pre_o(.., d), for d a multiple of
-// four; maximum and sum behind them.  Rows are neighbours, so threads that own rows read and write whole lines.
-__device__ inline float *pre_o(const AttendArgs &a, int h, int row, int g, int d) {
-    const size_t rg = (size_t)a.v.pre_rows * a.v.G;
-    return a.pre + (((size_t)h * (a.v.D >> 2) + (d >> 2)) * rg + (size_t)row * a.v.G + g) * 4;
+// Places of a row's results: chunk (or n_chunks for the sequence's own), key head, row of the call x query heads per key head.
+__device__ inline float *pre_o(const AttendArgs &a, int chunk, int h, int rowg) {
+    return a.pre + (((size_t)chunk * a.v.Hkv + h) * ((size_t)a.v.pre_rows * a.v.G) + rowg) * a.v.D;
 }
-__device__ inline float *pre_ml(const AttendArgs &a, int h, int row, int g) {
-    const size_t rg = (size_t)a.v.pre_rows * a.v.G;
-    return a.pre + ((size_t)a.v.Hkv * a.v.D * rg) + ((size_t)h * rg + (size_t)row * a.v.G + g) * 2;
+__device__ inline float2 *pre_ml(const AttendArgs &a, int chunk, int h, int rowg) {
+    return a.pre_ml + ((size_t)chunk * a.v.Hkv + h) * ((size_t)a.v.pre_rows * a.v.G) + rowg;
 }
 
 __device__ inline Seq seq_of(const View &v, int b) {
     Seq s;
-    if (v.prefix) {
+    if (b < v.lead) {
         const Rows r = rows_of(v);
         s.row0 = r.base;
-        s.nq = r.n;
-        s.L = v.shared;
+        s.nq = s.ahead = r.n;
+        s.first = b * v.chunk;
+        s.L = min(v.shared, s.first + v.chunk);
         return s;
     }
+    b -= v.lead;
     s.L = min(max(__ldg(v.lens + b), 0), v.cap);
     if (v.q_start) {
         s.row0 = __ldg(v.q_start + b);
@@ -165,7 +176,7 @@ __device__ inline Seq seq_of(const View &v, int b) {
 
 // Number of the page that holds a slot; a number outside the pool reads page 0.
 __device__ inline int page_of(const View &v, int b, int slot) {
-    const int p = __ldg(v.table + (size_t)b * v.width + (slot >> v.page_shift));
+    const int p = __ldg((b < v.lead ? v.lead_table : v.table + (size_t)(b - v.lead) * v.width) + (slot >> v.page_shift));
     return (unsigned)p < (unsigned)v.n_pages ? p : 0;
 }
 

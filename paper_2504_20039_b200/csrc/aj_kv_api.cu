@@ -23,7 +23,10 @@ struct aj_kv_s {
     unsigned *counters = nullptr;  // [n_counters] attention items, then [max_B] eviction
     int n_counters = 0;
     int *status = nullptr;
-    float *pre = nullptr;          // aj_kv_reserve_shared: the prefix pass's results, and its own partial results where the handle had no room
+    // aj_kv_reserve_shared: results of a shared call's parts, and partial results and arrivals of the kernel over the shared slots
+    float *pre = nullptr, *pre_parts = nullptr;
+    float2 *pre_ml = nullptr, *own_ml = nullptr;
+    unsigned *pre_counters = nullptr;
     int pre_rows = 0;
     int clusters[4] = {};          // see prepare_evict
     EncodeTiledFn encode = nullptr;
@@ -157,6 +160,47 @@ bool attend_maps(aj_kv h, const kv::AttendArgs &a, CUtensorMap (&maps)[4], int *
     return !tma || (at_address(h, &maps[2], h->rows1, a.q) && (tma != 8 || at_address(h, &maps[3], h->rows8, a.q)));
 }
 
+// Into how many chunks the shared slots are cut.  An item is a chunk, a key head and a piece of up to 256 query rows: as many
+// as there are SMs, so that hardly an item spans CTAs (which costs a join by one CTA), but at most MAX_CHUNKS.
+void cut_shared(kv::View &v, int num_sms) {
+    const int tiles = v.shared / 128, per_piece = 2 * (128 / v.G);
+    const long long items = (long long)v.Hkv * ((v.pre_rows + per_piece - 1) / per_piece);
+    int n = items < num_sms ? (int)(num_sms / items) : 1;
+    if (n > kv::MAX_CHUNKS) n = kv::MAX_CHUNKS;
+    if (n > tiles) n = tiles;
+    const int each = (tiles + n - 1) / n;
+    v.chunk = each * 128;
+    v.n_chunks = (tiles + each - 1) / each;
+}
+// Is it worth the parts and their join?  Sequences that share pages read them from L2 when they are attended one by one, so what is
+// saved is the stream from L2 (few rows), or row tiles that a window does not fill (more rows).  Measured, us, together and one by
+// one: 64 tokens behind 2048 slots 65 and 88, 26 behind 7040 29 and 56, 12 behind 1088 23 and 14; 31 windows of 17 rows behind 4352
+// 66 and 85, 32 of 33 behind 1504 87 and 76, prompts behind 8192 241 and 186.
+bool worth_sharing(const kv::View &v) {
+    if (v.n_q * v.G <= kv::FEW_ROWS) return (double)(v.n_seq - 1) * v.shared * v.Hkv * v.D * 4 > 118e6;  // 20 us of the stream
+    const long long per_piece = 2 * (128 / v.G), together = (v.pre_rows + per_piece - 1) / per_piece;
+    // (of a ragged batch the host knows the sum at most: half a piece more for each sequence)
+    const long long one_by_one = v.q_start ? together + v.n_seq / 2 : v.n_seq * ((v.n_q + per_piece - 1) / per_piece);
+    return (one_by_one - together) * v.Hkv * (v.shared / 128) > 2300;  // 30 us of 148 SMs
+}
+// Rows x chunks that a workspace for max_rows rows must hold.
+int pre_capacity(aj_kv h, int max_rows) {
+    const int few = 2 * (128 * h->Hkv / h->Hq) * (h->num_sms / h->Hkv + 1);
+    return max_rows > few ? max_rows : few;
+}
+
+void free_shared(aj_kv h) {
+    cudaFree(h->pre);
+    cudaFree(h->pre_ml);
+    cudaFree(h->own_ml);
+    cudaFree(h->pre_parts);
+    cudaFree(h->pre_counters);
+    h->pre = h->pre_parts = nullptr;
+    h->pre_ml = h->own_ml = nullptr;
+    h->pre_counters = nullptr;
+    h->pre_rows = 0;
+}
+
 // What the tcgen05 kernels need beside the handle's workspace.
 bool prepare_maps(aj_kv h) {
     void *fn = nullptr;
@@ -189,7 +233,7 @@ aj_status aj_kv_create(aj_kv *out, int device, int max_B, int max_q, int Hq, int
     if (device < 0 || max_B < 1 || max_B > 4096 || max_q < 1 || max_q > (1 << 20) || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || D < 1)
         return AJ_ERR_INVALID_ARG;
     if (dtype != AJ_BF16 && dtype != AJ_F32) return AJ_ERR_INVALID_ARG;
-    if (flags & ~AJ_KV_FLAG_FORCE_SIMT) return AJ_ERR_INVALID_ARG;
+    if (flags & ~(AJ_KV_FLAG_FORCE_SIMT | AJ_KV_FLAG_FORCE_SHARED)) return AJ_ERR_INVALID_ARG;
     if (D % 8 != 0 || D > 256 || Hq > 1024 || (long long)max_B * Hkv > 65535) return AJ_ERR_UNSUPPORTED;
     if (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128) return AJ_ERR_UNSUPPORTED;
     if ((long long)max_B * max_q * Hq > (1ll << 30)) return AJ_ERR_UNSUPPORTED;
@@ -264,7 +308,7 @@ aj_status aj_kv_destroy(aj_kv h) {
     cudaFree(h->parts);
     cudaFree(h->counters);
     cudaFree(h->status);
-    cudaFree(h->pre);
+    free_shared(h);
     delete h;
     return AJ_OK;
 }
@@ -345,12 +389,10 @@ aj_status aj_kv_reserve_shared(aj_kv h, int max_rows) {
     Guard guard(h->device);
     if (!guard.ok()) return AJ_ERR_CUDA;
     if (!h->tensor || h->Hq / h->Hkv > 128 || max_rows == 0) {  // nothing to reserve: calls attend sequence by sequence
-        cudaFree(h->pre);
-        h->pre = nullptr;
-        h->pre_rows = 0;
+        free_shared(h);
         return AJ_OK;
     }
-    // the prefix pass always runs on the tcgen05 kernel, which a handle for single tokens was not made for
+    // the shared slots always go to the tcgen05 kernel, which a handle for single tokens was not made for
     if (!h->encode) {
         if (!prepare_maps(h) || !encode_pages(h, h->parts)) {
             h->encode = nullptr;
@@ -358,21 +400,24 @@ aj_status aj_kv_reserve_shared(aj_kv h, int max_rows) {
             return AJ_ERR_CUDA;
         }
     }
-    float *pre = nullptr, *parts = nullptr;
-    const size_t rows = (size_t)max_rows * h->Hq, need = kv::umma_parts_floats(h->D, h->num_sms);
-    if (cudaMalloc(&pre, rows * (h->D + 2) * 4) != cudaSuccess || (need > h->parts_floats && cudaMalloc(&parts, need * 4) != cudaSuccess)) {
+    const size_t heads = (size_t)pre_capacity(h, max_rows) * h->Hq, own = (size_t)max_rows * h->Hq;
+    aj_kv_s n;  // the new workspace
+    n.pre_rows = max_rows;
+    if (cudaMalloc(&n.pre, (heads + own) * h->D * 4) != cudaSuccess || cudaMalloc(&n.pre_ml, heads * 8) != cudaSuccess ||
+        cudaMalloc(&n.own_ml, own * 8) != cudaSuccess || cudaMalloc(&n.pre_parts, kv::umma_parts_floats(h->D, h->num_sms) * 4) != cudaSuccess ||
+        cudaMalloc(&n.pre_counters, (size_t)h->num_sms * 8) != cudaSuccess || zero_now(n.pre_counters, (size_t)h->num_sms * 8) != cudaSuccess ||
+        kv::mark_now(n.own_ml, own) != cudaSuccess) {
         cudaGetLastError();
-        cudaFree(pre);
+        free_shared(&n);
         return AJ_ERR_CUDA;
     }
-    cudaFree(h->pre);
-    h->pre = pre;
+    free_shared(h);
+    h->pre = n.pre;
+    h->pre_ml = n.pre_ml;
+    h->own_ml = n.own_ml;
+    h->pre_parts = n.pre_parts;
+    h->pre_counters = n.pre_counters;
     h->pre_rows = max_rows;
-    if (parts) {
-        cudaFree(h->parts);
-        h->parts = parts;
-        h->parts_floats = need;
-    }
     return AJ_OK;
 }
 
@@ -395,32 +440,43 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
     kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
     a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, 0, 0);
     a.v.shared = whole;
+    a.v.lead_table = shared_table;
     a.v.n_seq = B;
     a.v.total = B * n_q;
-    a.v.pre_rows = h->pre_rows;
+    a.v.pre_rows = a.v.total < h->pre_rows ? a.v.total : h->pre_rows;
+    if (!(h->flags & AJ_KV_FLAG_FORCE_SHARED) && !worth_sharing(a.v))
+        return aj_kv_attend(h, q, q_stride, k_pages, v_pages, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, scale, 0, 0, out, out_stride,
+                            lse, cuda_stream);
+    cut_shared(a.v, h->num_sms);
     a.pre = h->pre;
+    a.pre_ml = h->pre_ml;
+    a.own_ml = h->own_ml;
     CUtensorMap maps[4];
     int q_tma;
     if (!attend_maps(h, a, maps, &q_tma)) return AJ_ERR_CUDA;
-    kv::AttendArgs p = a;
-    p.v.prefix = 1;
-    p.v.B = 1;
-    p.v.n_q = a.v.total < h->pre_rows ? a.v.total : h->pre_rows;
-    p.v.table = shared_table;
-    p.v.width = (shared + h->page - 1) / h->page;
-    p.v.cap = p.v.width * h->page;
-    p.out = nullptr;
-    p.lse = nullptr;
-    h->last_launches = 2;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
-    const cudaError_t e = kv::launch_attend_umma(p, maps, q_tma, h->num_sms, s);
-    if (e != cudaSuccess) return done(e);
+    cudaError_t e;
+    kv::AttendArgs p = a;
+    p.v.lead = a.v.n_chunks;
     if (n_q * a.v.G <= kv::FEW_ROWS) {
+        // the shared slots on the tcgen05 kernel, the sequences' own on the one for few rows, side by side: each with a workspace
         h->last_path = "shared_few";
-        return done(kv::launch_attend_few(a, h->num_sms, s));
+        h->last_launches = 3;
+        p.v.B = p.v.lead;
+        p.v.align = p.v.chunk / 128 + 2;  // whole items
+        p.v.n_q = p.v.pre_rows;
+        p.parts = h->pre_parts;
+        p.counters = h->pre_counters;
+        e = kv::launch_attend_umma(p, maps, q_tma, h->num_sms, s);
+        if (e == cudaSuccess) e = kv::launch_attend_few(a, h->num_sms, s, true);
+    } else {
+        h->last_path = "shared_umma";
+        h->last_launches = 2;
+        p.v.B = p.v.lead + B;
+        e = kv::launch_attend_umma(p, maps, q_tma, h->num_sms, s);
     }
-    h->last_path = "shared_umma";
-    return done(kv::launch_attend_umma(a, maps, q_tma, h->num_sms, s));
+    if (e == cudaSuccess) e = kv::launch_join(a, s);
+    return done(e);
 }
 
 aj_status aj_kv_weigh(aj_kv h, const void *q, long long q_stride, const float *lse, const void *k_pages, int n_pages,

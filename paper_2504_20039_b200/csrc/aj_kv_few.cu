@@ -94,7 +94,13 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
     __syncthreads();
     const int total = base, per = (total + gridDim.x - 1) / gridDim.x;
     const int u0 = min(total, (int)blockIdx.x * per), u1 = min(total, u0 + per);
-    if (u0 >= u1) return;
+    // A shared call: the kernel before it (over the shared slots) and this one run side by side; the join waits for this one only,
+    // so this one waits for the other before it ends.
+    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (u0 >= u1) {
+        if (v.shared) asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
 
     auto seek = [&](int u) {
         Cursor c;
@@ -297,17 +303,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                     }
                 }
             auto store = [&](int r, int d, float4 x, float mm, float ll) {  // four elements of an output row
-                if (v.shared && cur.s.first) {  // the prefix's part
-                    const int at = cur.s.row0 - rows_of(v).base + r / v.G, g = r % v.G;
-                    const float2 ml = *reinterpret_cast<const float2 *>(pre_ml(a, cur.h, at, g));
-                    const float4 y = *reinterpret_cast<const float4 *>(pre_o(a, cur.h, at, g, d));
-                    const float top = fmaxf(mm, ml.x), ref = top == -INFINITY ? 0.0f : top, c0 = ex2(mm - ref), c1 = ex2(ml.x - ref);
-                    x.x = c0 * x.x + c1 * y.x;
-                    x.y = c0 * x.y + c1 * y.y;
-                    x.z = c0 * x.z + c1 * y.z;
-                    x.w = c0 * x.w + c1 * y.w;
-                    ll = c0 * ll + c1 * ml.y;
-                    mm = top;
+                if (v.shared && cur.s.first) {  // a part of the row, to be joined with the shared slots'
+                    const int rr = cur.s.row0 - rows_of(v).base, rowg = rr * v.G + r;
+                    *reinterpret_cast<float4 *>(pre_o(a, v.n_chunks, cur.h, rowg) + d) = x;
+                    if (d == 0) a.own_ml[(size_t)(rr + r / v.G) * v.Hq + cur.h * v.G + r % v.G] = make_float2(mm, ll);
+                    return;
                 }
                 const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
                 const size_t row = (size_t)cur.s.row0 + r / v.G;
@@ -401,14 +401,24 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
         advance(cur);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (v.shared) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaStream_t s) {
+template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap) {
     using C = Few<D, NT>;
     const size_t smem = (size_t)STAGES * C::STAGE + C::SCRATCH + (a.v.B + 1) * 4;
     auto kernel = attend_few_kernel<D, NT>;
-    kernel<<<2 * num_sms < C::MAX_PARTS ? 2 * num_sms : C::MAX_PARTS, 32 * WARPS, smem, s>>>(a);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * num_sms < C::MAX_PARTS ? 2 * num_sms : C::MAX_PARTS);
+    cfg.blockDim = dim3(32 * WARPS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 }  // namespace
@@ -422,10 +432,10 @@ cudaError_t prepare_attend_few() {
 
 size_t few_parts_floats(int D, int num_sms) { return (size_t)(2 * num_sms < 296 ? 2 * num_sms : 296) * 2 * 16 * (D + 2); }
 
-cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s) {
+cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap) {
     const bool one = a.v.n_q * a.v.G <= 8;
-    if (a.v.D == 64) return one ? few<64, 1>(a, num_sms, s) : few<64, 2>(a, num_sms, s);
-    return one ? few<128, 1>(a, num_sms, s) : few<128, 2>(a, num_sms, s);
+    if (a.v.D == 64) return one ? few<64, 1>(a, num_sms, s, overlap) : few<64, 2>(a, num_sms, s, overlap);
+    return one ? few<128, 1>(a, num_sms, s, overlap) : few<128, 2>(a, num_sms, s, overlap);
 }
 
 }  // namespace kv

@@ -59,8 +59,7 @@ AJ_HD Piece piece_of(const View &v, const Seqs &q, int qt, int tpt) {
     p.ta = qt * q.each + min(qt, q.more);
     p.n_tok = q.each + (qt < q.more);
     p.tok0 = p.n_tok <= tpt ? p.n_tok : (p.n_tok + 1) >> 1;
-    // (tokens of the prefix pass come behind all slots)
-    const int p_lo = (v.prefix ? q.s.L : q.s.L - q.s.nq) + p.ta, end = min(q.s.L, max(0, p_lo + p.n_tok));
+    const int p_lo = q.s.L - q.s.nq + q.s.ahead + p.ta, end = min(q.s.L, max(0, p_lo + p.n_tok));
     p.first = v.window ? min(max(0, p_lo - v.window + 1), end) : q.s.first;
     p.first_tile = p.first / TILE;
     p.n_sink = min((min(v.sinks, p.first) + TILE - 1) / TILE, p.first_tile);

@@ -61,7 +61,7 @@ template <int D> struct Cfg {
     static constexpr int BARS = 2 * STAGES + 24;
     static constexpr int ML_AT = (2 + STAGES) * TILE_BYTES + BARS * 8 + 16;  // maxima and sums of both streams' rows
     static constexpr int SMEM = ML_AT + 4 * 128 * 4;
-    static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + 1) * 8, "the prefix sums of the largest batch fit the ring");
+    static_assert(SMEM <= 232448 && STAGES * TILE_BYTES >= (4096 + MAX_CHUNKS + 1) * 8, "the prefix sums of the largest batch fit the ring");
     static constexpr int PART = 256 * (D + 2);                 // floats of one partial result
 };
 
@@ -269,9 +269,11 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // what comes behind waits for its part itself
     // a piece of less than four tiles costs more in the join than its tiles (one window of 17 rows: 35 -> 28 us)
     // (a CTA's places fit an int, the line's need not; see the bounds at units_of)
-    const int per = (int)max(4ll, (total + gridDim.x - 1) / gridDim.x);
+    int per = (int)max(v.align ? 1ll : 4ll, (total + gridDim.x - 1) / gridDim.x);
+    if (v.align) per = (per + v.align - 1) / v.align * v.align;
     const long long u0 = min(total, (long long)blockIdx.x * per);
     const int u1 = (int)(min(total, u0 + per) - u0);  // from here on places are counted from u0
     auto give_up = [&]() {
@@ -540,7 +542,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
                 const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
                 const int n_rows = tok * v.G;
-                const int p_first = (v.prefix ? c.q.s.L : c.q.s.L - c.q.s.nq) + ta;  // slot of the stream's first token
+                const int p_first = c.q.s.L - c.q.s.nq + c.q.s.ahead + ta;  // slot of the stream's first token
                 const int my_p = p_first + token(min(row, n_rows - 1)), p_last = p_first + tok - 1;
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
@@ -717,20 +719,12 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                         for (int i = 0; i < n_parts; i++)
                             ll += i == mine ? w_mine * l : ex2(__ldcg(part_of_cta(i) + 256 * D + at) - ref) * __ldcg(part_of_cta(i) + 256 * (D + 1) + at);
                     }
-                    const int t_row = token(row), g_row = row - t_row * v.G;
-                    // a batch that shares its first slots: their part of the row, and what it and the rest are scaled by
-                    const bool behind = v.shared && c.p.first && row < n_rows;
-                    const int at_pre = behind || v.prefix ? c.q.s.row0 - rows_of(v).base + ta + t_row : 0;
-                    float c_own = 1.0f, c_pre = 0.0f;
-                    if (behind) {
-                        const float2 ml = *reinterpret_cast<const float2 *>(pre_ml(a, c.h, at_pre, g_row));
-                        const float top = fmaxf(mm, ml.x), r0 = top == -INFINITY ? 0.0f : top;
-                        c_own = ex2(mm - r0);
-                        c_pre = ex2(ml.x - r0);
-                        ll = c_own * ll + c_pre * ml.y;
-                        mm = top;
-                    }
                     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
+                    const int t_row = token(row), g_row = row - t_row * v.G;
+                    // a shared call: a part of the row, to be joined with the others
+                    const int part_of_row = c.b < v.lead ? c.b : v.shared && c.p.first ? v.n_chunks : -1;
+                    const int rel = part_of_row >= 0 ? c.q.s.row0 - rows_of(v).base + ta + t_row : 0;
+                    float *po = part_of_row >= 0 ? pre_o(a, part_of_row, c.h, rel * v.G + g_row) : nullptr;
                     const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
                     const int head = c.h * v.G + g_row;
                     __nv_bfloat16 *o = (__nv_bfloat16 *)a.out + out_row * a.out_stride + (size_t)head * D;
@@ -765,23 +759,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             for (int i = 0; i < 32; i++) y[i] += w_mine * own[i];
                             if (row < n_rows) add(mine + 1, n_parts);
                         }
-                        if (v.prefix) {
+                        if (po) {
                             if (row < n_rows) {
 #pragma unroll
-                                for (int i = 0; i < 32; i += 4)
-                                    *reinterpret_cast<float4 *>(pre_o(a, c.h, at_pre, g_row, k * 32 + i)) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+                                for (int i = 0; i < 32; i += 8) {
+                                    const uint32_t *w = reinterpret_cast<const uint32_t *>(y);
+                                    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(po + k * 32 + i), I8(w, i) : "memory");
+                                }
                             }
                             continue;
-                        }
-                        if (behind) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                const float4 f = *reinterpret_cast<const float4 *>(pre_o(a, c.h, at_pre, g_row, k * 32 + i));
-                                y[i] = c_own * y[i] + c_pre * f.x;
-                                y[i + 1] = c_own * y[i + 1] + c_pre * f.y;
-                                y[i + 2] = c_own * y[i + 2] + c_pre * f.z;
-                                y[i + 3] = c_own * y[i + 3] + c_pre * f.w;
-                            }
                         }
                         if (row < n_rows) {
                             uint32_t w[16];
@@ -797,8 +783,13 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                             }
                         }
                     }
-                    if (v.prefix && x == who && row < n_rows) *reinterpret_cast<float2 *>(pre_ml(a, c.h, at_pre, g_row)) = make_float2(mm, ll);
-                    if (x == who && row < n_rows && a.lse) a.lse[out_row * v.Hq + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * LN2;
+                    if (po && x == who && row < n_rows) {
+                        if (part_of_row < v.n_chunks)
+                            *pre_ml(a, part_of_row, c.h, rel * v.G + g_row) = make_float2(mm, ll);
+                        else
+                            a.own_ml[(size_t)rel * v.Hq + head] = make_float2(mm, ll);
+                    }
+                    if (!po && x == who && row < n_rows && a.lse) a.lse[out_row * v.Hq + head] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * LN2;
                     if (lead && !whole) *counter = 0;
                 }
                 __syncwarp();

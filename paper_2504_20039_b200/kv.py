@@ -9,7 +9,7 @@ import ctypes
 from . import binding
 from .binding import AJ_BF16, AJ_ERR_INVALID_ARG, AJ_OK, AjError
 
-AJ_KV_FLAG_FORCE_SIMT = 1
+AJ_KV_FLAG_FORCE_SIMT, AJ_KV_FLAG_FORCE_SHARED = 1, 4
 
 EXPORTS = ("aj_kv_create", "aj_kv_destroy", "aj_kv_append", "aj_kv_attend", "aj_kv_reserve_shared", "aj_kv_attend_shared", "aj_kv_weigh", "aj_kv_evict", "aj_kv_last_status",
            "aj_kv_last_launch_count", "aj_kv_last_path")

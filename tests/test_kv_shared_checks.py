@@ -54,19 +54,21 @@ int main() {
         for (int S : {128, 384, 4096})
             for (int nq : {1, 7, 31, 32, 33, 64, 65, 1000}) {
                 const int tpt = 128 / G;
-                View p;  // the prefix pass: every piece sees all of the prefix's tiles and no others
+                View p;  // a chunk of the shared slots: every piece of the batch's tokens sees all of its tiles and no others
                 p.Hkv = 1;
                 p.shared = S;
-                p.prefix = 1;
-                const Seqs a = pieces_of(Seq{0, nq, S}, tpt);
+                Seq chunk{0, nq, S};
+                chunk.ahead = nq;
+                chunk.first = S / 2 / 128 * 128;
+                const Seqs a = pieces_of(chunk, tpt);
                 int tokens = 0;
                 for (int i = 0; i < a.n; i++) {
                     const Piece x = piece_of(p, a, i, tpt);
                     tokens += x.n_tok;
-                    bad += x.units != S / 128 || x.first_tile != 0 || x.first != 0 || x.n_sink != 0;
+                    bad += x.units != (S - chunk.first) / 128 || x.first_tile != chunk.first / 128 || x.first != chunk.first || x.n_sink != 0;
                 }
                 bad += tokens != nq;
-                View v;  // the second pass: tiles from the prefix's end to the last token's
+                View v;  // a sequence behind them: tiles from the prefix's end to the last token's
                 v.Hkv = 1;
                 v.shared = S;
                 for (int before : {0, 1, 127, 128, 900}) {
