@@ -31,14 +31,22 @@ struct Args {
     float4 *parts = nullptr;   // [rows][n_v]: a tile's largest logit, S = sum 2^d and T = sum d 2^d, d = (logit - largest) * c
     long long ld = 0;
     int tile = 0, n_v = 0;     // entries per tile, tiles
+    // Which tiles' logits are stored: all, or (gate) those that may hold an alternative or that hold a given token.  The largest
+    // logits that a row's tiles had so far lie in n_top slots, as ordered integers, a tile's number modulo n_top being its slot:
+    // n_top tiles reach the least of the slots, so what lies below it is no alternative.  Zero between calls.
+    int gate = 0;
+    unsigned *slots = nullptr;  // [rows][n_top]
     int *status = nullptr;
 };
+
+constexpr int GATE_TOP = 16, GATE_TOKENS = 8;  // up to so many alternatives and given tokens per row
 
 // How the tcgen05 kernel cuts a group of rows.
 struct Plan {
     bool pair = false;         // two SMs per tile
     int tile = 0, n_v = 0, n_m = 0;  // entries per tile, tiles of entries, tiles of rows
     int box_rows = 0, num_kb = 0, stages = 0, grid = 0;
+    int kps = 1;               // k-blocks per stage: 1 or 2
 };
 cudaError_t prepare_umma(int num_sms, int *max_pairs);
 int one_sm_tile(int V, int num_sms);
@@ -48,7 +56,7 @@ cudaError_t launch_umma(const CUtensorMap &mh, const CUtensorMap &mw, const Args
 cudaError_t launch_simt(const Args &a, cudaStream_t s);
 cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s);
 cudaError_t prepare_finish();
-// The finishing kernel keeps a key per tile and AJ_SCORE_MAX_TOP tiles of logits in shared memory (64 + 128 KB at most).
+// The finishing kernel keeps a key per tile and AJ_SCORE_MAX_TOP tiles of logits in shared memory (32 + 128 KB at most).
 constexpr int MAX_TILES = 8192, MAX_V = MAX_TILES * 256;
 
 #ifdef __CUDACC__
@@ -61,6 +69,11 @@ __device__ inline float ex2(float x) {
 __device__ inline float max_nan(float a, float b) {  // NaN if one of them is
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ inline float max3_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 

@@ -28,6 +28,7 @@ struct aj_score_s {
     int rows_n = 0, rows_box = 0;
     float *logits = nullptr;
     float4 *parts = nullptr;
+    unsigned *slots = nullptr;
     int *status = nullptr;
     int last_launches = 0;
     const char *last_path = "none";
@@ -178,8 +179,10 @@ aj_status aj_score_create(aj_score *out, int device, int max_rows, int d, int V,
     // up to 128 rows in the one-SM kernel's tiles, or all of a group in tiles of 256: a row is whole tiles, so less than one more than V
     const size_t few = h->group < 128 ? h->group : 128, n_one = (V + h->tile - 1) / h->tile, n_wide = (V + 255) / 256;
     const size_t parts = few * n_one > h->group * n_wide ? few * n_one : h->group * n_wide;
+    const size_t slots = (size_t)h->group * score::GATE_TOP * 4;
     if (cudaMalloc(&h->logits, (size_t)h->group * (V + 255) * 4) != cudaSuccess || cudaMalloc(&h->parts, parts * 16) != cudaSuccess ||
-        cudaMalloc(&h->status, 256) != cudaSuccess || zero_now(h->status, 256) != cudaSuccess) {
+        cudaMalloc(&h->slots, slots) != cudaSuccess || zero_now(h->slots, slots) != cudaSuccess || cudaMalloc(&h->status, 256) != cudaSuccess ||
+        zero_now(h->status, 256) != cudaSuccess) {
         cudaGetLastError();
         aj_score_destroy(h);
         return AJ_ERR_CUDA;
@@ -197,6 +200,7 @@ aj_status aj_score_destroy(aj_score h) {
     Guard guard(h->device);
     cudaFree(h->logits);
     cudaFree(h->parts);
+    cudaFree(h->slots);
     cudaFree(h->status);
     delete h;
     return AJ_OK;
@@ -248,8 +252,8 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
         if (tensor) {
             const score::Plan p = score::plan_umma(a.rows, h->d, h->V, h->dtype, h->tile, h->num_sms, h->max_pairs);
             a.tile = p.tile;
-            a.n_v = p.n_v;
-            a.ld = (long long)p.n_v * p.tile;
+            a.n_v = (h->V + p.tile - 1) / p.tile;
+            a.ld = (long long)a.n_v * p.tile;
             if (h->rows_stride != h_stride || h->rows_n != a.rows || h->rows_box != p.box_rows) {
                 h->rows_stride = -1;
                 if (!encode(h, &h->rows, h->logits, a.rows, a.rows > 1 ? h_stride : h->d, p.box_rows)) return AJ_ERR_CUDA;
@@ -257,6 +261,8 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
             }
             CUtensorMap mh, mw;
             if (!at_address(h, &mh, h->rows, a.h) || !at_address(h, &mw, p.pair ? h->w_pair : h->w_one, W)) return AJ_ERR_CUDA;
+            a.gate = n_top <= score::GATE_TOP && n_tok <= score::GATE_TOKENS;
+            a.slots = h->slots;
             h->last_path = p.pair ? "umma_two_sm" : "umma_one_sm";
             err = score::launch_umma(mh, mw, a, p, s);
             h->last_launches += 2;

@@ -2,9 +2,9 @@
 //
 //   logits[m, v] = sum_k h[m, k] W[v, k]   one fixed order over k, f32
 //
-// A CTA of 256 threads computes a tile of TM rows x 64 entries from k-slices of 32 staged in shared memory as f32.  With few
-// rows (TM = 8) the products are bound by the stream of W, with more (TM = 64) by the multiply-adds and the reads of shared
-// memory that feed them (4 x 4 outputs per thread).  A second kernel, a warp per row and tile, makes the tiles' sums.
+// Up to 8 rows: a warp per entry, its lanes along k, all rows at once; bound by the stream of W.  More rows: a CTA of 256
+// threads computes a tile of 64 rows x 64 entries from k-slices of 32 staged in shared memory as f32, 4 x 4 outputs per thread; bound by
+// the reads of shared memory that feed the multiply-adds.  A second kernel, a warp per row and tile, makes the tiles' sums.
 #include "aj_score.cuh"
 
 namespace aj {
@@ -19,10 +19,39 @@ template <> __device__ inline float widen<float>(float x) { return x; }
 template <> __device__ inline float widen<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <> __device__ inline float widen<__nv_fp8_e4m3>(__nv_fp8_e4m3 x) { return float(x); }
 
-template <typename T, int TM>
+// Up to 8 rows: a warp takes entries in turn.
+template <typename T> __global__ void __launch_bounds__(256) few_logits_kernel(Args a) {
+    const T *h = (const T *)a.h, *W = (const T *)a.W;
+    const int lane = threadIdx.x & 31;
+    for (long long v = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); v < a.ld; v += (long long)gridDim.x * 8) {
+        float acc[8] = {};
+        if (v < a.V) {
+#pragma unroll 4
+            for (int k = lane; k < a.d; k += 32) {
+                const float w = widen(W[(size_t)v * a.d + k]);
+#pragma unroll
+                for (int m = 0; m < 8; m++)
+                    if (m < a.rows) acc[m] += w * widen(h[(size_t)m * a.h_stride + k]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 8; m++) {
+            if (m >= a.rows) break;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) acc[m] += __shfl_xor_sync(~0u, acc[m], o);
+            if (lane == 0) {
+                float x = acc[m];
+                if (a.h_scale && v < a.V) x = x * a.h_scale[m] * a.w_scale[v];
+                a.logits[(size_t)m * a.ld + v] = v < a.V ? x : -INFINITY;
+            }
+        }
+    }
+}
+
+template <typename T>
 __global__ void __launch_bounds__(256) logits_kernel(Args a) {
-    constexpr int RM = TM >= 64 ? 4 : 1, RV = TM >= 64 ? 4 : 2;  // outputs per thread
-    constexpr int TX = BV / RV;                                  // threads along the entries
+    constexpr int TM = 64, RM = 4, RV = 4;  // outputs per thread
+    constexpr int TX = BV / RV;             // threads along the entries
     static_assert(TX * (TM / RM) == 256, "256 threads cover the tile");
     __shared__ float sh[BK][TM + 4], sw[BK][BV + 4];
     const T *h = (const T *)a.h, *W = (const T *)a.W;
@@ -96,9 +125,9 @@ __global__ void __launch_bounds__(256) parts_kernel(Args a) {
 template <typename T> void logits(const Args &a, cudaStream_t s) {
     const unsigned gx = (unsigned)((a.ld + BV - 1) / BV);
     if (a.rows <= 8)
-        logits_kernel<T, 8><<<dim3(gx, 1), 256, 0, s>>>(a);
+        few_logits_kernel<T><<<(unsigned)((a.ld + 7) / 8 < 2048 ? (a.ld + 7) / 8 : 2048), 256, 0, s>>>(a);
     else
-        logits_kernel<T, 64><<<dim3(gx, (a.rows + 63) / 64), 256, 0, s>>>(a);
+        logits_kernel<T><<<dim3(gx, (a.rows + 63) / 64), 256, 0, s>>>(a);
 }
 
 }  // namespace

@@ -11,7 +11,7 @@
 //
 //   warp 0      TMA: 128-byte wide boxes of h and W (128-byte swizzle) into a ring of stages, one 128-byte k-block each
 //   warp 1      issues tcgen05.mma into one of two accumulators of 256 columns
-//   warps 2-5   epilogue: maximum, then exponentials and the logits' store, while the other accumulator fills
+//   warps 2-5   epilogue: maximum, exponentials and the logits' store, while the other accumulator fills
 //
 // bf16 and e4m3 differ in the instruction and in the scales that the epilogue puts on the sums (times h_scale, times w_scale).
 // Every logit is one sum over k in a fixed order.  Every wait is bounded (aj_ptx.cuh).
@@ -65,8 +65,8 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
     const int unit = PAIR ? blockIdx.x >> 1 : blockIdx.x, units = PAIR ? gridDim.x >> 1 : gridDim.x;
     constexpr int ROWS = PAIR ? 256 : 128;
     const int n_tiles = p.n_m * p.n_v, tile = p.tile, tile_cta = PAIR ? tile >> 1 : tile;
-    const uint32_t a_bytes = (uint32_t)p.box_rows * 128u, stage_bytes = a_bytes + (uint32_t)tile_cta * 128u;
-    const int stages = p.stages;
+    const int stages = p.stages, kps = p.kps;
+    const uint32_t a_bytes = (uint32_t)p.box_rows * 128u, sub_bytes = a_bytes + (uint32_t)tile_cta * 128u, stage_bytes = kps * sub_bytes;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; s++) {
@@ -110,22 +110,24 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
             for (int t = unit; ok && t < n_tiles; t += units) {
                 const int v_tile = t / p.n_m, m_tile = t - v_tile * p.n_m;
                 const int row = m_tile * ROWS + (int)rank * 128, v = v_tile * tile + (int)rank * tile_cta;
-                for (int kb = 0; kb < p.num_kb; kb++) {
+                for (int kb = 0; kb < p.num_kb; kb += kps) {
                     if (!mbar_wait(empty(s), ph ^ 1u, abort_flag)) {
                         give_up();
                         ok = false;
                         break;
                     }
-                    const uint32_t dst = base + s * stage_bytes;
-                    if (PAIR) {
-                        const uint32_t bar = map_to_cta(full(s), 0);
-                        if (rank == 0) mbar_expect_tx(full(s), 2u * stage_bytes);
-                        tma_load_2d_pair(dst + a_bytes, &tmap_w, kb * BK, v, bar, pol_w);
-                        tma_load_2d_pair(dst, &tmap_h, kb * BK, row, bar, pol_h);
-                    } else {
-                        mbar_expect_tx(full(s), stage_bytes);
-                        tma_load_2d(dst + a_bytes, &tmap_w, kb * BK, v, full(s), pol_w);
-                        tma_load_2d(dst, &tmap_h, kb * BK, row, full(s), pol_h);
+                    const uint32_t bar = PAIR ? map_to_cta(full(s), 0) : full(s);
+                    if (rank == 0) mbar_expect_tx(full(s), (PAIR ? 2u : 1u) * stage_bytes);
+                    for (int j = 0; j < kps; j++) {
+                        const uint32_t dst = base + s * stage_bytes + j * sub_bytes;
+                        const int kc = (kb + j) * BK;
+                        if (PAIR) {
+                            tma_load_2d_pair(dst + a_bytes, &tmap_w, kc, v, bar, pol_w);
+                            tma_load_2d_pair(dst, &tmap_h, kc, row, bar, pol_h);
+                        } else {
+                            tma_load_2d(dst + a_bytes, &tmap_w, kc, v, bar, pol_w);
+                            tma_load_2d(dst, &tmap_h, kc, row, bar, pol_h);
+                        }
                     }
                     if (++s == stages) {
                         s = 0;
@@ -140,7 +142,7 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
             const uint32_t idesc = EIGHT ? instr_desc_e4m3(ROWS, tile) : instr_desc(ROWS, tile);
             int s = 0, it = 0;
             uint32_t ph = 0;
-            bool ok = true;
+            bool ok = true, ready = false;
             for (int t = unit; ok && t < n_tiles; t += units, ++it) {
                 const int b = it & 1;
                 if (!mbar_wait(acc_empty(b), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag)) {
@@ -149,33 +151,37 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
                 }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(b * 256);
-                for (int kb = 0; kb < p.num_kb; kb++) {
-                    if (!mbar_wait(full(s), ph, abort_flag)) {
+                for (int kb = 0; kb < p.num_kb; kb += kps) {
+                    if (!ready && !mbar_wait(full(s), ph, abort_flag)) {
                         give_up();
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t at = base + s * stage_bytes;
-                    const unsigned long long ad = smem_desc_sw128(at), bd = smem_desc_sw128(at + a_bytes);
+                    const int s_next = s + 1 == stages ? 0 : s + 1;
+                    const uint32_t ph_next = s + 1 == stages ? ph ^ 1u : ph;
+                    for (int j = 0; j < kps; j++) {
+                        const uint32_t at = base + s * stage_bytes + j * sub_bytes;
+                        const unsigned long long ad = smem_desc_sw128(at), bd = smem_desc_sw128(at + a_bytes);
 #pragma unroll
-                    for (int k = 0; k < 4; k++) {
-                        const uint32_t acc = (uint32_t)((kb | k) != 0);
-                        if constexpr (EIGHT)
-                            umma_e4m3<PAIR>(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
-                        else if constexpr (PAIR)
-                            umma_bf16_pair(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
-                        else
-                            umma_bf16(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
+                        for (int k = 0; k < 4; k++) {
+                            const uint32_t acc = (uint32_t)((kb | j | k) != 0);
+                            if constexpr (EIGHT)
+                                umma_e4m3<PAIR>(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
+                            else if constexpr (PAIR)
+                                umma_bf16_pair(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
+                            else
+                                umma_bf16(d, ad + 2ull * k, bd + 2ull * k, idesc, acc);
+                            // the next stage is looked at while this one's MMAs run, not after them
+                            if (k == 2 && j + 1 == kps) ready = mbar_test(full(s_next), ph_next);
+                        }
                     }
                     if (PAIR)
                         umma_commit_pair(empty(s));
                     else
                         umma_commit(empty(s));
-                    if (++s == stages) {
-                        s = 0;
-                        ph ^= 1u;
-                    }
+                    s = s_next;
+                    ph = ph_next;
                 }
                 if (ok) {
                     if (PAIR)
@@ -196,6 +202,16 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
             const bool valid = row < a.rows;
             const int v0 = v_tile * tile;
             const float sh = EIGHT && valid ? __ldg(a.h_scale + row) : 1.0f;
+            // asked before the accumulator is ready; an old slot is only lower, and then a tile is stored that need not be
+            uint32_t least = 0;
+            bool asked = false;
+            if (a.gate) {
+                least = ~0u;
+                if (valid) {
+                    for (int i = 0; i < a.n_top; i++) least = min(least, __ldcg(a.slots + (size_t)row * a.n_top + i));
+                    for (int i = 0; i < a.n_tok; i++) asked |= (unsigned)(__ldg(a.tokens + (size_t)row * a.n_tok + i) - v0) < (unsigned)tile;
+                }
+            }
             // the whole warp takes one decision, so the aligned TMEM loads below stay converged
             if (!__all_sync(~0u, mbar_wait(acc_full(b), (uint32_t)(it >> 1) & 1u, abort_flag))) {
                 give_up();
@@ -226,33 +242,49 @@ score_umma_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_const
                         }
                     }
                 };
-                float mx = -INFINITY;
+                // One pass: S and T relative to the largest logit so far, which a chunk may raise.
+                float mx = -INFINITY, S = 0.0f, T = 0.0f;
 #pragma unroll 1
                 for (int j = 0; j < tile; j += 32) {
                     float x[32];
                     load(j, x);
+                    float m4[4] = {mx, mx, mx, mx};
 #pragma unroll
-                    for (int i = 0; i < 32; i++) mx = max_nan(mx, x[i]);
-                }
-                float S[4] = {}, T[4] = {};
-                float *to = a.logits + (size_t)row * a.ld + v0;
-#pragma unroll 1
-                for (int j = 0; j < tile; j += 32) {
-                    float x[32];
-                    load(j, x);
-                    if (valid) {
+                    for (int i = 0; i < 32; i += 8)
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) store8(to + j + i, x + i);
-                    }
+                        for (int k = 0; k < 4; k++) m4[k] = max3_nan(m4[k], x[i + k], x[i + 4 + k]);
+                    const float top = max3_nan(max3_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
+                    // (all of them -infinity: nothing to raise, the differences are NaN and count as -150)
+                    const float up = fmaxf((mx - top) * c, -150.0f), w = ex2(up);
+                    T = w * (T + up * S);
+                    S *= w;
+                    mx = top;
+                    float s4[4] = {}, t4[4] = {};
 #pragma unroll
                     for (int i = 0; i < 32; i++) {
-                        const float d = fmaxf((x[i] - mx) * c, -150.0f), e = ex2(d);  // (2^-150 is zero: so is d 2^d)
-                        S[i & 3] += e;
-                        T[i & 3] += d * e;
+                        const float d = fmaxf((x[i] - top) * c, -150.0f), e = ex2(d);  // 2^-150 is zero, and so is d 2^d
+                        s4[i & 3] += e;
+                        t4[i & 3] += d * e;
                     }
-                    __syncwarp();
+                    S += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    T += (t4[0] + t4[1]) + (t4[2] + t4[3]);
                 }
-                if (valid) a.parts[(size_t)row * p.n_v + v_tile] = make_float4(mx, (S[0] + S[1]) + (S[2] + S[3]), (T[0] + T[1]) + (T[2] + T[3]), 0.0f);
+                const bool store = valid && (!a.gate || asked || (a.n_top && ordered_image(mx) >= least));
+                if (a.gate && a.n_top && store) atomicMax(a.slots + (size_t)row * a.n_top + v_tile % a.n_top, ordered_image(mx));
+                if (__any_sync(~0u, store)) {
+                    float *to = a.logits + (size_t)row * a.ld + v0;
+#pragma unroll 1
+                    for (int j = 0; j < tile; j += 32) {
+                        float x[32];
+                        load(j, x);
+                        if (store) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8) store8(to + j + i, x + i);
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (valid) a.parts[(size_t)row * p.n_v + v_tile] = make_float4(mx, S, T, 0.0f);
             }
             tc_fence_before();
             __syncwarp();
@@ -359,7 +391,8 @@ Plan plan_umma(int rows, int d, int V, int dtype, int tile, int num_sms, int max
     p.n_m = p.pair ? (rows + 255) / 256 : 1;
     p.box_rows = p.pair ? 128 : (rows + 7) & ~7;
     p.num_kb = (int)(((long long)d * (dtype == E4M3 ? 1 : 2) + 127) / 128);
-    const int stage = (p.box_rows + (p.pair ? 128 : p.tile)) * 128;
+    p.kps = p.pair && p.num_kb % 2 == 0 ? 2 : 1;
+    const int stage = (p.box_rows + (p.pair ? 128 : p.tile)) * 128 * p.kps;
     // the MMA reads 16 KB from a stage's rows on: past the end of the ring only where a stage is smaller, and then still within
     // the block's shared memory
     const int ring = stage >= 16384 ? RING : RING - 16384;
