@@ -24,7 +24,7 @@ enum { AJ_E4M3 = 2 };
 enum { AJ_SCORE_FLAG_FORCE_SIMT = 1u };
 
 /* Most alternatives and given tokens per row. */
-enum { AJ_SCORE_MAX_TOP = 64, AJ_SCORE_MAX_TOKENS = 1024 };
+enum { AJ_SCORE_MAX_TOP = 32, AJ_SCORE_MAX_TOKENS = 1024 };
 
 /*
  * Residual addition and root-mean-square norm of each row, output in the storage type, in 8 bits, or both.

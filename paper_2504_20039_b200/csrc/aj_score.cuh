@@ -56,7 +56,7 @@ cudaError_t launch_umma(const CUtensorMap &mh, const CUtensorMap &mw, const Args
 cudaError_t launch_simt(const Args &a, cudaStream_t s);
 cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s);
 cudaError_t prepare_finish();
-// The finishing kernel keeps a key per tile and AJ_SCORE_MAX_TOP tiles of logits in shared memory (32 + 128 KB at most).
+// The finishing kernel keeps two keys per tile, or per entry of AJ_SCORE_MAX_TOP tiles, in shared memory (128 KB at most).
 constexpr int MAX_TILES = 8192, MAX_V = MAX_TILES * 256;
 
 #ifdef __CUDACC__

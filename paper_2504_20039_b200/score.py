@@ -11,7 +11,7 @@ from .binding import AJ_BF16, AJ_ERR_INVALID_ARG, AJ_F32, AJ_OK, AjError
 
 AJ_E4M3 = 2
 AJ_SCORE_FLAG_FORCE_SIMT = 1
-AJ_SCORE_MAX_TOP, AJ_SCORE_MAX_TOKENS = 64, 1024
+AJ_SCORE_MAX_TOP, AJ_SCORE_MAX_TOKENS = 32, 1024
 
 EXPORTS = ("aj_add_norm", "aj_score_create", "aj_score_destroy", "aj_score_tokens", "aj_score_last_status", "aj_score_last_launch_count",
            "aj_score_last_path")

@@ -14,7 +14,7 @@ def paths(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32", "e4m3"])
-@pytest.mark.parametrize("rows,d,V,n_top", [(1, 64, 1, 1), (1, 8, 3, 3), (5, 256, 1000, 5), (2, 64, 255, 20), (17, 512, 257, 1), (17, 256, 5000, 64), (33, 72, 3001, 8),
+@pytest.mark.parametrize("rows,d,V,n_top", [(1, 64, 1, 1), (1, 8, 3, 3), (5, 256, 1000, 5), (2, 64, 255, 20), (17, 512, 257, 1), (17, 256, 5000, 32), (3, 64, 8000, 32), (200, 64, 7900, 32), (140, 64, 300000, 32), (33, 72, 3001, 8),
                                             (64, 320, 2048, 5), (96, 128, 4099, 20), (128, 256, 777, 3), (129, 192, 2500, 5), (256, 512, 6001, 8),
                                             (257, 264, 1111, 5), (300, 1024, 20000, 20), (513, 128, 515, 0), (777, 448, 3333, 4)])
 def test_sizes(rows, d, V, n_top, dtype):

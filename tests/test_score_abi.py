@@ -48,7 +48,7 @@ def test_creation_checks_need_no_device(built):
         return e.value.status
 
     ok = (0, 4, 64, 1000, aj.AJ_BF16, 5, 0)
-    for i, bad in [(0, -1), (1, 0), (2, 0), (3, 0), (4, 3), (4, -1), (5, -1), (5, 65), (6, 2)]:
+    for i, bad in [(0, -1), (1, 0), (2, 0), (3, 0), (4, 3), (4, -1), (5, -1), (5, 33), (6, 2)]:
         args = list(ok)
         args[i] = bad
         assert status(*args) == aj.AJ_ERR_INVALID_ARG, args
