@@ -26,7 +26,7 @@ struct View {
     // then begin behind the shared slots.  Each leaves its unnormalised results, for aj_kv_join.cu.
     int shared = 0, lead = 0, chunk = 0, n_chunks = 0;
     const int *lead_table = nullptr;
-    int align = 0;  // places of the line that a CTA's share is a multiple of; 0: any
+    int align = 0;  // places of the line that every piece takes and a CTA's share is a multiple of; 0: as many as it has
     int n_seq = 0, total = 0, pre_rows = 0;  // sequences; rows without q_start; rows that the results have room for
 };
 

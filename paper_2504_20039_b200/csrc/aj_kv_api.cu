@@ -160,28 +160,34 @@ bool attend_maps(aj_kv h, const kv::AttendArgs &a, CUtensorMap (&maps)[4], int *
     return !tma || (at_address(h, &maps[2], h->rows1, a.q) && (tma != 8 || at_address(h, &maps[3], h->rows8, a.q)));
 }
 
-// Into how many chunks the shared slots are cut.  An item is a chunk, a key head and a piece of up to 256 query rows: as many
-// as there are SMs, so that hardly an item spans CTAs (which costs a join by one CTA), but at most MAX_CHUNKS.
-void cut_shared(kv::View &v, int num_sms) {
+// Into how many chunks the shared slots are cut.  An item is a chunk, a key head and a piece of up to 256 query rows.  With few
+// rows per sequence, chunks of six tiles on up to half of the SMs, while the sequences' own slots are attended on the others (64 tokens
+// behind 2048 slots: 37 us, with every SM for one and then the other 62); else as many items as there are SMs, so that hardly
+// one spans CTAs, which costs a join by one CTA.  Returns the CTAs for it.
+int cut_shared(kv::View &v, int num_sms) {
     const int tiles = v.shared / 128, per_piece = 2 * (128 / v.G);
     const long long items = (long long)v.Hkv * ((v.pre_rows + per_piece - 1) / per_piece);
-    int n = items < num_sms ? (int)(num_sms / items) : 1;
+    const bool few = v.n_q * v.G <= kv::FEW_ROWS;
+    const int most = few ? num_sms / 2 : num_sms;
+    int n = items < most ? (int)(most / items) : 1;
+    if (few && n > (tiles + 5) / 6) n = (tiles + 5) / 6;
     if (n > kv::MAX_CHUNKS) n = kv::MAX_CHUNKS;
-    if (n > tiles) n = tiles;
     const int each = (tiles + n - 1) / n;
     v.chunk = each * 128;
     v.n_chunks = (tiles + each - 1) / each;
+    return (int)(items * v.n_chunks < most ? items * v.n_chunks : most);
 }
 // Is it worth the parts and their join?  Sequences that share pages read them from L2 when they are attended one by one, so what is
-// saved is the stream from L2 (few rows), or row tiles that a window does not fill (more rows).  Measured, us, together and one by
-// one: 64 tokens behind 2048 slots 65 and 88, 26 behind 7040 29 and 56, 12 behind 1088 23 and 14; 31 windows of 17 rows behind 4352
-// 66 and 85, 32 of 33 behind 1504 87 and 76, prompts behind 8192 241 and 186.
+// saved is the stream from L2 (few rows: at 5.9 TB/s, against 12 us and 2 for each tile of a chunk), or row tiles that a window
+// does not fill (more rows).  Measured, us, together and one by one: 64 tokens behind 2048 slots 37 and 88, behind 512 34 and 39, behind
+// 256 34 and 31; 16 behind 4096 29 and 46, behind 1024 22 and 21; 2 behind 32768 82 and 49; 32 windows of 9 rows behind 2048
+// 52 and 88, 16 of 33 behind 8192 115 and 164, 32 of 33 behind 1504 86 and 75.
 bool worth_sharing(const kv::View &v) {
-    if (v.n_q * v.G <= kv::FEW_ROWS) return (double)(v.n_seq - 1) * v.shared * v.Hkv * v.D * 4 > 118e6;  // 20 us of the stream
+    if (v.n_q * v.G <= kv::FEW_ROWS) return (double)v.n_seq * v.shared * v.Hkv * v.D * 4 / 5.9e6 > 12 + v.chunk / 64;
     const long long per_piece = 2 * (128 / v.G), together = (v.pre_rows + per_piece - 1) / per_piece;
     // (of a ragged batch the host knows the sum at most: half a piece more for each sequence)
     const long long one_by_one = v.q_start ? together + v.n_seq / 2 : v.n_seq * ((v.n_q + per_piece - 1) / per_piece);
-    return (one_by_one - together) * v.Hkv * (v.shared / 128) > 2300;  // 30 us of 148 SMs
+    return (one_by_one - together) * v.Hkv * (v.shared / 128) > 2300;
 }
 // Rows x chunks that a workspace for max_rows rows must hold.
 int pre_capacity(aj_kv h, int max_rows) {
@@ -444,10 +450,10 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
     a.v.n_seq = B;
     a.v.total = B * n_q;
     a.v.pre_rows = a.v.total < h->pre_rows ? a.v.total : h->pre_rows;
+    const int ctas = cut_shared(a.v, h->num_sms);
     if (!(h->flags & AJ_KV_FLAG_FORCE_SHARED) && !worth_sharing(a.v))
         return aj_kv_attend(h, q, q_stride, k_pages, v_pages, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, scale, 0, 0, out, out_stride,
                             lse, cuda_stream);
-    cut_shared(a.v, h->num_sms);
     a.pre = h->pre;
     a.pre_ml = h->pre_ml;
     a.own_ml = h->own_ml;
@@ -467,8 +473,8 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
         p.v.n_q = p.v.pre_rows;
         p.parts = h->pre_parts;
         p.counters = h->pre_counters;
-        e = kv::launch_attend_umma(p, maps, q_tma, h->num_sms, s);
-        if (e == cudaSuccess) e = kv::launch_attend_few(a, h->num_sms, s, true);
+        e = kv::launch_attend_umma(p, maps, q_tma, ctas, s);
+        if (e == cudaSuccess) e = kv::launch_attend_few(a, h->num_sms - ctas, s, true);
     } else {
         h->last_path = "shared_umma";
         h->last_launches = 2;

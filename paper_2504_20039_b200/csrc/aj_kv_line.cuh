@@ -19,6 +19,7 @@ constexpr int CHARGE = 2;
 struct Piece {
     int ta, n_tok, tok0;          // first token, tokens, tokens of stream 0 (== n_tok: both streams share the rows)
     int first, n_sink, first_tile, units;
+    int places;                   // on the line: its tiles, or the same number for every piece (View::align)
 };
 
 struct Seqs {                     // a sequence and how its new tokens are cut into pieces
@@ -38,9 +39,9 @@ struct Part {
 };
 AJ_HD Part part_of(const Line &c, int left) {
     Part p;
-    p.line = min(c.p.units - c.unit, left);
+    p.line = min(c.p.places - c.unit, left);
     p.first = max(c.unit, 0);
-    p.n = max(0, c.unit + p.line - p.first);
+    p.n = max(0, min(c.unit + p.line, c.p.units) - p.first);
     return p;
 }
 
@@ -64,6 +65,7 @@ AJ_HD Piece piece_of(const View &v, const Seqs &q, int qt, int tpt) {
     p.first_tile = p.first / TILE;
     p.n_sink = min((min(v.sinks, p.first) + TILE - 1) / TILE, p.first_tile);
     p.units = max(1, p.n_sink + (end + TILE - 1) / TILE - p.first_tile);
+    p.places = v.align ? max(p.units, v.align - CHARGE) : p.units;
     return p;
 }
 
@@ -73,7 +75,7 @@ AJ_HD Piece piece_of(const View &v, const Seqs &q, int qt, int tpt) {
 // CTA's share of it, an item and the pieces' numbers stay below 2^31.
 AJ_HD long long units_of(const View &v, const Seqs &q, int tpt, int at, int step) {
     long long u = 0;
-    for (int i = at; i < q.n; i += step) u += CHARGE + piece_of(v, q, i, tpt).units;
+    for (int i = at; i < q.n; i += step) u += CHARGE + piece_of(v, q, i, tpt).places;
     return u;
 }
 

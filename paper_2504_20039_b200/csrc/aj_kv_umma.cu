@@ -113,7 +113,7 @@ __device__ inline Line seek(const View &v, int tpt, const long long *pre, long l
     c.h = (int)(r / per_head);
     r -= c.h * per_head;
     for (int q0 = 0;; q0 += 32) {
-        const int n = q0 + lane < c.q.n ? CHARGE + piece_of(v, c.q, q0 + lane, tpt).units : 0;
+        const int n = q0 + lane < c.q.n ? CHARGE + piece_of(v, c.q, q0 + lane, tpt).places : 0;
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -243,6 +243,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     long long *pre = reinterpret_cast<long long *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
+    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // what comes behind waits for its part itself
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
@@ -269,7 +270,6 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // what comes behind waits for its part itself
     // a piece of less than four tiles costs more in the join than its tiles (one window of 17 rows: 35 -> 28 us)
     // (a CTA's places fit an int, the line's need not; see the bounds at units_of)
     int per = (int)max(v.align ? 1ll : 4ll, (total + gridDim.x - 1) / gridDim.x);
