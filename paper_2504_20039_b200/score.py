@@ -26,12 +26,11 @@ _ARGS = {
     "aj_score_last_launch_count": [_vp],
     "aj_score_last_path": [_vp],
 }
-_fns = None
-_types = None
+_fns = _types = _f32 = _i32 = _f8 = _add_norm = None
 
 
 def _lib():
-    global _fns, _types
+    global _fns, _types, _f32, _i32, _f8, _add_norm
     if _fns is None:
         import torch
 
@@ -42,6 +41,7 @@ def _lib():
             fn.argtypes, fn.restype = args, ctypes.c_char_p if name == "aj_score_last_path" else _ci
             fns[name] = fn
         _types = {torch.bfloat16: AJ_BF16, torch.float32: AJ_F32, torch.float8_e4m3fn: AJ_E4M3}
+        _f32, _i32, _f8, _add_norm = torch.float32, torch.int32, torch.float8_e4m3fn, fns["aj_add_norm"]
         _fns = fns
     return _fns
 
@@ -52,34 +52,31 @@ def add_norm(x, weight, eps: float = 1e-5, out=None, residual=None, residual_out
 
     x, residual, residual_out, out [rows, d] (rows may be strided) bf16 or f32, weight [d] f32, out8 [rows, d] float8_e4m3fn with
     scale8 [rows] f32: a row's values are out8 * scale8.  residual_out may be x or residual, out may be x or residual."""
-    f = _fns or _lib()
-    dt = x.dtype
-    if x.dim() != 2:
-        if check:
-            raise AjError(AJ_ERR_INVALID_ARG, "aj_add_norm")
-        return AJ_ERR_INVALID_ARG
-    rows, d = shape = x.shape
-    dev = x.get_device()
-    xs = x.stride()
-    ok = (dt in _types and dev >= 0 and (xs[1] == 1 or d == 1) and weight.numel() == d and weight.dtype.itemsize == 4 and weight.is_floating_point()
-          and weight.is_contiguous() and weight.get_device() == dev)
-    args = []
-    for t, want in ((residual, dt), (residual_out, dt), (out, dt), (out8, None)):
-        if t is None:
-            args.append((None, 0))
-            continue
-        ts = t.stride()
-        ok = (ok and t.shape == shape and (t.dtype is dt if want is not None else _types.get(t.dtype) == AJ_E4M3) and t.get_device() == dev
-              and (ts[1] == 1 or d == 1))
-        args.append((t.data_ptr(), ts[0]))
-    if scale8 is not None:
-        ok = ok and scale8.numel() == rows and _types.get(scale8.dtype) == AJ_F32 and scale8.is_contiguous() and scale8.get_device() == dev
-    if not ok:
-        st = AJ_ERR_INVALID_ARG
-    else:
-        (r, rs), (ro, ros), (o, os), (o8, o8s) = args
-        st = f["aj_add_norm"](dev, x.data_ptr(), xs[0], r, rs, weight.data_ptr(), eps, rows, d, _types[dt], ro, ros, o, os, o8, o8s,
-                              None if scale8 is None else scale8.data_ptr(), stream or None)
+    fn = _add_norm or _lib()["aj_add_norm"]
+    st = AJ_ERR_INVALID_ARG
+    dt, shape, dev = x.dtype, x.shape, x.get_device()
+    if len(shape) == 2 and dt in _types and dev >= 0 and weight.dtype is _f32 and weight.numel() == shape[1] and weight.is_contiguous() and weight.get_device() == dev:
+        xs = x.stride()
+        ok = xs[1] == 1 or shape[1] == 1
+        r = ro = o = o8 = s8 = None
+        rs = ros = os = o8s = 0
+        if residual is not None:
+            r, (rs, e) = residual.data_ptr(), residual.stride()
+            ok = ok and e == xs[1] and residual.dtype is dt and residual.shape == shape and residual.get_device() == dev
+        if residual_out is not None:
+            ro, (ros, e) = residual_out.data_ptr(), residual_out.stride()
+            ok = ok and e == xs[1] and residual_out.dtype is dt and residual_out.shape == shape and residual_out.get_device() == dev
+        if out is not None:
+            o, (os, e) = out.data_ptr(), out.stride()
+            ok = ok and e == xs[1] and out.dtype is dt and out.shape == shape and out.get_device() == dev
+        if out8 is not None:
+            o8, (o8s, e) = out8.data_ptr(), out8.stride()
+            ok = ok and e == xs[1] and out8.dtype is _f8 and out8.shape == shape and out8.get_device() == dev
+        if scale8 is not None:
+            s8 = scale8.data_ptr()
+            ok = ok and scale8.dtype is _f32 and scale8.numel() == shape[0] and scale8.is_contiguous() and scale8.get_device() == dev
+        if ok:
+            st = fn(dev, x.data_ptr(), xs[0], r, rs, weight.data_ptr(), eps, shape[0], shape[1], _types[dt], ro, ros, o, os, o8, o8s, s8, stream or None)
     if check and st != AJ_OK:
         raise AjError(st, "aj_add_norm")
     return st
@@ -101,7 +98,6 @@ class ScoreHandle:
             raise AjError(st, "aj_score_create")
         self._score, self._device, self._d, self._V = f["aj_score_tokens"], device, d, V
         self._dtype = {AJ_BF16: torch.bfloat16, AJ_F32: torch.float32, AJ_E4M3: torch.float8_e4m3fn}[dtype]
-        self._i32, self._f32 = torch.int32, torch.float32
 
     def score(self, h, W, tokens=None, logprob=None, lse=None, entropy=None, top_id=None, top_logprob=None, inv_temperature: float = 1.0,
               h_scale=None, w_scale=None, stream: int = 0, check: bool = True) -> int:
@@ -109,24 +105,41 @@ class ScoreHandle:
 
         h [rows, d] (rows may be strided), W [V, d]; tokens [rows, n_tok] int32 with logprob [rows, n_tok]; lse, entropy [rows];
         top_id [rows, n_top] int32 with top_logprob [rows, n_top]; h_scale [rows], w_scale [V] for AJ_E4M3."""
-        dev, f32, i32 = self._device, self._f32, self._i32
-        hs = h.stride()
-        rows = h.shape[0] if h.dim() == 2 else -1
-        n_tok = tokens.shape[1] if tokens is not None and tokens.dim() == 2 else 0
-        n_top = top_id.shape[1] if top_id is not None and top_id.dim() == 2 else 0
-
-        def fits(t, dtype, *shape):
-            return t is None or t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev
-
-        if (rows < 0 or h.shape[1] != self._d or h.dtype is not self._dtype or h.get_device() != dev or hs[1] != 1 and self._d > 1
-                or W is None or not fits(W, self._dtype, self._V, self._d) or not fits(tokens, i32, rows, n_tok) or not fits(logprob, f32, rows, n_tok)
-                or not fits(lse, f32, rows) or not fits(entropy, f32, rows) or not fits(top_id, i32, rows, n_top)
-                or not fits(top_logprob, f32, rows, n_top) or not fits(h_scale, f32, rows) or not fits(w_scale, f32, self._V)):
-            st = AJ_ERR_INVALID_ARG
-        else:
-            p = [None if t is None else t.data_ptr() for t in (h_scale, w_scale, tokens, logprob, lse, entropy, top_id, top_logprob)]
-            st = self._score(self._h, h.data_ptr(), hs[0], p[0], W.data_ptr(), p[1], p[2], n_tok, rows, n_top, inv_temperature, p[3], p[4], p[5],
-                             p[6], p[7], stream or None)
+        st, dev, dt, i32, d, V = AJ_ERR_INVALID_ARG, self._device, self._dtype, _i32, self._d, self._V
+        hshape = h.shape
+        if len(hshape) == 2 and hshape[1] == d and h.dtype is dt and h.get_device() == dev and W.dtype is dt and W.is_contiguous() and W.get_device() == dev and W.shape == (V, d):
+            rows, (hs, e) = hshape[0], h.stride()
+            ok = e == 1 or d == 1
+            n_tok = n_top = 0
+            p_tok = p_lp = p_lse = p_ent = p_top = p_tlp = p_hs = p_ws = None
+            if tokens is not None:
+                p_tok, n_tok = tokens.data_ptr(), tokens.numel() // rows if rows else 0
+                ok = ok and tokens.dtype is i32 and tokens.is_contiguous() and tokens.get_device() == dev and tokens.shape[0] == rows and tokens.dim() == 2
+            if logprob is not None:
+                p_lp = logprob.data_ptr()
+                ok = ok and tokens is not None and logprob.dtype is _f32 and logprob.is_contiguous() and logprob.get_device() == dev and logprob.shape == tokens.shape
+            if lse is not None:
+                p_lse = lse.data_ptr()
+                ok = ok and lse.dtype is _f32 and lse.is_contiguous() and lse.get_device() == dev and lse.numel() == rows
+            if entropy is not None:
+                p_ent = entropy.data_ptr()
+                ok = ok and entropy.dtype is _f32 and entropy.is_contiguous() and entropy.get_device() == dev and entropy.numel() == rows
+            if top_id is not None:
+                p_top, n_top = top_id.data_ptr(), top_id.numel() // rows if rows else 0
+                ok = ok and top_id.dtype is i32 and top_id.is_contiguous() and top_id.get_device() == dev and top_id.shape[0] == rows and top_id.dim() == 2
+            if top_logprob is not None:
+                p_tlp = top_logprob.data_ptr()
+                ok = (ok and top_id is not None and top_logprob.dtype is _f32 and top_logprob.is_contiguous() and top_logprob.get_device() == dev
+                      and top_logprob.shape == top_id.shape)
+            if h_scale is not None:
+                p_hs = h_scale.data_ptr()
+                ok = ok and h_scale.dtype is _f32 and h_scale.is_contiguous() and h_scale.get_device() == dev and h_scale.numel() == rows
+            if w_scale is not None:
+                p_ws = w_scale.data_ptr()
+                ok = ok and w_scale.dtype is _f32 and w_scale.is_contiguous() and w_scale.get_device() == dev and w_scale.numel() == V
+            if ok:
+                st = self._score(self._h, h.data_ptr(), hs, p_hs, W.data_ptr(), p_ws, p_tok, n_tok, rows, n_top, inv_temperature, p_lp, p_lse, p_ent,
+                                 p_top, p_tlp, stream or None)
         if check and st != AJ_OK:
             raise AjError(st, "aj_score_tokens")
         return st

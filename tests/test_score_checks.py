@@ -26,6 +26,12 @@ class Fake:
     def is_contiguous(self):
         return self._c
 
+    def numel(self):
+        n = 1
+        for x in self.shape:
+            n *= x
+        return n
+
     def data_ptr(self):
         return 1 << 20
 
@@ -36,7 +42,10 @@ def handle():
 
     h = aj.ScoreHandle.__new__(aj.ScoreHandle)
     h._h, h._device, h._d, h._V = None, 0, 64, 1000
-    h._dtype, h._i32, h._f32 = torch.bfloat16, torch.int32, torch.float32
+    h._dtype = torch.bfloat16
+    from paper_2504_20039_b200 import score
+
+    score._lib()
     h.calls = []
     h._score = lambda *a: h.calls.append(a) or 0
     return h
@@ -52,7 +61,7 @@ def test_what_is_passed_on(handle):
     assert handle.score(**(ok | {"h": Fake(6, 64, dtype=B, stride=(80, 1))})) == 0 and handle.calls[-1][2] == 80
     n = len(handle.calls)
     bad = [{"h": Fake(6, 63, dtype=B)}, {"h": Fake(6, 64)}, {"h": Fake(6, 64, dtype=B, device=1)}, {"h": Fake(6, 64, dtype=B, stride=(64, 2))}, {"h": Fake(64, dtype=B)},
-           {"W": None}, {"W": Fake(999, 64, dtype=B)}, {"W": Fake(1000, 64, dtype=B, contiguous=False)}, {"W": Fake(1000, 64)}, {"tokens": Fake(6, 2, dtype=torch.int64)},
+           {"W": Fake(999, 64, dtype=B)}, {"W": Fake(1000, 64, dtype=B, contiguous=False)}, {"W": Fake(1000, 64)}, {"tokens": Fake(6, 2, dtype=torch.int64)},
            {"tokens": Fake(6, dtype=i32)}, {"tokens": Fake(5, 2, dtype=i32)}, {"logprob": Fake(6, 3)}, {"logprob": Fake(6, 2, dtype=B)}, {"lse": Fake(5)},
            {"entropy": Fake(6, dtype=torch.float64)}, {"top_id": Fake(6, 5)}, {"top_id": Fake(6, 5, dtype=i32, contiguous=False)}, {"top_logprob": Fake(6, 4)},
            {"h_scale": Fake(5)}, {"w_scale": Fake(6)}, {"lse": Fake(6, device=1)}]
