@@ -49,8 +49,8 @@ aj_status aj_add_norm(int device, const void *x, long long x_stride, const void 
  *   max_rows   rows of hidden states a later call may bring
  *   dtype      storage of the hidden states and of W: AJ_BF16, AJ_F32 or AJ_E4M3
  *   max_top    alternatives a later call may ask for (0 .. AJ_SCORE_MAX_TOP)
- * The handle owns a device workspace: logits of up to 2560 rows at a time (4 bytes each) and per-tile sums; more rows are
- * worked off in groups.  Calls on one handle share it, so calls that overlap on the GPU race.  Ready for any stream on return.
+ * The handle owns a device workspace: logits of up to 2560 rows at a time (4 bytes each, about 2 GB at most) and per-tile
+ * sums; more rows are worked off in groups.  Calls on one handle share it, so calls that overlap on the GPU race.  Ready for any stream on return.
  * Errors: AJ_ERR_INVALID_ARG, AJ_ERR_UNSUPPORTED (d > 65536, V > 2^21), AJ_ERR_CUDA, AJ_ERR_NOT_SM100.
  */
 aj_status aj_score_create(aj_score *out, int device, int max_rows, int d, int V, int dtype, int max_top, unsigned flags);

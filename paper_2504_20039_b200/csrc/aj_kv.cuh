@@ -94,7 +94,8 @@ cudaError_t launch_attend_simt(const AttendArgs &a, bool bf16, int num_sms, cuda
 // lengths); 20 rows and more pass the registers of the first.  Accumulating the weight: 4 rows 74 and 82 us, 16 rows 85 and
 // 87, 20 rows 90 and 88, 132 rows (8 sequences) 70 and 34.
 constexpr int FEW_ROWS = 16;
-cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap = false);
+// (of a shared call: as a programmatic dependent of the kernel over the shared slots, on num_sms SMs)
+cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s);
 size_t few_parts_floats(int D, int num_sms);
 // many rows: at most 128 query heads per key head; bf16, head size 64 or 128
 // maps: K pages, V pages, queries in boxes of one token and of eight; q_tma: 0 if the queries have no maps, 1 if only boxes
@@ -148,9 +149,10 @@ __device__ inline float2 *pre_ml(const AttendArgs &a, int chunk, int h, int rowg
     return a.pre_ml + ((size_t)chunk * a.v.Hkv + h) * ((size_t)a.v.pre_rows * a.v.G) + rowg;
 }
 
-__device__ inline Seq seq_of(const View &v, int b) {
+// SHARED: of a shared call, with its chunks.  (Asked of every call, this cost 1 to 18 % of others' time.)
+template <bool SHARED = false> __device__ inline Seq seq_of(const View &v, int b) {
     Seq s;
-    if (b < v.lead) {
+    if (SHARED && b < v.lead) {
         const Rows r = rows_of(v);
         s.row0 = r.base;
         s.nq = s.ahead = r.n;
@@ -158,7 +160,7 @@ __device__ inline Seq seq_of(const View &v, int b) {
         s.L = min(v.shared, s.first + v.chunk);
         return s;
     }
-    b -= v.lead;
+    if (SHARED) b -= v.lead;
     s.L = min(max(__ldg(v.lens + b), 0), v.cap);
     if (v.q_start) {
         s.row0 = __ldg(v.q_start + b);
@@ -167,7 +169,7 @@ __device__ inline Seq seq_of(const View &v, int b) {
         s.row0 = b * v.n_q;
         s.nq = v.n_q;
     }
-    if (v.shared) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
+    if (SHARED) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
         const Rows r = rows_of(v);
         if (s.L - s.nq >= v.shared && s.row0 >= r.base && s.nq <= r.n && s.row0 - r.base <= r.n - s.nq) s.first = v.shared;
     }
@@ -175,8 +177,9 @@ __device__ inline Seq seq_of(const View &v, int b) {
 }
 
 // Number of the page that holds a slot; a number outside the pool reads page 0.
-__device__ inline int page_of(const View &v, int b, int slot) {
-    const int p = __ldg((b < v.lead ? v.lead_table : v.table + (size_t)(b - v.lead) * v.width) + (slot >> v.page_shift));
+template <bool SHARED = false> __device__ inline int page_of(const View &v, int b, int slot) {
+    const int *row = SHARED && b < v.lead ? v.lead_table : v.table + (size_t)(SHARED ? b - v.lead : b) * v.width;
+    const int p = __ldg(row + (slot >> v.page_shift));
     return (unsigned)p < (unsigned)v.n_pages ? p : 0;
 }
 

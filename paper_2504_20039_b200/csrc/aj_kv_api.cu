@@ -398,6 +398,7 @@ aj_status aj_kv_reserve_shared(aj_kv h, int max_rows) {
         free_shared(h);
         return AJ_OK;
     }
+    if (max_rows <= h->pre_rows) return AJ_OK;
     // the shared slots always go to the tcgen05 kernel, which a handle for single tokens was not made for
     if (!h->encode) {
         if (!prepare_maps(h) || !encode_pages(h, h->parts)) {
@@ -474,7 +475,7 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
         p.parts = h->pre_parts;
         p.counters = h->pre_counters;
         e = kv::launch_attend_umma(p, maps, q_tma, ctas, s);
-        if (e == cudaSuccess) e = kv::launch_attend_few(a, h->num_sms - ctas, s, true);
+        if (e == cudaSuccess) e = kv::launch_attend_few(a, h->num_sms - ctas, s);
     } else {
         h->last_path = "shared_umma";
         h->last_launches = 2;
@@ -560,6 +561,8 @@ aj_status aj_kv_last_status(aj_kv h) {
     }
     // a call that gave up may have left items without their last arrival: the counts of later calls begin at zero again
     if (s != 0 && (zero_now(h->counters, ((size_t)h->n_counters + h->max_B) * 4) != cudaSuccess || zero_now(h->status, 4) != cudaSuccess))
+        return AJ_ERR_CUDA;
+    if (s != 0 && h->pre && (zero_now(h->pre_counters, (size_t)h->num_sms * 8) != cudaSuccess || kv::mark_now(h->own_ml, (size_t)h->pre_rows * h->Hq) != cudaSuccess))
         return AJ_ERR_CUDA;
     return s == DEV_TIMEOUT ? AJ_ERR_TIMEOUT : AJ_OK;
 }

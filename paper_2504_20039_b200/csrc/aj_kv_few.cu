@@ -57,7 +57,7 @@ struct Cursor {
     Span sp;
 };
 
-template <int D, int NT>
+template <int D, int NT, bool SHARED>
 __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a) {
     using C = Few<D, NT>;
     constexpr int ROWB = D * 2, CPR = D / 8, RPI = 32 / CPR, KS = D / 16;
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
     int base = 0;
     for (int b0 = 0; b0 < v.B; b0 += 32 * WARPS) {
         const int b = b0 + threadIdx.x;
-        int n = b < v.B ? span_of(v, seq_of(v, b)).units * v.Hkv : 0;
+        int n = b < v.B ? span_of(v, seq_of<SHARED>(v, b)).units * v.Hkv : 0;
         const int own = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -96,9 +96,9 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
     const int u0 = min(total, (int)blockIdx.x * per), u1 = min(total, u0 + per);
     // A shared call: the kernel before it (over the shared slots) and this one run side by side; the join waits for this one only,
     // so this one waits for the other before it ends.
-    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (SHARED) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (u0 >= u1) {
-        if (v.shared) asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (SHARED) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
 
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
             if (pre[mid] <= u) lo = mid; else hi = mid;
         }
         c.b = lo;
-        c.s = seq_of(v, lo);
+        c.s = seq_of<SHARED>(v, lo);
         c.sp = span_of(v, c.s);
         const int r = u - pre[lo];
         c.h = r / c.sp.units;
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
         do {
             if (++c.b >= v.B) return;
         } while (pre[c.b] == pre[c.b + 1]);
-        c.s = seq_of(v, c.b);
+        c.s = seq_of<SHARED>(v, c.b);
         c.sp = span_of(v, c.s);
     };
     auto slot_of = [&](const Cursor &c) {  // first slot of this warp's 16 in the cursor's block
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
                     }
                 }
             auto store = [&](int r, int d, float4 x, float mm, float ll) {  // four elements of an output row
-                if (v.shared && cur.s.first) {  // a part of the row, to be joined with the shared slots'
+                if (SHARED && cur.s.first) {  // a part of the row, to be joined with the shared slots
                     const int rr = cur.s.row0 - rows_of(v).base, rowg = rr * v.G + r;
                     *reinterpret_cast<float4 *>(pre_o(a, v.n_chunks, cur.h, rowg) + d) = x;
                     if (d == 0) a.own_ml[(size_t)(rr + r / v.G) * v.Hq + cur.h * v.G + r % v.G] = make_float2(mm, ll);
@@ -401,13 +401,13 @@ __global__ void __launch_bounds__(32 * WARPS, 2) attend_few_kernel(AttendArgs a)
         advance(cur);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (v.shared) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (SHARED) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap) {
+template <int D, int NT, bool SHARED> cudaError_t few(const AttendArgs &a, int num_sms, cudaStream_t s) {
     using C = Few<D, NT>;
     const size_t smem = (size_t)STAGES * C::STAGE + C::SCRATCH + (a.v.B + 1) * 4;
-    auto kernel = attend_few_kernel<D, NT>;
+    auto kernel = attend_few_kernel<D, NT, SHARED>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * num_sms < C::MAX_PARTS ? 2 * num_sms : C::MAX_PARTS);
     cfg.blockDim = dim3(32 * WARPS);
@@ -417,25 +417,34 @@ template <int D, int NT> cudaError_t few(const AttendArgs &a, int num_sms, cudaS
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = overlap ? 1 : 0;
+    cfg.numAttrs = SHARED ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 }  // namespace
 
+template <bool SHARED> static cudaError_t prepare() {
+    cudaError_t e = allow_shared(attend_few_kernel<64, 1, SHARED>);
+    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<64, 2, SHARED>);
+    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<128, 1, SHARED>);
+    return e == cudaSuccess ? allow_shared(attend_few_kernel<128, 2, SHARED>) : e;
+}
+
 cudaError_t prepare_attend_few() {
-    cudaError_t e = allow_shared(attend_few_kernel<64, 1>);
-    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<64, 2>);
-    if (e == cudaSuccess) e = allow_shared(attend_few_kernel<128, 1>);
-    return e == cudaSuccess ? allow_shared(attend_few_kernel<128, 2>) : e;
+    const cudaError_t e = prepare<false>();
+    return e == cudaSuccess ? prepare<true>() : e;
 }
 
 size_t few_parts_floats(int D, int num_sms) { return (size_t)(2 * num_sms < 296 ? 2 * num_sms : 296) * 2 * 16 * (D + 2); }
 
-cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s, bool overlap) {
+template <bool SHARED> static cudaError_t launch(const AttendArgs &a, int num_sms, cudaStream_t s) {
     const bool one = a.v.n_q * a.v.G <= 8;
-    if (a.v.D == 64) return one ? few<64, 1>(a, num_sms, s, overlap) : few<64, 2>(a, num_sms, s, overlap);
-    return one ? few<128, 1>(a, num_sms, s, overlap) : few<128, 2>(a, num_sms, s, overlap);
+    if (a.v.D == 64) return one ? few<64, 1, SHARED>(a, num_sms, s) : few<64, 2, SHARED>(a, num_sms, s);
+    return one ? few<128, 1, SHARED>(a, num_sms, s) : few<128, 2, SHARED>(a, num_sms, s);
+}
+
+cudaError_t launch_attend_few(const AttendArgs &a, int num_sms, cudaStream_t s) {
+    return a.v.shared ? launch<true>(a, num_sms, s) : launch<false>(a, num_sms, s);
 }
 
 }  // namespace kv

@@ -66,13 +66,13 @@ template <int D> struct Cfg {
 };
 
 // Prefix sums over the sequences of their tiles, by all threads; returns the total.
-__device__ inline long long build_line(const View &v, int tpt, long long *pre) {
+template <bool SHARED> __device__ inline long long build_line(const View &v, int tpt, long long *pre) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (v.n_q <= 16 * tpt) {  // few pieces: a thread per sequence; else a warp
-        for (int b = threadIdx.x; b < v.B; b += blockDim.x) pre[b + 1] = units_of(v, pieces_of(seq_of(v, b), tpt), tpt, 0, 1) * v.Hkv;
+        for (int b = threadIdx.x; b < v.B; b += blockDim.x) pre[b + 1] = units_of(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, 0, 1) * v.Hkv;
     } else {
         for (int b = warp; b < v.B; b += blockDim.x >> 5) {
-            long long u = units_of(v, pieces_of(seq_of(v, b), tpt), tpt, lane, 32);
+            long long u = units_of(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, lane, 32);
 #pragma unroll
             for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
             if (lane == 0) pre[b + 1] = u * v.Hkv;
@@ -98,7 +98,7 @@ __device__ inline long long build_line(const View &v, int tpt, long long *pre) {
 }
 
 // By a whole warp.
-__device__ inline Line seek(const View &v, int tpt, const long long *pre, long long u) {
+template <bool SHARED> __device__ inline Line seek(const View &v, int tpt, const long long *pre, long long u) {
     Line c;
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = v.B;  // pre[lo] <= u < pre[hi]
@@ -107,7 +107,7 @@ __device__ inline Line seek(const View &v, int tpt, const long long *pre, long l
         if (pre[mid] <= u) lo = mid; else hi = mid;
     }
     c.b = lo;
-    c.q = pieces_of(seq_of(v, lo), tpt);
+    c.q = pieces_of(seq_of<SHARED>(v, lo), tpt);
     const long long per_head = (pre[lo + 1] - pre[lo]) / v.Hkv;
     long long r = u - pre[lo];
     c.h = (int)(r / per_head);
@@ -134,7 +134,7 @@ __device__ inline Line seek(const View &v, int tpt, const long long *pre, long l
 }
 
 // To the first tile of the next item.
-__device__ inline void next_item(const View &v, int tpt, Line &c) {
+template <bool SHARED> __device__ inline void next_item(const View &v, int tpt, Line &c) {
     c.unit = -CHARGE;
     if (++c.qt == c.q.n) {
         c.qt = 0;
@@ -142,7 +142,7 @@ __device__ inline void next_item(const View &v, int tpt, Line &c) {
             c.h = 0;
             do {
                 if (++c.b >= v.B) return;
-                c.q = pieces_of(seq_of(v, c.b), tpt);
+                c.q = pieces_of(seq_of<SHARED>(v, c.b), tpt);
             } while (c.q.n == 0);
         }
     }
@@ -220,7 +220,7 @@ __device__ inline uint32_t pack2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t *>(&p);
 }
 
-template <int D>
+template <int D, bool SHARED>
 __global__ void __launch_bounds__(THREADS, 1)
 attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ CUtensorMap tmap_q1,
                    const __grid_constant__ CUtensorMap tmap_q8, AttendArgs a, int tpt, int g_shift, int q_tma) {
@@ -243,7 +243,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     long long *pre = reinterpret_cast<long long *>(smem + 2 * C::TILE_BYTES);  // the line's prefix sums lie in the ring until the first copy
     const View &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // warp: uniform
-    if (v.shared) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // what comes behind waits for its part itself
+    if (SHARED) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // what comes behind waits for its part itself
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < NS; s++) {
@@ -265,15 +265,15 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         fence_barrier_init();
     }
     if (warp == 8) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
-    const long long total = build_line(v, tpt, pre);  // synchronises the CTA
+    const long long total = build_line<SHARED>(v, tpt, pre);  // synchronises the CTA
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     // a piece of less than four tiles costs more in the join than its tiles (one window of 17 rows: 35 -> 28 us)
     // (a CTA's places fit an int, the line's need not; see the bounds at units_of)
-    int per = (int)max(v.align ? 1ll : 4ll, (total + gridDim.x - 1) / gridDim.x);
-    if (v.align) per = (per + v.align - 1) / v.align * v.align;
+    int per = (int)max(SHARED && v.align ? 1ll : 4ll, (total + gridDim.x - 1) / gridDim.x);
+    if (SHARED && v.align) per = (per + v.align - 1) / v.align * v.align;
     const long long u0 = min(total, (long long)blockIdx.x * per);
     const int u1 = (int)(min(total, u0 + per) - u0);  // from here on places are counted from u0
     auto give_up = [&]() {
@@ -284,7 +284,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (u1 > 0) {
         if (warp >= 8) {
           asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_OTHER));
-          Line c = seek(v, tpt, pre, u0);
+          Line c = seek<SHARED>(v, tpt, pre, u0);
           fence_async_shared();
           __syncthreads();  // the prefix sums are read: the ring may be filled
           if (warp == 9) {
@@ -294,7 +294,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const uint32_t box_bytes = (uint32_t)v.page * 128u;
             uint32_t g = 0;
             bool ok = true;
-            for (int u = 0; ok && u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; ok && u < u1; next_item<SHARED>(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -307,7 +307,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     // length and pages that no row of the item sees are not fetched.
                     const int slot0 = tile_of(c.p, pt.first + t) * TILE, slot = slot0 + (lane << v.page_shift);
                     const bool on = lane < per_tile && slot < c.q.s.L && (slot + v.page > c.p.first || slot < v.sinks);
-                    const int row = on ? (page_of(v, c.b, slot) * v.Hkv + c.h) << v.page_shift : 0;
+                    const int row = on ? (page_of<SHARED>(v, c.b, slot) * v.Hkv + c.h) << v.page_shift : 0;
                     const unsigned which = __ballot_sync(~0u, on);
                     ok = __all_sync(~0u, mbar_wait(empty(s), ((g / NS) & 1u) ^ 1u, abort_flag));
                     if (!ok) {
@@ -352,7 +352,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // 10,000 cycles per item where TMA takes 1,500).  Rows past its tokens keep what they held: no other row
             // depends on them.  The next item's come in while the softmax and the last product of this one run.
             uint32_t n_q[2] = {0, 0};  // items whose queries have been asked for
-            for (int u = 0; u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; u < u1; next_item<SHARED>(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 u += pt.line;
                 for (int x = 0; x < 2 && pt.n > 0; x++) {
@@ -419,7 +419,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             };
             // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
             // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
-            for (int u = 0; ok && u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; ok && u < u1; next_item<SHARED>(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
@@ -511,7 +511,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         } else {
             // ---------------------------------------------------------------- softmax of stream x
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_SOFTMAX));
-            Line c = seek(v, tpt, pre, u0);
+            Line c = seek<SHARED>(v, tpt, pre, u0);
             // rows of a query tile without a token stay zero (or what an item before had there): the tensor cores draw less
             // power on zeros, and power is what limits the clock
             for (int i = threadIdx.x; i < 2 * C::TILE_BYTES / 16; i += 256) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0, 0, 0, 0);
@@ -533,7 +533,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const float scale = a.scale_log2;
             const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31) == 0;  // rows on 32 bytes
             auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
-            for (int u = 0; u < u1; next_item(v, tpt, c)) {
+            for (int u = 0; u < u1; next_item<SHARED>(v, tpt, c)) {
                 const Part pt = part_of(c, u1 - u);
                 const int n = pt.n, unit = c.unit;
                 u += pt.line;
@@ -722,7 +722,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;  // a sum that is NaN stays one
                     const int t_row = token(row), g_row = row - t_row * v.G;
                     // a shared call: a part of the row, to be joined with the others
-                    const int part_of_row = c.b < v.lead ? c.b : v.shared && c.p.first ? v.n_chunks : -1;
+                    const int part_of_row = !SHARED ? -1 : c.b < v.lead ? c.b : c.p.first ? v.n_chunks : -1;
                     const int rel = part_of_row >= 0 ? c.q.s.row0 - rows_of(v).base + ta + t_row : 0;
                     float *po = part_of_row >= 0 ? pre_o(a, part_of_row, c.h, rel * v.G + g_row) : nullptr;
                     const size_t out_row = (size_t)c.q.s.row0 + ta + t_row;
@@ -805,10 +805,10 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (warp == 8) tmem_dealloc(*tmem_slot, 512);
 }
 
-template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
+template <int D, bool SHARED> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
     using C = Cfg<D>;
     const int tpt = 128 / a.v.G;
-    auto kernel = attend_umma_kernel<D>;
+    auto kernel = attend_umma_kernel<D, SHARED>;
     int g_shift = -1;  // log2 of the query heads per key head, if it is a power of two
     for (int i = 0; i < 8; i++)
         if (a.v.G == 1 << i) g_shift = i;
@@ -821,12 +821,15 @@ template <int D> cudaError_t umma(const AttendArgs &a, const CUtensorMap (&maps)
 size_t umma_parts_floats(int D, int num_sms) { return (size_t)num_sms * 2 * 256 * (D + 2); }
 
 cudaError_t prepare_attend_umma() {
-    const cudaError_t e = allow_shared(attend_umma_kernel<64>);
-    return e == cudaSuccess ? allow_shared(attend_umma_kernel<128>) : e;
+    cudaError_t e = allow_shared(attend_umma_kernel<64, false>);
+    if (e == cudaSuccess) e = allow_shared(attend_umma_kernel<64, true>);
+    if (e == cudaSuccess) e = allow_shared(attend_umma_kernel<128, false>);
+    return e == cudaSuccess ? allow_shared(attend_umma_kernel<128, true>) : e;
 }
 
 cudaError_t launch_attend_umma(const AttendArgs &a, const CUtensorMap (&maps)[4], int q_tma, int num_sms, cudaStream_t s) {
-    return a.v.D == 64 ? umma<64>(a, maps, q_tma, num_sms, s) : umma<128>(a, maps, q_tma, num_sms, s);
+    if (a.v.shared) return a.v.D == 64 ? umma<64, true>(a, maps, q_tma, num_sms, s) : umma<128, true>(a, maps, q_tma, num_sms, s);
+    return a.v.D == 64 ? umma<64, false>(a, maps, q_tma, num_sms, s) : umma<128, false>(a, maps, q_tma, num_sms, s);
 }
 
 }  // namespace kv

@@ -111,6 +111,15 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
     const int tok = threadIdx.x < a.n_tok ? a.tokens[(size_t)m * a.n_tok + threadIdx.x] : -1;
     if (threadIdx.x == 0) n_found = n_left[0] = n_left[1] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float4 sums[DIRECT_TILES];
+    if (a.direct) {
+        for (int t = warp; t < a.n_v; t += WARPS) {
+            const float4 q = part_of_tile(logits + (size_t)t * a.tile, a.tile, c);
+            if (lane == 0) sums[t] = q;
+        }
+        __syncthreads();
+        parts = sums;
+    }
     float4 p[KEEP];
 #pragma unroll
     for (int j = 0; j < KEEP; j++) p[j] = threadIdx.x + j * THREADS < a.n_v ? parts[threadIdx.x + j * THREADS] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
@@ -207,7 +216,7 @@ cudaError_t prepare_finish() {
     return cudaFuncSetAttribute(finish_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - (int)fa.sharedSizeBytes);
 }
 
-cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s) {
+cudaError_t launch_finish(const Args &a, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)a.rows);
     cfg.blockDim = dim3(THREADS);
@@ -217,7 +226,7 @@ cudaError_t launch_finish(const Args &a, bool overlap, cudaStream_t s) {
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = overlap;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, finish_kernel, a);

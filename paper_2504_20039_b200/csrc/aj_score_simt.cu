@@ -2,9 +2,10 @@
 //
 //   logits[m, v] = sum_k h[m, k] W[v, k]   one fixed order over k, f32
 //
-// Up to 8 rows: a warp per entry, its lanes along k, all rows at once; bound by the stream of W.  More rows: a CTA of 256
-// threads computes a tile of 64 rows x 64 entries from k-slices of 32 staged in shared memory as f32, 4 x 4 outputs per thread; bound by
-// the reads of shared memory that feed the multiply-adds.  A second kernel, a warp per row and tile, makes the tiles' sums.
+// Up to 8 rows: a warp per entry, its lanes along k (16 bytes at a time in f32), all rows at once; bound by the stream of W.
+// More rows: a CTA of 256 threads computes a tile of 64 rows x 128 entries, 8 x 4 outputs per thread, from k-slices of 16 in shared
+// memory as f32; the next slice is fetched into registers meanwhile.  Bound by the multiply-adds and the reads of shared memory that
+// feed them.  A second kernel, a warp per row and tile, makes the tiles' sums; a head of few tiles leaves that to the last step.
 #include "aj_score.cuh"
 
 namespace aj {
@@ -12,26 +13,37 @@ namespace score {
 
 namespace {
 
-constexpr int BV = 64, BK = 32;
-
 template <typename T> __device__ inline float widen(T x);
 template <> __device__ inline float widen<float>(float x) { return x; }
 template <> __device__ inline float widen<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <> __device__ inline float widen<__nv_fp8_e4m3>(__nv_fp8_e4m3 x) { return float(x); }
 
-// Up to 8 rows: a warp takes entries in turn.
-template <typename T> __global__ void __launch_bounds__(256) few_logits_kernel(Args a) {
+// Up to 8 rows: a warp takes entries in turn.  VEC: f32, rows on 16 bytes and whole 16-byte pieces.
+template <typename T, bool VEC> __global__ void __launch_bounds__(256) few_logits_kernel(Args a) {
     const T *h = (const T *)a.h, *W = (const T *)a.W;
     const int lane = threadIdx.x & 31;
     for (long long v = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); v < a.ld; v += (long long)gridDim.x * 8) {
         float acc[8] = {};
         if (v < a.V) {
-#pragma unroll 4
-            for (int k = lane; k < a.d; k += 32) {
-                const float w = widen(W[(size_t)v * a.d + k]);
+            if constexpr (VEC) {
+#pragma unroll 2
+                for (int k = lane * 4; k < a.d; k += 128) {
+                    const float4 w = __ldg(reinterpret_cast<const float4 *>(W + (size_t)v * a.d + k));
 #pragma unroll
-                for (int m = 0; m < 8; m++)
-                    if (m < a.rows) acc[m] += w * widen(h[(size_t)m * a.h_stride + k]);
+                    for (int m = 0; m < 8; m++) {
+                        if (m >= a.rows) break;
+                        const float4 x = __ldg(reinterpret_cast<const float4 *>(h + (size_t)m * a.h_stride + k));
+                        acc[m] += w.x * x.x + w.y * x.y + w.z * x.z + w.w * x.w;
+                    }
+                }
+            } else {
+#pragma unroll 4
+                for (int k = lane; k < a.d; k += 32) {
+                    const float w = widen(W[(size_t)v * a.d + k]);
+#pragma unroll
+                    for (int m = 0; m < 8; m++)
+                        if (m < a.rows) acc[m] += w * widen(h[(size_t)m * a.h_stride + k]);
+                }
             }
         }
 #pragma unroll
@@ -48,38 +60,44 @@ template <typename T> __global__ void __launch_bounds__(256) few_logits_kernel(A
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) logits_kernel(Args a) {
-    constexpr int TM = 64, RM = 4, RV = 4;  // outputs per thread
-    constexpr int TX = BV / RV;             // threads along the entries
-    static_assert(TX * (TM / RM) == 256, "256 threads cover the tile");
-    __shared__ float sh[BK][TM + 4], sw[BK][BV + 4];
+template <typename T> __global__ void __launch_bounds__(256) logits_kernel(Args a) {
+    constexpr int TM = 64, TV = 128, BK = 16, RM = 8, RV = 4, PH = TM * BK / 256, PW = TV * BK / 256;
+    __shared__ __align__(16) float sh[2][BK][TM + 4], sw[2][BK][TV + 4];
     const T *h = (const T *)a.h, *W = (const T *)a.W;
-    const int v0 = blockIdx.x * BV, m0 = blockIdx.y * TM;
-    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
+    const int v0 = blockIdx.x * TV, m0 = blockIdx.y * TM;
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;         // entries 4 tx .., rows 8 ty ..
+    const int lk = threadIdx.x & 15, lr = threadIdx.x >> 4;         // a thread fetches column lk of rows lr, lr + 16, ..
+    float rh[PH], rw[PW];
+    auto fetch = [&](int k0) {
+        const bool on = k0 + lk < a.d;
+#pragma unroll
+        for (int i = 0; i < PH; i++) rh[i] = on && m0 + lr + 16 * i < a.rows ? widen(h[(size_t)(m0 + lr + 16 * i) * a.h_stride + k0 + lk]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < PW; i++) rw[i] = on && v0 + lr + 16 * i < a.V ? widen(W[(size_t)(v0 + lr + 16 * i) * a.d + k0 + lk]) : 0.0f;
+    };
+    auto put = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < PH; i++) sh[b][lk][lr + 16 * i] = rh[i];
+#pragma unroll
+        for (int i = 0; i < PW; i++) sw[b][lk][lr + 16 * i] = rw[i];
+    };
     float acc[RM][RV] = {};
-    for (int k0 = 0; k0 < a.d; k0 += BK) {
-        for (int i = threadIdx.x; i < TM * BK; i += 256) {
-            const int m = i / BK, k = i % BK;
-            sh[k][m] = m0 + m < a.rows && k0 + k < a.d ? widen(h[(size_t)(m0 + m) * a.h_stride + k0 + k]) : 0.0f;
-        }
-        for (int i = threadIdx.x; i < BV * BK; i += 256) {
-            const int v = i / BK, k = i % BK;
-            sw[k][v] = v0 + v < a.V && k0 + k < a.d ? widen(W[(size_t)(v0 + v) * a.d + k0 + k]) : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll 8
+    fetch(0);
+    put(0);
+    __syncthreads();
+    for (int k0 = 0, b = 0; k0 < a.d; k0 += BK, b ^= 1) {
+        if (k0 + BK < a.d) fetch(k0 + BK);
+#pragma unroll
         for (int k = 0; k < BK; k++) {
-            float x[RM], y[RV];
-#pragma unroll
-            for (int i = 0; i < RM; i++) x[i] = sh[k][ty * RM + i];
-#pragma unroll
-            for (int j = 0; j < RV; j++) y[j] = sw[k][tx * RV + j];
+            const float4 x0 = *reinterpret_cast<const float4 *>(&sh[b][k][ty * RM]), x1 = *reinterpret_cast<const float4 *>(&sh[b][k][ty * RM + 4]);
+            const float4 w = *reinterpret_cast<const float4 *>(&sw[b][k][tx * RV]);
+            const float x[RM] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w}, y[RV] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < RM; i++)
 #pragma unroll
                 for (int j = 0; j < RV; j++) acc[i][j] += x[i] * y[j];
         }
+        if (k0 + BK < a.d) put(b ^ 1);
         __syncthreads();
     }
 #pragma unroll
@@ -100,34 +118,25 @@ __global__ void __launch_bounds__(256) logits_kernel(Args a) {
 
 // Largest logit, S and T of each tile of a row: a warp per tile.
 __global__ void __launch_bounds__(256) parts_kernel(Args a) {
-    const int lane = threadIdx.x & 31, t = blockIdx.x * 8 + (threadIdx.x >> 5), m = blockIdx.y;
+    const int t = blockIdx.x * 8 + (threadIdx.x >> 5), m = blockIdx.y;
     if (t >= a.n_v) return;
-    const float *x = a.logits + (size_t)m * a.ld + (size_t)t * a.tile;
-    const float c = a.inv_t * LOG2E;
-    float mx = -INFINITY;
-    for (int i = lane; i < a.tile; i += 32) mx = max_nan(mx, x[i]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(~0u, mx, o));
-    float S = 0.0f, T = 0.0f;
-    for (int i = lane; i < a.tile; i += 32) {
-        const float d = fmaxf((x[i] - mx) * c, -150.0f), e = ex2(d);
-        S += e;
-        T += d * e;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        S += __shfl_xor_sync(~0u, S, o);
-        T += __shfl_xor_sync(~0u, T, o);
-    }
-    if (lane == 0) a.parts[(size_t)m * a.n_v + t] = make_float4(mx, S, T, 0.0f);
+    const float4 p = part_of_tile(a.logits + (size_t)m * a.ld + (size_t)t * a.tile, a.tile, a.inv_t * LOG2E);
+    if ((threadIdx.x & 31) == 0) a.parts[(size_t)m * a.n_v + t] = p;
 }
 
 template <typename T> void logits(const Args &a, cudaStream_t s) {
-    const unsigned gx = (unsigned)((a.ld + BV - 1) / BV);
-    if (a.rows <= 8)
-        few_logits_kernel<T><<<(unsigned)((a.ld + 7) / 8 < 2048 ? (a.ld + 7) / 8 : 2048), 256, 0, s>>>(a);
-    else
-        logits_kernel<T><<<dim3(gx, (a.rows + 63) / 64), 256, 0, s>>>(a);
+    if (a.rows <= 8) {
+        const unsigned grid = (unsigned)((a.ld + 7) / 8 < 2048 ? (a.ld + 7) / 8 : 2048);
+        if constexpr (sizeof(T) == 4) {
+            if (((reinterpret_cast<uintptr_t>(a.h) | reinterpret_cast<uintptr_t>(a.W)) & 15) == 0 && a.d % 4 == 0 && (a.rows == 1 || a.h_stride % 4 == 0)) {
+                few_logits_kernel<T, true><<<grid, 256, 0, s>>>(a);
+                return;
+            }
+        }
+        few_logits_kernel<T, false><<<grid, 256, 0, s>>>(a);
+    } else {
+        logits_kernel<T><<<dim3((unsigned)((a.ld + 127) / 128), (a.rows + 63) / 64), 256, 0, s>>>(a);
+    }
 }
 
 }  // namespace
@@ -140,7 +149,7 @@ cudaError_t launch_simt(const Args &a, cudaStream_t s) {
     else
         logits<__nv_fp8_e4m3>(a, s);
     const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || a.direct) return e;
     parts_kernel<<<dim3((a.n_v + 7) / 8, a.rows), 256, 0, s>>>(a);
     return cudaGetLastError();
 }

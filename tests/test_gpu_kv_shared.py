@@ -115,7 +115,7 @@ def test_first_row_of_a_ragged_call():
     out = torch.full_like(q, 5.0)
     lse = torch.full((s.T + n, s.Hq), 5.0, device="cuda")
     h = s.handle(SHARED)
-    for rows in (s.T, 40):
+    for rows in (40, s.T):
         h.reserve_shared(rows)
         h.attend_shared(q, s.k, s.v, s.prefix, s.shared, s.block_table, s.seq_lens, out, s.B, s.max_n, s.scale, q_start=s.q_start + n, lse=lse)
         torch.cuda.synchronize()
