@@ -101,15 +101,15 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
     const int room = max(a.n_v, a.n_top * a.tile);
     unsigned long long *found = smem, *left = smem + room;
     __shared__ float red[3][WARPS];
-    __shared__ int chosen[64], n_found, n_left[2];
-    __shared__ uint32_t floor_image;
+    __shared__ int chosen[64], n_found, n_left[3];
+    __shared__ uint32_t floor_image, reached;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = blockIdx.x;
     const float4 *parts = a.parts + (size_t)m * a.n_v;
     const float *logits = a.logits + (size_t)m * a.ld;
     const float c = a.inv_t * LOG2E;
     // the given tokens are the caller's: their numbers can be read before the tiles are there
     const int tok = threadIdx.x < a.n_tok ? a.tokens[(size_t)m * a.n_tok + threadIdx.x] : -1;
-    if (threadIdx.x == 0) n_found = n_left[0] = n_left[1] = 0;
+    if (threadIdx.x == 0) n_found = n_left[0] = n_left[1] = n_left[2] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ float4 sums[DIRECT_TILES];
     if (a.direct) {
@@ -124,19 +124,25 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
 #pragma unroll
     for (int j = 0; j < KEEP; j++) p[j] = threadIdx.x + j * THREADS < a.n_v ? parts[threadIdx.x + j * THREADS] : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
     const float x_tok = (unsigned)tok < (unsigned)a.V ? logits[tok] : 0.0f;
-    if (a.gate && threadIdx.x < a.n_top) a.slots[(size_t)m * a.n_top + threadIdx.x] = 0u;
+    const bool gated = a.gate && a.n_top;  // the slots say what at least n_top tiles reach
+    if (gated && warp == 0) {
+        unsigned *slot = a.slots + (size_t)m * a.n_top + lane;
+        const uint32_t low = warp_min_u32(lane < a.n_top ? *slot : ~0u);
+        if (lane < a.n_top) *slot = 0u;
+        if (lane == 0) reached = low;
+    }
 
     float M = -INFINITY;
 #pragma unroll
     for (int j = 0; j < KEEP; j++) {
         const int t = threadIdx.x + j * THREADS;
         M = max_nan(M, p[j].x);
-        if (a.n_top && t < a.n_v) found[t] = key_of(p[j].x, t);
+        if (a.n_top && !gated && t < a.n_v) found[t] = key_of(p[j].x, t);
     }
     for (int t = threadIdx.x + KEEP * THREADS; t < a.n_v; t += THREADS) {
         const float x = parts[t].x;
         M = max_nan(M, x);
-        if (a.n_top) found[t] = key_of(x, t);
+        if (a.n_top && !gated) found[t] = key_of(x, t);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) M = max_nan(M, __shfl_xor_sync(~0u, M, o));
@@ -147,12 +153,26 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
     const bool fine = M > -INFINITY && M < INFINITY;  // false for NaN
     const float nan = __int_as_float(0x7fffffff);
     const int n_tiles = min(a.n_top, a.n_v);
-    if (n_tiles)
-        top_of(found, a.n_v, n_tiles, left, n_left, [&](unsigned long long k, int place) {
-            chosen[place] = (int)~(uint32_t)k;
-            // no alternative lies below the least of these tiles' largest (fewer tiles than alternatives: every entry counts)
-            if (place == n_tiles - 1) floor_image = a.n_top <= a.n_v ? (uint32_t)(k >> 32) : 0u;
-        });
+    auto choose = [&](unsigned long long k, int place) {
+        chosen[place] = (int)~(uint32_t)k;
+        // no alternative lies below the least of these tiles' largest (fewer tiles than alternatives: every entry counts)
+        if (place == n_tiles - 1) floor_image = a.n_top <= a.n_v ? (uint32_t)(k >> 32) : 0u;
+    };
+    if (gated) {  // a few more than n_top tiles, as a rule
+#pragma unroll
+        for (int j = 0; j < KEEP; j++) {
+            const int t = threadIdx.x + j * THREADS;
+            if (t < a.n_v && ordered_image(p[j].x) >= reached) found[atomicAdd(n_left, 1)] = key_of(p[j].x, t);
+        }
+        for (int t = threadIdx.x + KEEP * THREADS; t < a.n_v; t += THREADS) {
+            const float x = parts[t].x;
+            if (ordered_image(x) >= reached) found[atomicAdd(n_left, 1)] = key_of(x, t);
+        }
+        __syncthreads();
+        top_of(found, n_left[0], n_tiles, left, n_left + 1, choose);
+    } else if (n_tiles) {
+        top_of(found, a.n_v, n_tiles, left, n_left + 1, choose);
+    }
     float S = 0.0f, T = 0.0f;
     auto add = [&](const float4 &q) {
         const float d = fmaxf((q.x - M) * c, -150.0f), w = ex2(d);
@@ -204,7 +224,7 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
         for (int j = threadIdx.x; j < a.n_top; j += THREADS) put(j, j, nan);
         return;
     }
-    top_of(found, n_found, a.n_top, left, n_left + 1, [&](unsigned long long k, int place) { put(place, (int)~(uint32_t)k, logprob(key_value(k))); });
+    top_of(found, n_found, a.n_top, left, n_left + 2, [&](unsigned long long k, int place) { put(place, (int)~(uint32_t)k, logprob(key_value(k))); });
 }
 
 }  // namespace
