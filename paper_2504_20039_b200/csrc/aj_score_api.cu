@@ -96,7 +96,7 @@ aj_status aj_add_norm(int device, const void *x, long long x_stride, const void 
                       float eps, long long rows, int d, aj_dtype dtype, void *residual_out, long long residual_out_stride, void *out,
                       long long out_stride, void *out8, long long out8_stride, float *scale8, void *cuda_stream) {
     if (device < 0 || rows < 0 || d < 1 || (dtype != AJ_BF16 && dtype != AJ_F32) || !(eps >= 0.0f) || !(eps < 1e30f)) return AJ_ERR_INVALID_ARG;
-    if ((!out && !out8) || !out8 != !scale8) return AJ_ERR_INVALID_ARG;
+    if ((!out && !out8) || !out8 != !scale8 || (out && out == residual_out)) return AJ_ERR_INVALID_ARG;
     if (d > norm::MAX_D || rows > 0x7fffffffll) return AJ_ERR_UNSUPPORTED;
     if (rows == 0) return AJ_OK;
     if (!x || !weight) return AJ_ERR_INVALID_ARG;
@@ -223,8 +223,10 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
     if (!guard.ok()) return AJ_ERR_CUDA;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
     const bool tensor = h->tensor && !off(hidden, 16) && !off(W, 16) && (rows == 1 || h_stride * e % 16 == 0) && !off(w_scale, 16);
-    // groups of rows, evenly
-    const int n_groups = (rows + h->group - 1) / h->group, each = (rows + n_groups - 1) / n_groups;
+    // groups of rows, evenly, of whole row tiles
+    const int n_groups = (rows + h->group - 1) / h->group;
+    int each = (rows + n_groups - 1) / n_groups;
+    if (n_groups > 1) each = (each + 255) / 256 * 256 < h->group ? (each + 255) / 256 * 256 : h->group;
     for (int r0 = 0; r0 < rows; r0 += each) {
         score::Args a;
         a.h = (const char *)hidden + (size_t)r0 * h_stride * e;

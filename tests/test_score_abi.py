@@ -68,9 +68,9 @@ def test_norm_checks_need_no_device(built):
     f = score._lib()["aj_add_norm"]
     p = ctypes.c_void_p(1 << 20)
     #     device x  xs  r  rs  w  eps  rows d  dtype ro ros out os o8 o8s scale stream
-    ok = [0, p, 64, p, 64, p, 1e-5, 4, 64, 0, p, 64, p, 64, p, 64, p, None]
+    ok = [0, p, 64, p, 64, p, 1e-5, 4, 64, 0, ctypes.c_void_p(1 << 22), 64, p, 64, p, 64, p, None]
     for changes in [{0: -1}, {1: None}, {2: 63}, {4: 63}, {5: None}, {6: -1.0}, {6: float("nan")}, {7: -1}, {8: 0}, {9: 2}, {9: 7}, {11: 63}, {13: 63}, {15: 63},
-                    {12: None, 14: None, 16: None}, {14: None}, {16: None}, {1: ctypes.c_void_p(3)}, {5: ctypes.c_void_p(6)}]:
+                    {12: None, 14: None, 16: None}, {14: None}, {16: None}, {1: ctypes.c_void_p(3)}, {5: ctypes.c_void_p(6)}, {12: ctypes.c_void_p(1 << 21), 10: ctypes.c_void_p(1 << 21)}]:
         args = list(ok)
         for i, v in changes.items():
             args[i] = v
