@@ -6,6 +6,9 @@
 // More rows: a CTA of 256 threads computes a tile of 64 rows x 128 entries, 8 x 4 outputs per thread, from k-slices of 16 in shared
 // memory as f32; the next slice is fetched into registers meanwhile.  Bound by the multiply-adds and the reads of shared memory that
 // feed them.  A second kernel, a warp per row and tile, makes the tiles' sums; a head of few tiles leaves that to the last step.
+//
+// Measured, f32 (d = 4096): 5 rows, 128,256 entries 677 us, 3.1 TB/s; 264 rows, 32,000 entries 2365 us, 29 TFLOP/s; 17 rows, which fill a quarter of
+// a tile, 1832 us.
 #include "aj_score.cuh"
 
 namespace aj {

@@ -15,6 +15,10 @@
 //
 // bf16 and e4m3 differ in the instruction and in the scales that the epilogue puts on the sums (times h_scale, times w_scale).
 // Every logit is one sum over k in a fixed order.  Every wait is bounded (aj_ptx.cuh).
+//
+// Measured (d = 4096, 128,256 entries): 17 rows 162 us for 1.05 GB, 6.5 TB/s; in 8 bits 86 us, 6.1 TB/s; 2112 rows 1400 us alone, 1.58
+// PFLOP/s, and 1490 back to back, where the power limit lowers the clock (on zeros 1185); 2048 rows in 8 bits 750 us. 129 to 256 rows are bound
+// by W too (200 rows 204 us); 264 rows take as long as 512 (344 us), for whole row tiles are multiplied.
 #include "aj_score.cuh"
 #include "aj_ptx.cuh"
 
@@ -391,7 +395,7 @@ Plan plan_umma(int rows, int d, int V, int dtype, int tile, int num_sms, int max
     p.n_m = p.pair ? (rows + 255) / 256 : 1;
     p.box_rows = p.pair ? 128 : (rows + 7) & ~7;
     p.num_kb = (int)(((long long)d * (dtype == E4M3 ? 1 : 2) + 127) / 128);
-    // two k-blocks per stage, so that the issuing thread tests and commits half as often (2048 rows 1515 -> 1322 us, 17 rows 169 -> 166),
+    // two k-blocks per stage, so that the issuing thread tests and commits half as often (2048 rows 1515 -> 1350 us, 17 rows 169 -> 166),
     // where three such stages fit
     const int sub = (p.box_rows + (p.pair ? 128 : p.tile)) * 128;
     p.kps = p.num_kb % 2 == 0 && RING / (2 * sub) >= 3 ? 2 : 1;
