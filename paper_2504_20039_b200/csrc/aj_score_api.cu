@@ -96,9 +96,9 @@ aj_status aj_add_norm(int device, const void *x, long long x_stride, const void 
                       float eps, long long rows, int d, aj_dtype dtype, void *residual_out, long long residual_out_stride, void *out,
                       long long out_stride, void *out8, long long out8_stride, float *scale8, void *cuda_stream) {
     if (device < 0 || rows < 0 || d < 1 || (dtype != AJ_BF16 && dtype != AJ_F32) || !(eps >= 0.0f) || !(eps < 1e30f)) return AJ_ERR_INVALID_ARG;
+    if (rows == 0) return d > norm::MAX_D ? AJ_ERR_UNSUPPORTED : AJ_OK;  // (tensors without rows have no address)
     if ((!out && !out8) || !out8 != !scale8 || (out && out == residual_out)) return AJ_ERR_INVALID_ARG;
     if (d > norm::MAX_D || rows > 0x7fffffffll) return AJ_ERR_UNSUPPORTED;
-    if (rows == 0) return AJ_OK;
     if (!x || !weight) return AJ_ERR_INVALID_ARG;
     // a single row needs no stride
     auto short_rows = [&](const void *p, long long stride) { return p && rows > 1 && stride < d; };

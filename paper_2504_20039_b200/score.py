@@ -57,21 +57,30 @@ def add_norm(x, weight, eps: float = 1e-5, out=None, residual=None, residual_out
     dt, shape, dev = x.dtype, x.shape, x.get_device()
     if len(shape) == 2 and dt in _types and dev >= 0 and weight.dtype is _f32 and weight.numel() == shape[1] and weight.is_contiguous() and weight.get_device() == dev:
         xs = x.stride()
-        ok = xs[1] == 1 or shape[1] == 1
+        thin = shape[1] == 1  # rows of one element: any stride along them
+        ok = xs[1] == 1 or thin
         r = ro = o = o8 = s8 = None
         rs = ros = os = o8s = 0
         if residual is not None:
-            r, (rs, e) = residual.data_ptr(), residual.stride()
-            ok = ok and e == xs[1] and residual.dtype is dt and residual.shape == shape and residual.get_device() == dev
+            ok = ok and residual.dtype is dt and residual.shape == shape and residual.get_device() == dev
+            if ok:
+                r, (rs, e) = residual.data_ptr(), residual.stride()
+                ok = e == 1 or thin
         if residual_out is not None:
-            ro, (ros, e) = residual_out.data_ptr(), residual_out.stride()
-            ok = ok and e == xs[1] and residual_out.dtype is dt and residual_out.shape == shape and residual_out.get_device() == dev
+            ok = ok and residual_out.dtype is dt and residual_out.shape == shape and residual_out.get_device() == dev
+            if ok:
+                ro, (ros, e) = residual_out.data_ptr(), residual_out.stride()
+                ok = e == 1 or thin
         if out is not None:
-            o, (os, e) = out.data_ptr(), out.stride()
-            ok = ok and e == xs[1] and out.dtype is dt and out.shape == shape and out.get_device() == dev
+            ok = ok and out.dtype is dt and out.shape == shape and out.get_device() == dev
+            if ok:
+                o, (os, e) = out.data_ptr(), out.stride()
+                ok = e == 1 or thin
         if out8 is not None:
-            o8, (o8s, e) = out8.data_ptr(), out8.stride()
-            ok = ok and e == xs[1] and out8.dtype is _f8 and out8.shape == shape and out8.get_device() == dev
+            ok = ok and out8.dtype is _f8 and out8.shape == shape and out8.get_device() == dev
+            if ok:
+                o8, (o8s, e) = out8.data_ptr(), out8.stride()
+                ok = e == 1 or thin
         if scale8 is not None:
             s8 = scale8.data_ptr()
             ok = ok and scale8.dtype is _f32 and scale8.numel() == shape[0] and scale8.is_contiguous() and scale8.get_device() == dev
