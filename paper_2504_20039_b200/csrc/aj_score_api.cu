@@ -86,6 +86,8 @@ template <typename F> bool driver_entry(const char *name, F *out) {
     return true;
 }
 
+bool fits_int(int64_t x) { return x >= -0x7fffffffll && x <= 0x7fffffffll; }
+
 int elem(int dtype) { return dtype == AJ_BF16 ? 2 : dtype == AJ_F32 ? 4 : 1; }
 
 }  // namespace
@@ -129,6 +131,12 @@ aj_status aj_add_norm(int device, const void *x, long long x_stride, const void 
     const bool wide = d % 8 == 0 && !ragged(x, x_stride, e, 16) && !ragged(residual, residual_stride, e, 16) &&
                       !ragged(residual_out, residual_out_stride, e, 16) && !ragged(out, out_stride, e, 16) && !ragged(out8, out8_stride, 1, 8) && !off(weight, 16);
     return done(norm::launch(a, dtype == AJ_BF16, wide, (cudaStream_t)cuda_stream));
+}
+
+aj_status aj_add_norm_call(const aj_norm_args *a) {
+    if (!a || !fits_int(a->device) || !fits_int(a->d) || !fits_int(a->dtype)) return AJ_ERR_INVALID_ARG;
+    return aj_add_norm((int)a->device, a->x, a->x_stride, a->residual, a->residual_stride, a->weight, (float)a->eps, a->rows, (int)a->d, (aj_dtype)a->dtype,
+                       a->residual_out, a->residual_out_stride, a->out, a->out_stride, a->out8, a->out8_stride, a->scale8, a->cuda_stream);
 }
 
 aj_status aj_score_create(aj_score *out, int device, int max_rows, int d, int V, int dtype, int max_top, unsigned flags) {
@@ -281,6 +289,12 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
         if (err != cudaSuccess) return done(err);
     }
     return AJ_OK;
+}
+
+aj_status aj_score_call(aj_score h, const aj_score_args *a) {
+    if (!a || !fits_int(a->n_tok) || !fits_int(a->rows) || !fits_int(a->n_top)) return AJ_ERR_INVALID_ARG;
+    return aj_score_tokens(h, a->hidden, a->h_stride, a->h_scale, a->W, a->w_scale, a->tokens, (int)a->n_tok, (int)a->rows, (int)a->n_top,
+                           (float)a->inv_temperature, a->logprob, a->lse, a->entropy, a->top_id, a->top_logprob, a->cuda_stream);
 }
 
 aj_status aj_score_last_status(aj_score h) {

@@ -5,6 +5,7 @@ Tensors are torch tensors on the handle's device (strides and extents are read f
 from __future__ import annotations
 
 import ctypes
+import struct
 
 from . import binding
 from .binding import AJ_BF16, AJ_ERR_INVALID_ARG, AJ_F32, AJ_OK, AjError
@@ -13,12 +14,14 @@ AJ_E4M3 = 2
 AJ_SCORE_FLAG_FORCE_SIMT = 1
 AJ_SCORE_MAX_TOP, AJ_SCORE_MAX_TOKENS = 32, 1024
 
-EXPORTS = ("aj_add_norm", "aj_score_create", "aj_score_destroy", "aj_score_tokens", "aj_score_last_status", "aj_score_last_launch_count",
+EXPORTS = ("aj_add_norm", "aj_add_norm_call", "aj_score_create", "aj_score_destroy", "aj_score_tokens", "aj_score_call", "aj_score_last_status", "aj_score_last_launch_count",
            "aj_score_last_path")
 
 _vp, _ci, _cf, _cl, _cu = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_longlong, ctypes.c_uint
 _ARGS = {
     "aj_add_norm": [_ci, _vp, _cl, _vp, _cl, _vp, _cf, _cl, _ci, _ci, _vp, _cl, _vp, _cl, _vp, _cl, _vp, _vp],
+    "aj_add_norm_call": [ctypes.c_char_p],
+    "aj_score_call": [_vp, ctypes.c_char_p],
     "aj_score_create": [ctypes.POINTER(_vp), _ci, _ci, _ci, _ci, _ci, _ci, _cu],
     "aj_score_destroy": [_vp],
     "aj_score_tokens": [_vp, _vp, _cl, _vp, _vp, _vp, _vp, _ci, _ci, _ci, _cf, _vp, _vp, _vp, _vp, _vp, _vp],
@@ -26,6 +29,8 @@ _ARGS = {
     "aj_score_last_launch_count": [_vp],
     "aj_score_last_path": [_vp],
 }
+# aj_norm_args and aj_score_args: eight bytes a field; a pointer that is not given is 0
+_NORM_ARGS, _SCORE_ARGS = struct.Struct("6qd11q"), struct.Struct("9qd6q")
 _fns = _types = _f32 = _i32 = _f8 = _add_norm = None
 
 
@@ -41,7 +46,7 @@ def _lib():
             fn.argtypes, fn.restype = args, ctypes.c_char_p if name == "aj_score_last_path" else _ci
             fns[name] = fn
         _types = {torch.bfloat16: AJ_BF16, torch.float32: AJ_F32, torch.float8_e4m3fn: AJ_E4M3}
-        _f32, _i32, _f8, _add_norm = torch.float32, torch.int32, torch.float8_e4m3fn, fns["aj_add_norm"]
+        _f32, _i32, _f8, _add_norm = torch.float32, torch.int32, torch.float8_e4m3fn, fns["aj_add_norm_call"]
         _fns = fns
     return _fns
 
@@ -52,15 +57,14 @@ def add_norm(x, weight, eps: float = 1e-5, out=None, residual=None, residual_out
 
     x, residual, residual_out, out [rows, d] (rows may be strided) bf16 or f32, weight [d] f32, out8 [rows, d] float8_e4m3fn with
     scale8 [rows] f32: a row's values are out8 * scale8.  residual_out may be x or residual, out may be x or residual."""
-    fn = _add_norm or _lib()["aj_add_norm"]
+    fn = _add_norm or _lib()["aj_add_norm_call"]
     st = AJ_ERR_INVALID_ARG
     dt, shape, dev = x.dtype, x.shape, x.get_device()
     if len(shape) == 2 and dt in _types and dev >= 0 and weight.dtype is _f32 and weight.numel() == shape[1] and weight.is_contiguous() and weight.get_device() == dev:
         xs = x.stride()
         thin = shape[1] == 1  # rows of one element: any stride along them
         ok = xs[1] == 1 or thin
-        r = ro = o = o8 = s8 = None
-        rs = ros = os = o8s = 0
+        r = ro = o = o8 = s8 = rs = ros = os = o8s = 0
         if residual is not None:
             ok = ok and residual.dtype is dt and residual.shape == shape and residual.get_device() == dev
             if ok:
@@ -85,7 +89,7 @@ def add_norm(x, weight, eps: float = 1e-5, out=None, residual=None, residual_out
             s8 = scale8.data_ptr()
             ok = ok and scale8.dtype is _f32 and scale8.numel() == shape[0] and scale8.is_contiguous() and scale8.get_device() == dev
         if ok:
-            st = fn(dev, x.data_ptr(), xs[0], r, rs, weight.data_ptr(), eps, shape[0], shape[1], _types[dt], ro, ros, o, os, o8, o8s, s8, stream or None)
+            st = fn(_NORM_ARGS.pack(dev, x.data_ptr(), xs[0], r, rs, weight.data_ptr(), eps, shape[0], shape[1], _types[dt], ro, ros, o, os, o8, o8s, s8, stream or 0))
     if check and st != AJ_OK:
         raise AjError(st, "aj_add_norm")
     return st
@@ -105,7 +109,7 @@ class ScoreHandle:
         if st != AJ_OK:
             self._h = _vp()
             raise AjError(st, "aj_score_create")
-        self._score, self._device, self._d, self._V = f["aj_score_tokens"], device, d, V
+        self._score, self._device, self._d, self._V = f["aj_score_call"], device, d, V
         self._dtype = {AJ_BF16: torch.bfloat16, AJ_F32: torch.float32, AJ_E4M3: torch.float8_e4m3fn}[dtype]
 
     def score(self, h, W, tokens=None, logprob=None, lse=None, entropy=None, top_id=None, top_logprob=None, inv_temperature: float = 1.0,
@@ -120,7 +124,7 @@ class ScoreHandle:
             rows, (hs, e) = hshape[0], h.stride()
             ok = e == 1 or d == 1
             n_tok = n_top = 0
-            p_tok = p_lp = p_lse = p_ent = p_top = p_tlp = p_hs = p_ws = None
+            p_tok = p_lp = p_lse = p_ent = p_top = p_tlp = p_hs = p_ws = 0
             if tokens is not None:
                 p_tok, n_tok = tokens.data_ptr(), tokens.numel() // rows if rows else 0
                 ok = ok and tokens.dtype is i32 and tokens.is_contiguous() and tokens.get_device() == dev and tokens.shape[0] == rows and tokens.dim() == 2
@@ -147,8 +151,8 @@ class ScoreHandle:
                 p_ws = w_scale.data_ptr()
                 ok = ok and w_scale.dtype is _f32 and w_scale.is_contiguous() and w_scale.get_device() == dev and w_scale.numel() == V
             if ok:
-                st = self._score(self._h, h.data_ptr(), hs, p_hs, W.data_ptr(), p_ws, p_tok, n_tok, rows, n_top, inv_temperature, p_lp, p_lse, p_ent,
-                                 p_top, p_tlp, stream or None)
+                st = self._score(self._h, _SCORE_ARGS.pack(h.data_ptr(), hs, p_hs, W.data_ptr(), p_ws, p_tok, n_tok, rows, n_top, inv_temperature, p_lp, p_lse,
+                                                           p_ent, p_top, p_tlp, stream or 0))
         if check and st != AJ_OK:
             raise AjError(st, "aj_score_tokens")
         return st

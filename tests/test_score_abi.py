@@ -60,6 +60,38 @@ def test_creation_checks_need_no_device(built):
         assert status(*ok) == aj.AJ_ERR_CUDA
 
 
+def test_the_argument_structures_are_eight_bytes_a_field(tmp_path):
+    """What the binding packs is what the header declares."""
+    from paper_2504_20039_b200 import score
+
+    src = tmp_path / "t.c"
+    src.write_text('#include <stdio.h>\n#include "aj_score.h"\n'
+                   'int main(void) { printf("%d %d %d %d %d %d\\n", (int)sizeof(aj_norm_args), (int)offsetof(aj_norm_args, eps), (int)offsetof(aj_norm_args, cuda_stream),'
+                   ' (int)sizeof(aj_score_args), (int)offsetof(aj_score_args, inv_temperature), (int)offsetof(aj_score_args, cuda_stream)); return 0; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(tmp_path / "t")], check=True)
+    got = [int(x) for x in subprocess.run([str(tmp_path / "t")], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [score._NORM_ARGS.size, 48, 17 * 8, score._SCORE_ARGS.size, 72, 15 * 8]
+
+
+def test_the_argument_structures_are_checked(built):
+    from paper_2504_20039_b200 import score
+
+    import paper_2504_20039_b200 as aj
+
+    p = 1 << 20
+    ok = [0, p, 64, p, 64, p, 1e-5, 0, 64, 0, 1 << 22, 64, p, 64, p, 64, p, 0]
+    f = score._lib()["aj_add_norm_call"]
+    assert f(score._NORM_ARGS.pack(*ok)) == aj.AJ_OK  # no rows
+    for i, bad in ((0, -1), (0, 1 << 32), (2, 63), (6, -1.0), (7, -1), (8, 0), (8, 1 << 32), (9, 7), (9, 1 << 33)):
+        args = list(ok)
+        args[7] = 4
+        args[i] = bad
+        assert f(score._NORM_ARGS.pack(*args)) == aj.AJ_ERR_INVALID_ARG, (i, bad)
+    assert f(None) == aj.AJ_ERR_INVALID_ARG
+    g = score._lib()["aj_score_call"]
+    assert g(None, score._SCORE_ARGS.pack(*([p] * 6), 1, 4, 1, 1.0, *([p] * 5), 0)) == aj.AJ_ERR_INVALID_ARG and g(None, None) == aj.AJ_ERR_INVALID_ARG
+
+
 def test_norm_checks_need_no_device(built):
     from paper_2504_20039_b200 import score
 

@@ -1,4 +1,6 @@
 """ScoreHandle refuses tensors that do not fit, before anything reaches the library (a handle without a device, fake tensors)."""
+import struct
+
 import pytest
 import torch
 
@@ -56,9 +58,10 @@ def test_what_is_passed_on(handle):
     ok = dict(h=Fake(6, 64, dtype=B), W=Fake(1000, 64, dtype=B), tokens=Fake(6, 2, dtype=i32), logprob=Fake(6, 2), lse=Fake(6), entropy=Fake(6),
               top_id=Fake(6, 5, dtype=i32), top_logprob=Fake(6, 5))
     assert handle.score(**ok) == 0
-    a = handle.calls[-1]
-    assert a[2] == 64 and a[7:11] == (2, 6, 5, 1.0)
-    assert handle.score(**(ok | {"h": Fake(6, 64, dtype=B, stride=(80, 1))})) == 0 and handle.calls[-1][2] == 80
+    fields = lambda: struct.unpack("9qd6q", handle.calls[-1][1])  # noqa: E731
+    assert fields() == (1 << 20, 64, 0, 1 << 20, 0, 1 << 20, 2, 6, 5, 1.0, 1 << 20, 1 << 20, 1 << 20, 1 << 20, 1 << 20, 0)
+    assert handle.score(**(ok | {"h": Fake(6, 64, dtype=B, stride=(80, 1)), "lse": None, "stream": 77})) == 0
+    assert fields()[1] == 80 and fields()[11] == 0 and fields()[15] == 77
     n = len(handle.calls)
     bad = [{"h": Fake(6, 63, dtype=B)}, {"h": Fake(6, 64)}, {"h": Fake(6, 64, dtype=B, device=1)}, {"h": Fake(6, 64, dtype=B, stride=(64, 2))}, {"h": Fake(64, dtype=B)},
            {"W": Fake(999, 64, dtype=B)}, {"W": Fake(1000, 64, dtype=B, contiguous=False)}, {"W": Fake(1000, 64)}, {"tokens": Fake(6, 2, dtype=torch.int64)},
