@@ -3,12 +3,12 @@
 //   logits[m, v] = sum_k h[m, k] W[v, k]   one fixed order over k, f32
 //
 // Up to 8 rows: a warp per entry, its lanes along k (16 bytes at a time in f32), all rows at once; bound by the stream of W.
-// More rows: a CTA of 256 threads computes a tile of 64 rows x 128 entries, 8 x 4 outputs per thread, from k-slices of 16 in shared
+// More rows: a CTA of 256 threads computes a tile of 16, 32 or 64 rows x 128 entries, 2, 4 or 8 x 4 outputs per thread, from k-slices of 16 in shared
 // memory as f32; the next slice is fetched into registers meanwhile.  Bound by the multiply-adds and the reads of shared memory that
 // feed them.  A second kernel, a warp per row and tile, makes the tiles' sums; a head of few tiles leaves that to the last step.
 //
-// Measured, f32 (d = 4096): 5 rows, 128,256 entries 677 us, 3.1 TB/s; 264 rows, 32,000 entries 2365 us, 29 TFLOP/s; 17 rows, which fill a quarter of
-// a tile, 1832 us.
+// Measured, f32 (d = 4096): 5 rows, 128,256 entries 677 us, 3.1 TB/s; 264 rows, 32,000 entries 2313 us, 30 TFLOP/s; 17 rows in tiles of
+// 32 1117 us (in tiles of 64 1832).
 #include "aj_score.cuh"
 
 namespace aj {
@@ -63,12 +63,13 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(256) few_logit
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(256) logits_kernel(Args a) {
-    constexpr int TM = 64, TV = 128, BK = 16, RM = 8, RV = 4, PH = TM * BK / 256, PW = TV * BK / 256;
+// RM: rows per thread, 2, 4 or 8
+template <typename T, int RM> __global__ void __launch_bounds__(256) logits_kernel(Args a) {
+    constexpr int TM = 8 * RM, TV = 128, BK = 16, RV = 4, PH = TM * BK / 256, PW = TV * BK / 256;
     __shared__ __align__(16) float sh[2][BK][TM + 4], sw[2][BK][TV + 4];
     const T *h = (const T *)a.h, *W = (const T *)a.W;
     const int v0 = blockIdx.x * TV, m0 = blockIdx.y * TM;
-    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;         // entries 4 tx .., rows 8 ty ..
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;         // entries 4 tx .., rows RM ty ..
     const int lk = threadIdx.x & 15, lr = threadIdx.x >> 4;         // a thread fetches column lk of rows lr, lr + 16, ..
     float rh[PH], rw[PW];
     auto fetch = [&](int k0) {
@@ -92,9 +93,14 @@ template <typename T> __global__ void __launch_bounds__(256) logits_kernel(Args 
         if (k0 + BK < a.d) fetch(k0 + BK);
 #pragma unroll
         for (int k = 0; k < BK; k++) {
-            const float4 x0 = *reinterpret_cast<const float4 *>(&sh[b][k][ty * RM]), x1 = *reinterpret_cast<const float4 *>(&sh[b][k][ty * RM + 4]);
             const float4 w = *reinterpret_cast<const float4 *>(&sw[b][k][tx * RV]);
-            const float x[RM] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w}, y[RV] = {w.x, w.y, w.z, w.w};
+            const float y[RV] = {w.x, w.y, w.z, w.w};
+            float x[RM];
+#pragma unroll
+            for (int i = 0; i < RM; i += 2) {
+                const float2 z = *reinterpret_cast<const float2 *>(&sh[b][k][ty * RM + i]);
+                x[i] = z.x, x[i + 1] = z.y;
+            }
 #pragma unroll
             for (int i = 0; i < RM; i++)
 #pragma unroll
@@ -138,7 +144,14 @@ template <typename T> void logits(const Args &a, cudaStream_t s) {
         }
         few_logits_kernel<T, false><<<grid, 256, 0, s>>>(a);
     } else {
-        logits_kernel<T><<<dim3((unsigned)((a.ld + 127) / 128), (a.rows + 63) / 64), 256, 0, s>>>(a);
+        // a tile of 64 rows costs the same however many of them there are
+        const unsigned gx = (unsigned)((a.ld + 127) / 128);
+        if (a.rows <= 16)
+            logits_kernel<T, 2><<<gx, 256, 0, s>>>(a);
+        else if (a.rows <= 32)
+            logits_kernel<T, 4><<<gx, 256, 0, s>>>(a);
+        else
+            logits_kernel<T, 8><<<dim3(gx, (a.rows + 63) / 64), 256, 0, s>>>(a);
     }
 }
 
