@@ -400,10 +400,11 @@ Plan plan_umma(int rows, int d, int V, int dtype, int tile, int num_sms, int max
     const int sub = (p.box_rows + (p.pair ? 128 : p.tile)) * 128;
     p.kps = p.num_kb % 2 == 0 && RING / (2 * sub) >= 3 ? 2 : 1;
     const int stage = sub * p.kps;
-    // the MMA reads 16 KB from a stage's rows on: past the end of the ring only where a stage is smaller, and then still within
-    // the block's shared memory
-    const int ring = stage >= 16384 ? RING : RING - 16384;
-    p.stages = ring / stage < MAX_STAGES ? ring / stage : MAX_STAGES;
+    // the MMA reads 128 rows (16 KB) from a k-block's rows on, of which box_rows are staged: past the k-block where it is smaller, so
+    // the last k-block of the last stage begins no later than 16 KB before the end of the block's shared memory
+    const int latest = (SMEM - 16384 - (p.kps - 1) * sub) / stage + 1;
+    p.stages = RING / stage < latest ? RING / stage : latest;
+    if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
     const int n = p.n_m * p.n_v;
     p.grid = p.pair ? 2 * (n < max_pairs ? n : max_pairs) : (n < num_sms ? n : num_sms);
     return p;

@@ -1,0 +1,52 @@
+"""How aj_score_tokens cuts its work (csrc/aj_score_umma.cu), compiled for the host: the ring of stages over every number of rows, tile, width
+and type, against the shared memory of a block."""
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PROGRAM = r"""
+#include <cstdio>
+#include "aj_score_umma.cu"
+using namespace aj::score;
+int main() {
+    const int block = 227 * 1024;  // shared memory of a block
+    long long seen = 0, past = 0, thin = 0;
+    for (int dtype : {(int)BF16, (int)E4M3})
+        for (int d : {16, 64, 128, 192, 256, 1792, 2048, 4096, 4160, 65536})
+            for (int tile = 32; tile <= 256; tile += 32)
+                for (int rows = 1; rows <= 300; rows++) {
+                    const Plan p = plan_umma(rows, d, 50257, dtype, tile, 148, 74);
+                    const int entries = p.pair ? p.tile / 2 : p.tile, sub = (p.box_rows + entries) * 128;  // bytes of a k-block
+                    seen++;
+                    thin += p.stages < 3;
+                    for (int s = 0; s < p.stages; s++)
+                        for (int j = 0; j < p.kps; j++) {
+                            const int at = (s * p.kps + j) * sub;
+                            // copies: box_rows, then the entries; products: 128 rows from the k-block's start, its entries
+                            const bool bad = at + sub > RING || at + 128 * 128 > block || SMEM > block;
+                            if (bad && past++ == 0) printf("dtype %d d %d tile %d rows %d: k-block %d of stage %d of %d at %d\n", dtype, d, tile, rows, j, s, p.stages, at);
+                        }
+                }
+    printf("%lld %lld %lld\n", seen, past, thin);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def output(tmp_path_factory):
+    d = tmp_path_factory.mktemp("plan")
+    (d / "plan.cu").write_text(PROGRAM)
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    subprocess.run([nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(ROOT, "paper_2504_20039_b200", "csrc"),
+                    "-o", str(d / "plan"), str(d / "plan.cu")], check=True)
+    return subprocess.run([str(d / "plan")], check=True, capture_output=True, text=True).stdout
+
+
+def test_nothing_past_the_blocks_shared_memory(output):
+    seen, past, thin = map(int, output.splitlines()[-1].split())
+    assert seen == 2 * 10 * 8 * 300
+    assert past == 0, output
+    assert thin == 0
