@@ -135,14 +135,17 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) add_norm_kernel(Args a)
 #pragma unroll
         for (int w = 0; w < WARPS; w++) top = max_nan(top, red[1][w]);
     }
-    if (at == 0) a.scale8[row] = top / 448.0f;
-    const float q = top == 0.0f ? 0.0f : 448.0f / top;
+    const float scale = top / 448.0f;
+    if (at == 0) a.scale8[row] = scale;
+    // f32 does not hold 448 / top below 448 / 2^128: there the row and its scale are lifted by 2^96 (no scale: zeros)
+    const float lift = top < 0x1p-119f ? 0x1p96f : 1.0f, lifted = scale * lift;
+    const float q = top >= 0x1p-119f ? 448.0f / top : lifted == 0.0f ? 0.0f : 1.0f / lifted;
 #pragma unroll
     for (int c = 0; c < C; c++) {
         const int i = (c * TPR + at) * 8, n = a.d - i;
         if (n <= 0) continue;
 #pragma unroll
-        for (int j = 0; j < 8; j++) s[c][j] *= q;
+        for (int j = 0; j < 8; j++) s[c][j] = s[c][j] * lift * q;
         store8_e4m3<WIDE>(a.out8 + row * a.out8_stride + i, n, s[c]);
     }
 }
