@@ -35,7 +35,7 @@ enum { AJ_SCORE_MAX_TOP = 32, AJ_SCORE_MAX_TOKENS = 1024 };
  *   residual, residual_out NULL: no addition, the sum is not wanted
  *   weight [d] f32; out8 [rows, d] bytes, scale8 [rows] f32: both or neither; at least one of out and out8
  * residual_out may be x or residual, out may be x or residual (with the same strides); other overlaps are not allowed.
- * A row of zeros gets scale 0 and zeros.  A scale below 2^-126 has fewer bits, and below 2^-150 it is 0, with zeros; out8 goes by the scale
+ * A row of zeros gets scale 0 and zeros, with eps = 0 too.  A scale below 2^-126 has fewer bits, and below 2^-150 it is 0, with zeros; out8 goes by the scale
  * as it is stored.  A row with a NaN, or whose square sum leaves f32's range, has no meaningful numbers;
  * its scale is then NaN if a y is.  rows may be 0.
  * d <= 32768.  Rows and weight on 16 bytes, 8-bit rows on 8 bytes, and d a multiple of 8 are fastest; all else goes element by element.

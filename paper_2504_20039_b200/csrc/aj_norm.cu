@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) add_norm_kernel(Args a)
 #pragma unroll
         for (int w = 0; w < WARPS; w++) sum += red[0][w];
     }
-    const float inv = rsqrtf(sum / (float)a.d + a.eps);
+    const float mean = sum / (float)a.d + a.eps, inv = mean == 0.0f ? 0.0f : rsqrtf(mean);  // (zeros under eps = 0 stay zeros)
     float top = 0.0f;
 #pragma unroll
     for (int c = 0; c < C; c++) {

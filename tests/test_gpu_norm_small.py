@@ -51,3 +51,24 @@ def test_small_weights_to_8_bits(w_size):
     out8, sc = torch.zeros(20, 512, device="cuda").to(torch.float8_e4m3fn), torch.full((20,), 9.0, device="cuda")
     aj.add_norm(x.cuda(), w.cuda(), 1e-5, out8=out8, scale8=sc)
     check8_against_its_scale(out8, sc, norm_reference(x, None, w, 1e-5)[1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [8, 300, 4096])
+def test_rows_of_zeros_under_any_eps(d, dtype):
+    """Zeros and scale 0, with eps = 0 too; the rows beside them keep their numbers."""
+    import paper_2504_20039_b200 as aj
+
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    x = torch.randn(5, d, generator=torch.Generator().manual_seed(d)).to(dt)
+    x[1], x[3] = 0.0, -0.0
+    w = torch.ones(d)
+    for eps in (0.0, 1e-30, 1e-5):
+        out, out8, sc = torch.full((5, d), 7.0, dtype=dt, device="cuda"), torch.ones(5, d, device="cuda").to(torch.float8_e4m3fn), torch.full((5,), 9.0, device="cuda")
+        aj.add_norm(x.cuda(), w.cuda(), eps, out=out, out8=out8, scale8=sc)
+        for i in (1, 3):
+            assert not out[i].any() and not out[i].isnan().any() and sc[i] == 0 and not out8[i].float().any() and not out8[i].float().isnan().any()
+        y = norm_reference(x[::2], None, w, eps)[1]
+        check8_against_its_scale(out8[::2], sc[::2], y)
+        # 64 roundings and the last one
+        assert ((out[::2].double().cpu() - y).abs() <= y.abs() * ((2.0**-8 if dtype == "bf16" else U) + 64 * U)).all()
