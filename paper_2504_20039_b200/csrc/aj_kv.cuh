@@ -25,6 +25,7 @@ struct View {
     // the sequences, as sequences whose new tokens are those of the whole batch and see all of the chunk.  The sequences themselves
     // then begin behind the shared slots.  Each leaves its unnormalised results, for aj_kv_join.cu.
     int shared = 0, lead = 0, chunk = 0, n_chunks = 0;
+    int behind = 0;  // slots before its new tokens of a sequence that shares: the whole tiles and what is shared of the next
     const int *lead_table = nullptr;
     int align = 0;  // places of the line that every piece takes and a CTA's share is a multiple of; 0: as many as it has
     int n_seq = 0, total = 0, pre_rows = 0;  // sequences; rows without q_start; rows that the results have room for
@@ -171,7 +172,7 @@ template <bool SHARED = false> __device__ inline Seq seq_of(const View &v, int b
     }
     if (SHARED) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
         const Rows r = rows_of(v);
-        if (s.L - s.nq >= v.shared && s.row0 >= r.base && s.nq <= r.n && s.row0 - r.base <= r.n - s.nq) s.first = v.shared;
+        if (s.L - s.nq >= v.behind && s.row0 >= r.base && s.nq <= r.n && s.row0 - r.base <= r.n - s.nq) s.first = v.shared;
     }
     return s;
 }

@@ -447,6 +447,7 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
     kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
     a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, 0, 0);
     a.v.shared = whole;
+    a.v.behind = shared;
     a.v.lead_table = shared_table;
     a.v.n_seq = B;
     a.v.total = B * n_q;
