@@ -20,6 +20,11 @@ inline int group_rows(int V) {
     const long long n = (2ll << 30) / (4ll * V) / 256 * 256;
     return n < 256 ? 256 : n < GROUP_ROWS ? (int)n : GROUP_ROWS;
 }
+// Rows of each group of a call, evenly, in whole row tiles.  (In 64 bits: a call may have 2^31 - 1 rows.)
+inline long long rows_each(long long rows, int group) {
+    const long long n = (rows + group - 1) / group, even = (rows + n - 1) / n, tiles = (even + 255) / 256 * 256;
+    return n == 1 ? even : tiles < group ? tiles : group;
+}
 
 // One group of rows on its way through a call.
 struct Args {

@@ -231,11 +231,8 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
     if (!guard.ok()) return AJ_ERR_CUDA;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
     const bool tensor = h->tensor && !off(hidden, 16) && !off(W, 16) && (rows == 1 || h_stride * e % 16 == 0) && !off(w_scale, 16);
-    // groups of rows, evenly, of whole row tiles
-    const int n_groups = (rows + h->group - 1) / h->group;
-    int each = (rows + n_groups - 1) / n_groups;
-    if (n_groups > 1) each = (each + 255) / 256 * 256 < h->group ? (each + 255) / 256 * 256 : h->group;
-    for (int r0 = 0; r0 < rows; r0 += each) {
+    const long long each = score::rows_each(rows, h->group);
+    for (long long r0 = 0; r0 < rows; r0 += each) {
         score::Args a;
         a.h = (const char *)hidden + (size_t)r0 * h_stride * e;
         a.W = W;
@@ -243,7 +240,7 @@ aj_status aj_score_tokens(aj_score h, const void *hidden, long long h_stride, co
         a.w_scale = w_scale;
         a.tokens = n_tok ? tokens + (size_t)r0 * n_tok : nullptr;
         a.h_stride = h_stride;
-        a.rows = rows - r0 < each ? rows - r0 : each;
+        a.rows = (int)(rows - r0 < each ? rows - r0 : each);
         a.d = h->d;
         a.V = h->V;
         a.n_tok = n_tok;

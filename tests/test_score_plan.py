@@ -8,10 +8,21 @@ import pytest
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 PROGRAM = r"""
+#include <climits>
 #include <cstdio>
 #include "aj_score_umma.cu"
 using namespace aj::score;
 int main() {
+    int torn = 0;  // calls whose groups do not cover the rows, in order, in as few groups as there can be
+    for (int group : {1, 17, 255, 256, 1024, 2560})
+        for (int rows : {1, 2, 255, 256, 257, 2560, 2561, 5200, 100000, INT_MAX - 900000, INT_MAX - 3000, INT_MAX - 1, INT_MAX}) {
+            if (group < 256 && rows > group) continue;  // (a handle for so few rows)
+            const long long each = rows_each(rows, group);
+            long long n = 0, r0 = 0;
+            for (; r0 < rows; r0 += each) n++;
+            torn += each < 1 || each > group || n > ((long long)rows + group - 1) / group || (n > 1 && each % 256 != 0);
+        }
+    printf("%d\n", torn);
     const int block = 227 * 1024;  // shared memory of a block
     long long seen = 0, past = 0, thin = 0;
     for (int dtype : {(int)BF16, (int)E4M3})
@@ -43,6 +54,10 @@ def output(tmp_path_factory):
     subprocess.run([nvcc, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(ROOT, "paper_2504_20039_b200", "csrc"),
                     "-o", str(d / "plan"), str(d / "plan.cu")], check=True)
     return subprocess.run([str(d / "plan")], check=True, capture_output=True, text=True).stdout
+
+
+def test_groups_of_rows(output):
+    assert output.splitlines()[0] == "0"
 
 
 def test_nothing_past_the_blocks_shared_memory(output):
