@@ -37,12 +37,13 @@ template <typename P> __device__ __forceinline__ int count_if(const unsigned lon
     return n;
 }
 
-// By all threads: take(key, place) for the n largest of `count` different keys (n <= count), with their places among them.  More
-// than 64 are first cut to those from the n-th largest value on (values alone, so that of equal ones all stay), found by
-// halving the range that it can lie in, with each thread's values in registers; that ends as soon as n values lie above the middle.  Each
-// key that is left then counts the ones before it.  `left` has room for all of them.
+// By all threads: take(key, place) for the n largest of `count` different keys (n <= count) of numbers below `limit`, with their places among
+// them.  More than 64 are first cut to those from the n-th largest value on, found by
+// halving the range that it can lie in, with each thread's values in registers; that ends as soon as n values lie above the middle.
+// Where that leaves more than 64 (equal values: a row of zeros of a padded batch, of NaN), the lowest numbers among the equal ones
+// are found in the same way.  Each key that is left then counts the ones before it.  `left` has room for all of them; keys are overwritten.
 template <typename F>
-__device__ __forceinline__ void top_of(const unsigned long long *keys, int count, int n, unsigned long long *left, int *n_left, F take) {
+__device__ __forceinline__ void top_of(unsigned long long *keys, int count, int n, int limit, unsigned long long *left, int *n_left, F take) {
     constexpr int KEEP = 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (count > 64) {
@@ -86,8 +87,35 @@ __device__ __forceinline__ void top_of(const unsigned long long *keys, int count
             if ((uint32_t)(k >> 32) >= lo) left[atomicAdd(n_left, 1)] = k;
         }
         __syncthreads();
-        keys = left;
         count = *n_left;
+        if (count > 64) {  // (ranking them all by counting took 1 ms a row with 20 alternatives)
+            __shared__ int n_kept;
+            if (threadIdx.x == 0) n_kept = 0;
+            uint32_t from = ~(uint32_t)(limit - 1), to = ~0u;
+            for (int it = 0; from < to; it ^= 1) {
+                const uint32_t mid = from + (to - from) / 2 + 1;
+                const unsigned long long least = (unsigned long long)lo << 32 | mid;
+                int c = 0;
+                for (int i = threadIdx.x; i < count; i += THREADS) c += left[i] >= least;
+                c = __reduce_add_sync(~0u, c);
+                if (lane == 0) sums[it][warp] = c;
+                __syncthreads();
+                c = 0;
+#pragma unroll
+                for (int w = 0; w < WARPS; w++) c += sums[it][w];
+                if (c >= n)
+                    from = mid;
+                else
+                    to = mid - 1;
+                if (c == n) break;
+            }
+            for (int i = threadIdx.x; i < count; i += THREADS)
+                if (left[i] >= ((unsigned long long)lo << 32 | from)) keys[atomicAdd(&n_kept, 1)] = left[i];
+            __syncthreads();
+            count = n_kept;
+        } else {
+            keys = left;
+        }
     }
     for (int i = threadIdx.x; i < count; i += THREADS) {
         const unsigned long long k = keys[i];
@@ -170,9 +198,9 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
             if (ordered_image(x) >= reached) found[atomicAdd(n_left, 1)] = key_of(x, t);
         }
         __syncthreads();
-        top_of(found, n_left[0], n_tiles, left, n_left + 1, choose);
+        top_of(found, n_left[0], n_tiles, a.n_v, left, n_left + 1, choose);
     } else if (n_tiles) {
-        top_of(found, a.n_v, n_tiles, left, n_left + 1, choose);
+        top_of(found, a.n_v, n_tiles, a.n_v, left, n_left + 1, choose);
     }
     float S = 0.0f, T = 0.0f;
     auto add = [&](const float4 &q) {
@@ -225,7 +253,7 @@ __global__ void __launch_bounds__(THREADS) finish_kernel(Args a) {
         for (int j = threadIdx.x; j < a.n_top; j += THREADS) put(j, j, nan);
         return;
     }
-    top_of(found, n_found, a.n_top, left, n_left + 2, [&](unsigned long long k, int place) { put(place, (int)~(uint32_t)k, logprob(key_value(k))); });
+    top_of(found, n_found, a.n_top, a.V, left, n_left + 2, [&](unsigned long long k, int place) { put(place, (int)~(uint32_t)k, logprob(key_value(k))); });
 }
 
 }  // namespace
