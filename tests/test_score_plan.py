@@ -23,6 +23,19 @@ int main() {
             torn += each < 1 || each > group || n > ((long long)rows + group - 1) / group || (n > 1 && each % 256 != 0);
         }
     printf("%d\n", torn);
+    for (int V : {3000, 8000, 12000, 16000, 32000, 50257, 100352, 128256, 151936, 200064, 256000}) printf("%d ", one_sm_tile(V, 148));
+    // a tile of up to 96 entries costs as much as one of 96, a wider one in proportion
+    int dear = 0, many = 0;
+    for (int V = 1; V <= MAX_V; V += V < 400000 ? 1 : 997) {
+        auto cost = [&](int t) { return ((V + t - 1) / t + 147) / 148 * (t > 96 ? t : 96); };
+        int least = cost(256);
+        for (int t = 32; t < 256; t += 32)
+            if ((V + t - 1) / t <= MAX_TILES && cost(t) < least) least = cost(t);
+        const int t = one_sm_tile(V, 148);
+        dear += cost(t) > 1.15 * least;
+        many += t % 32 != 0 || t > 256 || (V + t - 1) / t > MAX_TILES;
+    }
+    printf("%d %d\n", dear, many);
     const int block = 227 * 1024;  // shared memory of a block
     long long seen = 0, past = 0, thin = 0;
     for (int dtype : {(int)BF16, (int)E4M3})
@@ -58,6 +71,14 @@ def output(tmp_path_factory):
 
 def test_groups_of_rows(output):
     assert output.splitlines()[0] == "0"
+
+
+def test_widths_of_tiles(output):
+    """Widths that measured within 6 % of the best one of their head (1 to 128 rows, d from 256 to 8192, both types), on 148 SMs."""
+    *tiles, dear, many = map(int, output.splitlines()[1].split())
+    good = [(32,), (64, 96), (96, 128), (128, 160), (128, 224), (192,), (160, 192, 256), (224,), (160, 224), (224, 256), (160, 224, 256)]
+    assert all(t in g for t, g in zip(tiles, good, strict=True)), tiles
+    assert dear == many == 0
 
 
 def test_nothing_past_the_blocks_shared_memory(output):
