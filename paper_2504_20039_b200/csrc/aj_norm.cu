@@ -160,11 +160,10 @@ template <typename T, bool WIDE> cudaError_t pick(const Args &a, cudaStream_t s)
     if (a.d <= 256) return go<T, WIDE, 32, 1>(a, s);
     if (a.d <= 1024) return go<T, WIDE, 32, 4>(a, s);
     if (a.d <= 2048) return go<T, WIDE, 128, 2>(a, s);
-    // more pieces per thread where the rows fill the SMs (16000 rows of 8192 to 8 bits: 155 us and 160), more threads where one row's
-    // latency counts (one row of 4096: 2.4 us and 2.9)
-    const bool many = a.rows > 600;
-    if (a.d <= 4096) return many ? go<T, WIDE, 128, 4>(a, s) : go<T, WIDE, 256, 2>(a, s);
-    if (a.d <= 8192) return many ? go<T, WIDE, 256, 4>(a, s) : go<T, WIDE, 512, 2>(a, s);
+    if constexpr (sizeof(T) == 2)  // (f32 never asks for these)
+        if (a.d <= 8192 && fewer_threads(a.rows, a.d, true)) return a.d <= 4096 ? go<T, WIDE, 128, 4>(a, s) : go<T, WIDE, 256, 4>(a, s);
+    if (a.d <= 4096) return go<T, WIDE, 256, 2>(a, s);
+    if (a.d <= 8192) return go<T, WIDE, 512, 2>(a, s);
     if (a.d <= 16384) return go<T, WIDE, 512, 4>(a, s);
     return go<T, WIDE, 1024, 4>(a, s);
 }
