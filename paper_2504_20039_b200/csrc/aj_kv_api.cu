@@ -178,16 +178,20 @@ int cut_shared(kv::View &v, int num_sms) {
     return (int)(items * v.n_chunks < most ? items * v.n_chunks : most);
 }
 // Is it worth the parts and their join?  Sequences that share pages read them from L2 when they are attended one by one, so what is
-// saved is the stream from L2 (few rows: at 5.9 TB/s, against 12 us and 2 for each tile of a chunk), or row tiles that a window
-// does not fill (more rows).  Measured, us, together and one by one: 64 tokens behind 2048 slots 37 and 88, behind 512 34 and 39, behind
-// 256 34 and 31; 16 behind 4096 29 and 46, behind 1024 22 and 21; 2 behind 32768 82 and 49; 32 windows of 9 rows behind 2048
-// 52 and 88, 16 of 33 behind 8192 115 and 164, 32 of 33 behind 1504 86 and 75.
+// saved is the stream from L2 (few rows: at 5.9 TB/s, against 8 us and 1.5 for each tile of a chunk, at a head size of 128), or row tiles
+// that a window does not fill (more rows: 10 ns a tile, against 4 us and 0.8 ns for each row and head, whose parts go through L2; half of
+// that at 64).  Measured, us, together and one by one, 32 query and 8 key heads of 128: 64 tokens behind 2048 slots 32 and 80, behind 512 29 and 35,
+// behind 256 26 and 27; 16 behind 4096 24 and 43, behind 1024 19 and 21; 2 behind 32768 61 and 48; 32 windows of 9 rows behind 2048 52 and
+// 70, 16 of 33 behind 8192 108 and 134, 32 of 33 behind 1504 86 and 74; heads of 64: 16 tokens behind 4096 22 and 34, 32 windows of 33
+// behind 1504 72 and 66; 64 query heads: 32 of 33 behind 1504 147 and 118, 16 behind 8192 188 and 219.  Over 1584 calls of twelve
+// head counts, both sizes, 1 to 384 rows, 700 of them not looked at before: within 1 % of the better way on average, more than 8 % above it in 55.
 bool worth_sharing(const kv::View &v) {
-    if (v.n_q * v.G <= kv::FEW_ROWS) return (double)v.n_seq * v.shared * v.Hkv * v.D * 4 / 5.9e6 > 12 + v.chunk / 64;
+    const double size = v.D / 128.0;
+    if (v.n_q * v.G <= kv::FEW_ROWS) return (double)v.n_seq * v.shared * v.Hkv * v.D * 4 / 5.9e6 > 8 + 1.5 * (v.chunk / 128) * size;
     const long long per_piece = 2 * (128 / v.G), together = (v.pre_rows + per_piece - 1) / per_piece;
     // (of a ragged batch the host knows the sum at most: half a piece more for each sequence)
     const long long one_by_one = v.q_start ? together + v.n_seq / 2 : v.n_seq * ((v.n_q + per_piece - 1) / per_piece);
-    return (one_by_one - together) * v.Hkv * (v.shared / 128) > 2300;
+    return 0.010 * (double)((one_by_one - together) * v.Hkv * (v.shared / 128)) > 4 + 0.0008 * (double)v.pre_rows * v.Hq * size;
 }
 // Rows x chunks that a workspace for max_rows rows must hold.
 int pre_capacity(aj_kv h, int max_rows) {
