@@ -100,16 +100,17 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
  * which the sums are added:
  *   m = max(m1, m2),  out = (e^(m1 - m) O1 + e^(m2 - m) O2) / (e^(m1 - m) l1 + e^(m2 - m) l2)
  * with O, l, m the weighted values, their sum and the maximum over the shared slots (1) and over a sequence's others (2), f32.
+ * As in aj_kv_attend the weights are rounded to bf16 before they meet the values.
  *   shared        slots 0 .. shared - 1 of the sequences hold the same tokens (whole tiles of 128 of them are used together)
  *   shared_table  [shared / page_size, rounded up] int32: their pages
  * A sequence with at least `shared` slots before its new tokens is taken to share them.  Any other (a shorter one, one
  * of a padded batch) is attended by its own table alone; block_table names every page of a sequence, the shared ones too.
- * aj_kv_reserve_shared(h, max_rows) sets aside a workspace for max_rows new tokens of a call (2 * (D + 2) * Hq * 4 bytes each) unless
- * the handle has as much; a larger one takes the place of a smaller, and 0 frees it.  It allocates and may wait for the device: call it
+ * aj_kv_reserve_shared(h, max_rows) sets aside a workspace for max_rows new tokens of a call (2 * (D + 2) * Hq * 4 bytes each, and 20 to 60 MB
+ * however few they are) unless the handle has as much; a larger one takes the place of a smaller, and 0 frees it.  It allocates and may wait for the device: call it
  * outside of captures, and before capturing calls that use the workspace.  Sequences of a ragged call whose tokens lie past max_rows are attended alone.
  * f32, head sizes other than 64 and 128, Hq / Hkv > 128, pages off 128 bytes, one sequence, or less than 128 shared
  * slots: aj_kv_attend's kernels do the whole call, nothing is shared and nothing need be reserved.
- * Errors: as aj_kv_attend; AJ_ERR_WORKSPACE also for B * n_q rows above max_rows.
+ * Errors: as aj_kv_attend; AJ_ERR_WORKSPACE also for B * n_q rows above max_rows, whether or not sharing would pay.
  */
 aj_status aj_kv_reserve_shared(aj_kv h, int max_rows);
 aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const void *k_pages, const void *v_pages, int n_pages,

@@ -1,5 +1,5 @@
 // Host side of the key-value cache operators: argument checks, the handle's workspace, choice of kernel, launches.
-// No call synchronises or allocates but aj_kv_create, aj_kv_destroy and aj_kv_last_status.
+// No call synchronises or allocates but aj_kv_create, aj_kv_destroy, aj_kv_reserve_shared and aj_kv_last_status.
 #include "../../include/aj_kv.h"
 
 #include <new>
@@ -162,7 +162,7 @@ bool attend_maps(aj_kv h, const kv::AttendArgs &a, CUtensorMap (&maps)[4], int *
 
 // Into how many chunks the shared slots are cut.  An item is a chunk, a key head and a piece of up to 256 query rows.  With few
 // rows per sequence, chunks of six tiles on up to half of the SMs, while the sequences' own slots are attended on the others (64 tokens
-// behind 2048 slots: 37 us, with every SM for one and then the other 62); else as many items as there are SMs, so that hardly
+// behind 2048 slots: 32 to 38 us, with every SM for one and then the other 62); else as many items as there are SMs, so that hardly
 // one spans CTAs, which costs a join by one CTA.  Returns the CTAs for it.
 int cut_shared(kv::View &v, int num_sms) {
     const int tiles = v.shared / 128, per_piece = 2 * (128 / v.G);

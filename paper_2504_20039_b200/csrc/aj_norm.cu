@@ -2,8 +2,8 @@
 //
 // A row lives in registers from its loads to its stores, so everything is read and written once: the sum of squares and,
 // for 8 bits, the largest |y| are the only values that cross threads.  Short rows take a warp each, longer ones a CTA.
-// Bound by HBM, or by latency when there are few rows.  Measured: one row of 4096 2.4 us; 2112 rows of 4096 in both forms 15.2 us,
-// 5.1 TB/s; 16000 rows of 8192 to 8 bits 140 us, 6.5 TB/s.
+// Bound by HBM, or by latency when there are few rows.  Measured: one row of 4096 2.4 us (2.8 to 8 bits
+// too); 2112 rows of 4096 in both forms 15.9 us, 4.9 TB/s, 1.8 waves of eight CTAs per SM; 16000 rows of 8192 to 8 bits 141 us, 6.5 TB/s.
 #include "aj_norm.cuh"
 
 #include <cuda_bf16.h>

@@ -11,7 +11,8 @@
 // alternative.)  Keys are 64 bits (value, then the complement of the index), so no two are equal and the order of collecting them does not matter.
 //
 // Bound by latency: a CTA per row, some 8 KB of sums and n tiles per row.  17 rows with 8 alternatives take 4 us after the tiles are
-// there (loads 0.7, the tiles 1, their logits 1.1), without alternatives 2; 2112 rows 28, bound by instructions.
+// there (loads 0.7, the tiles 1, their logits 1.1), without alternatives 2; 2112 rows 21, bound by instructions.  Rows of equal logits
+// (zeros) take some 10 to 50 us more each wave of CTAs: more keys to halve.
 #include "aj_score.cuh"
 
 namespace aj {

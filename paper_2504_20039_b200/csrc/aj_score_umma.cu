@@ -16,9 +16,10 @@
 // bf16 and e4m3 differ in the instruction and in the scales that the epilogue puts on the sums (times h_scale, times w_scale).
 // Every logit is one sum over k in a fixed order.  Every wait is bounded (aj_ptx.cuh).
 //
-// Measured (d = 4096, 128,256 entries): 17 rows 162 us for 1.05 GB, 6.5 TB/s; in 8 bits 86 us, 6.1 TB/s; 2112 rows 1400 us alone, 1.58
-// PFLOP/s, and 1490 back to back, where the power limit lowers the clock (on zeros 1185); 2048 rows in 8 bits 750 us. 129 to 256 rows are bound
-// by W too (200 rows 204 us); 264 rows take as long as 512 (344 us), for whole row tiles are multiplied.
+// Measured (d = 4096, 128,256 entries, the whole call from a graph): 17 rows 165 to 170 us for 1.05 GB, 6.2 to 6.4 TB/s; in 8 bits 89 to 92 us,
+// 5.7 to 5.9 TB/s; 2112 rows 1410 us alone, 1.57 PFLOP/s, and 1490 to 1550 back to back, where the power limit lowers the clock (on zeros 1182); 2048
+// rows in 8 bits 783 us. 129 to 256 rows are bound by W too (200 rows 213 us, in 8 bits 122); 264 rows take nine tenths of what 512 take (350 to
+// 370 and 404 us; in 8 bits 206 and 229), for whole row tiles are multiplied.
 #include "aj_score.cuh"
 #include "aj_ptx.cuh"
 
