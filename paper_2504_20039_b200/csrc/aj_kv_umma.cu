@@ -69,10 +69,10 @@ template <int D> struct Cfg {
 template <bool SHARED> __device__ inline long long build_line(const View &v, int tpt, long long *pre) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (v.n_q <= 16 * tpt) {  // few pieces: a thread per sequence; else a warp
-        for (int b = threadIdx.x; b < v.B; b += blockDim.x) pre[b + 1] = units_of(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, 0, 1) * v.Hkv;
+        for (int b = threadIdx.x; b < v.B; b += blockDim.x) pre[b + 1] = units_of<SHARED>(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, 0, 1) * v.Hkv;
     } else {
         for (int b = warp; b < v.B; b += blockDim.x >> 5) {
-            long long u = units_of(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, lane, 32);
+            long long u = units_of<SHARED>(v, pieces_of(seq_of<SHARED>(v, b), tpt), tpt, lane, 32);
 #pragma unroll
             for (int o = 16; o; o >>= 1) u += __shfl_xor_sync(~0u, u, o);
             if (lane == 0) pre[b + 1] = u * v.Hkv;
@@ -113,7 +113,7 @@ template <bool SHARED> __device__ inline Line seek(const View &v, int tpt, const
     c.h = (int)(r / per_head);
     r -= c.h * per_head;
     for (int q0 = 0;; q0 += 32) {
-        const int n = q0 + lane < c.q.n ? CHARGE + piece_of(v, c.q, q0 + lane, tpt).places : 0;
+        const int n = q0 + lane < c.q.n ? CHARGE + piece_of<SHARED>(v, c.q, q0 + lane, tpt).places : 0;
         int x = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -129,7 +129,7 @@ template <bool SHARED> __device__ inline Line seek(const View &v, int tpt, const
         }
         r -= all;
     }
-    c.p = piece_of(v, c.q, c.qt, tpt);
+    c.p = piece_of<SHARED>(v, c.q, c.qt, tpt);
     return c;
 }
 
@@ -146,7 +146,7 @@ template <bool SHARED> __device__ inline void next_item(const View &v, int tpt, 
             } while (c.q.n == 0);
         }
     }
-    c.p = piece_of(v, c.q, c.qt, tpt);
+    c.p = piece_of<SHARED>(v, c.q, c.qt, tpt);
 }
 
 // Order of the K and V tiles of a segment of n tiles in the ring: K0 K1 V0 K2 V1 ... V(n-1).
@@ -295,7 +295,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             uint32_t g = 0;
             bool ok = true;
             for (int u = 0; ok && u < u1; next_item<SHARED>(v, tpt, c)) {
-                const Part pt = part_of(c, u1 - u);
+                const Part pt = part_of<SHARED>(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
                 for (int i = 0; ok && i < 2 * n; i++) {
@@ -353,7 +353,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // depends on them.  The next item's come in while the softmax and the last product of this one run.
             uint32_t n_q[2] = {0, 0};  // items whose queries have been asked for
             for (int u = 0; u < u1; next_item<SHARED>(v, tpt, c)) {
-                const Part pt = part_of(c, u1 - u);
+                const Part pt = part_of<SHARED>(c, u1 - u);
                 u += pt.line;
                 for (int x = 0; x < 2 && pt.n > 0; x++) {
                     if (!has_tile(c.p, x, pt.n)) continue;
@@ -420,7 +420,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             // Both warps walk over every tile and both release it: a warp that skipped the other stream's tiles could wait
             // for a stage's next phase while the previous one is still loading, and a parity wait would let it through.
             for (int u = 0; ok && u < u1; next_item<SHARED>(v, tpt, c)) {
-                const Part pt = part_of(c, u1 - u);
+                const Part pt = part_of<SHARED>(c, u1 - u);
                 const int n = pt.n;
                 u += pt.line;
                 const bool shared_rows = c.p.tok0 == c.p.n_tok;
@@ -534,7 +534,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
             const bool wide_out = ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.out_stride * 2)) & 31) == 0;  // rows on 32 bytes
             auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
             for (int u = 0; u < u1; next_item<SHARED>(v, tpt, c)) {
-                const Part pt = part_of(c, u1 - u);
+                const Part pt = part_of<SHARED>(c, u1 - u);
                 const int n = pt.n, unit = c.unit;
                 u += pt.line;
                 if (n == 0) continue;
@@ -542,7 +542,7 @@ attend_umma_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const int tok = shared_rows || x == 0 ? c.p.tok0 : c.p.n_tok - c.p.tok0;
                 const int ta = c.p.ta + (shared_rows || x == 0 ? 0 : c.p.tok0);
                 const int n_rows = tok * v.G;
-                const int p_first = c.q.s.L - c.q.s.nq + c.q.s.ahead + ta;  // slot of the stream's first token
+                const int p_first = c.q.s.L - c.q.s.nq + (SHARED ? c.q.s.ahead : 0) + ta;  // slot of the stream's first token
                 const int my_p = p_first + token(min(row, n_rows - 1)), p_last = p_first + tok - 1;
                 float m = -INFINITY, l = 0.0f;
                 const int step = shared_rows ? 2 : 1;
