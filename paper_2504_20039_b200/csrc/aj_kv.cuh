@@ -16,11 +16,16 @@ constexpr float RAISE = 30.0f;
 constexpr int MAX_CHUNKS = 16;  // of the slots that a batch shares
 
 // What a call says about the cache and its new tokens (device pointers).
-struct View {
+struct CacheView {
     const int *table = nullptr, *lens = nullptr, *q_start = nullptr;
     int B = 0, n_q = 0, width = 0, n_pages = 0, cap = 0;
     int Hq = 0, Hkv = 0, G = 0, D = 0, page = 0, page_shift = 0;
     int window = 0, sinks = 0;
+};
+
+// The same of a call whose sequences may share slots.  (Among every kernel's parameters these fields cost a single token's append 0.3 us of
+// the host's time.)
+struct View : CacheView {
     // A batch that shares its first slots (whole tiles of 128): the shared slots are cut into chunks, and `lead` chunks come before
     // the sequences, as sequences whose new tokens are those of the whole batch and see all of the chunk.  The sequences themselves
     // then begin behind the shared slots.  Each leaves its unnormalised results, for aj_kv_join.cu.
@@ -55,7 +60,7 @@ struct AttendArgs {
 };
 
 struct WeighArgs {
-    View v;
+    CacheView v;
     const void *q = nullptr, *k = nullptr;
     const float *lse = nullptr, *weight = nullptr;
     float *weight_out = nullptr;
@@ -66,7 +71,7 @@ struct WeighArgs {
 };
 
 struct AppendArgs {
-    View v;
+    CacheView v;
     const void *q = nullptr, *k = nullptr, *vv = nullptr;
     long long q_stride = 0, k_stride = 0, v_stride = 0, q_out_stride = 0;
     const float *q_norm = nullptr, *k_norm = nullptr, *cos_sin = nullptr;
@@ -79,7 +84,7 @@ struct AppendArgs {
 };
 
 struct EvictArgs {
-    View v;
+    CacheView v;
     void *k_pages = nullptr, *v_pages = nullptr;
     int keep = 0, sinks = 0, recent = 0, elem = 0;
     const float *weight = nullptr;
@@ -151,17 +156,19 @@ __device__ inline float2 *pre_ml(const AttendArgs &a, int chunk, int h, int rowg
 }
 
 // SHARED: of a shared call, with its chunks.  (Asked of every call, this cost 1 to 18 % of others' time.)
-template <bool SHARED = false> __device__ inline Seq seq_of(const View &v, int b) {
+template <bool SHARED = false, typename V> __device__ inline Seq seq_of(const V &v, int b) {
     Seq s;
-    if (SHARED && b < v.lead) {
-        const Rows r = rows_of(v);
-        s.row0 = r.base;
-        s.nq = s.ahead = r.n;
-        s.first = b * v.chunk;
-        s.L = min(v.shared, s.first + v.chunk);
-        return s;
+    if constexpr (SHARED) {
+        if (b < v.lead) {
+            const Rows r = rows_of(v);
+            s.row0 = r.base;
+            s.nq = s.ahead = r.n;
+            s.first = b * v.chunk;
+            s.L = min(v.shared, s.first + v.chunk);
+            return s;
+        }
+        b -= v.lead;
     }
-    if (SHARED) b -= v.lead;
     s.L = min(max(__ldg(v.lens + b), 0), v.cap);
     if (v.q_start) {
         s.row0 = __ldg(v.q_start + b);
@@ -170,7 +177,7 @@ template <bool SHARED = false> __device__ inline Seq seq_of(const View &v, int b
         s.row0 = b * v.n_q;
         s.nq = v.n_q;
     }
-    if (SHARED) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
+    if constexpr (SHARED) {  // a sequence that does not have all of the prefix before its new tokens, or no room for them, is on its own
         const Rows r = rows_of(v);
         if (s.L - s.nq >= v.behind && s.row0 >= r.base && s.nq <= r.n && s.row0 - r.base <= r.n - s.nq) s.first = v.shared;
     }
@@ -178,19 +185,23 @@ template <bool SHARED = false> __device__ inline Seq seq_of(const View &v, int b
 }
 
 // Number of the page that holds a slot; a number outside the pool reads page 0.
-template <bool SHARED = false> __device__ inline int page_of(const View &v, int b, int slot) {
-    const int *row = SHARED && b < v.lead ? v.lead_table : v.table + (size_t)(SHARED ? b - v.lead : b) * v.width;
+template <bool SHARED = false, typename V> __device__ inline int page_of(const V &v, int b, int slot) {
+    const int *row;
+    if constexpr (SHARED)
+        row = b < v.lead ? v.lead_table : v.table + (size_t)(b - v.lead) * v.width;
+    else
+        row = v.table + (size_t)b * v.width;
     const int p = __ldg(row + (slot >> v.page_shift));
     return (unsigned)p < (unsigned)v.n_pages ? p : 0;
 }
 
 // Row of the pages, as [n_pages * Hkv * page_size, D], that holds a slot of a key head.
-__device__ inline size_t page_row(const View &v, int b, int h, int slot) {
+__device__ inline size_t page_row(const CacheView &v, int b, int h, int slot) {
     return ((size_t)page_of(v, b, slot) * v.Hkv + h) * v.page + (slot & (v.page - 1));
 }
 
 // Does the token in slot p see slot j?
-__device__ inline bool sees(const View &v, int p, int j) {
+__device__ inline bool sees(const CacheView &v, int p, int j) {
     return j <= p && (v.window == 0 || j > p - v.window || j < v.sinks);
 }
 

@@ -79,9 +79,9 @@ aj_status check_rows(aj_kv h, const void *p, long long stride, int heads) {
     return AJ_OK;
 }
 
-kv::View view_of(aj_kv h, int n_pages, const int32_t *table, int width, const int32_t *lens, const int32_t *q_start, int B,
+kv::CacheView view_of(aj_kv h, int n_pages, const int32_t *table, int width, const int32_t *lens, const int32_t *q_start, int B,
                  int n_q, int window, int sinks) {
-    kv::View v;
+    kv::CacheView v;
     v.table = table;
     v.lens = lens;
     v.q_start = q_start;
@@ -377,7 +377,7 @@ aj_status aj_kv_attend(aj_kv h, const void *q, long long q_stride, const void *k
     Guard guard(h->device);
     if (!guard.ok()) return AJ_ERR_CUDA;
     kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
-    a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, window, sinks);
+    static_cast<kv::CacheView &>(a.v) = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, window, sinks);
     h->last_launches = 1;
     if (h->tensor && n_q * a.v.G <= kv::FEW_ROWS) {
         h->last_path = "few";
@@ -449,7 +449,7 @@ aj_status aj_kv_attend_shared(aj_kv h, const void *q, long long q_stride, const 
     Guard guard(h->device);
     if (!guard.ok()) return AJ_ERR_CUDA;
     kv::AttendArgs a = attend_args(h, q, q_stride, k_pages, v_pages, scale, out, out_stride, lse);
-    a.v = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, 0, 0);
+    static_cast<kv::CacheView &>(a.v) = view_of(h, n_pages, block_table, table_width, seq_lens, q_start, B, n_q, 0, 0);
     a.v.shared = whole;
     a.v.behind = shared;
     a.v.lead_table = shared_table;

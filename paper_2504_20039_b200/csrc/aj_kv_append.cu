@@ -83,7 +83,7 @@ constexpr int UNROLL = 8, FAST_WARPS = 4;  // 2 and 4 heads at a time: 185 and 1
 template <typename T, int D, bool PAIRS>
 __global__ void __launch_bounds__(32 * FAST_WARPS) append_vec_kernel(AppendArgs a, int chunks) {
     constexpr int E = 16 / (int)sizeof(T), LV = D / E, VW = 32 / LV;
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LV, i0 = (lane % LV) * E;
     const long long at = (long long)blockIdx.x * FAST_WARPS + warp;
     const int b = blockIdx.y, t = (int)(at / chunks), first = (int)(at - (long long)t * chunks) * (UNROLL * VW) + sub;

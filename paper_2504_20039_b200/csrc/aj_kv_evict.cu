@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(THREADS, AHEAD == 4 ? 1024 / THREADS : 1) evic
     constexpr int NWARP = THREADS / 32;
     extern __shared__ __align__(16) unsigned dyn[];
     __shared__ Shared sh;
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int part = blockIdx.x % n_split, item = blockIdx.x / n_split;
     const int h = item % v.Hkv, b = item / v.Hkv;

@@ -70,7 +70,7 @@ template <typename T, int NE, bool VEC, int R>
 __global__ void __launch_bounds__(32 * WARPS) attend_simt_kernel(AttendArgs a, int n_rb, int splits) {
     constexpr int KS = 32 / R;  // keys a warp takes at a time
     extern __shared__ float sm[];
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int D = v.D, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int item = blockIdx.x, split = blockIdx.y;
     const int rb = item % n_rb, h = (item / n_rb) % v.Hkv, b = item / (n_rb * v.Hkv);
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(32 * WARPS) attend_simt_kernel(AttendArgs a, i
 template <typename T, int NE, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS) weigh_simt_kernel(WeighArgs a) {
     constexpr int R = 8, KS = 4;
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int D = v.D, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int h = blockIdx.y % v.Hkv, b = blockIdx.y / v.Hkv;
     const Seq s = seq_of(v, b);

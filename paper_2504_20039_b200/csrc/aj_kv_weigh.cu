@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) weigh_kernel(WeighArgs a, int g
     extern __shared__ __align__(128) unsigned char smem[];
     long long *pre = reinterpret_cast<long long *>(smem + STAGES * C::STAGE);  // [B + 1]
     __shared__ long long wsum[WARPS];
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, q4 = lane & 3, r8 = lane >> 2;
     auto token = [&](int r) { return g_shift >= 0 ? r >> g_shift : r / v.G; };
 

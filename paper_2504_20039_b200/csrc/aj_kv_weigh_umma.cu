@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(THREADS, 1) weigh_umma_kernel(const __grid_con
     float *neg = reinterpret_cast<float *>(smem + C::NEG_AT);
     int *row_slot = reinterpret_cast<int *>(neg + ROWS);
     long long *pre = reinterpret_cast<long long *>(smem + C::PRE_AT);  // [B + 1]
-    const View &v = a.v;
+    const CacheView &v = a.v;
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
